@@ -63,7 +63,7 @@
 extern "C" {
 #endif
 
-#define SNN_ABI_VERSION 11
+#define SNN_ABI_VERSION 12
 
 typedef enum snn_status {
     SNN_OK = 0,
@@ -461,6 +461,157 @@ size_t snn_layer_dcur_t_bytes(const snn_layer_desc *d);
 #define SNN_DCUR_T_TRANSPOSED 1
 #define SNN_DCUR_T_PLANES 2
 int32_t snn_layer_dcur_t_layout(const snn_layer_desc *d);
+
+/* ---- leaky sequence block ---------------------------------------------------
+ * Operators of a sequence model built from the same leaky integration as the
+ * neurons above: a state that decays and adds its input once per step, here a
+ * matrix per head, with the norms, gate and residual that stand around it.
+ *
+ * Linear attention with a decay per head.  Per sequence and head, with query
+ * q_t, key k_t (d_k values), value v_t (d_v values), decay g and fp32 state S:
+ *     S_t = g S_{t-1} + k_t^T v_t          (d_k x d_v, S_{-1} = state_in)
+ *     o_t = scale q_t S_t
+ * q [T,B,heads,d_k], k [T,B,kv_heads,d_k], v [T,B,kv_heads,d_v] and
+ * o [T,B,heads,d_v] are strided: element (t,b,h,i) lies at
+ * t stride[0] + b stride[1] + h stride[2] + i, so they may be slices of one
+ * packed projection.  Query head h reads key and value head
+ * h / (heads / kv_heads).  Gradients have their tensors' strides.
+ *
+ * lens (device int32 [B], or NULL: every sequence has T tokens) gives each
+ * sequence's length, taken as within [0, T]; tokens at and past it are not
+ * read, their outputs and gradients are 0, and the state ends at the last token
+ * before it.  A token never reaches an earlier token's output, whatever its
+ * values (infinities and NaN included).  Sums and the state are fp32; 16-bit
+ * operands are multiplied exactly, and where a score or the state becomes an
+ * operand of a 16-bit product it is held as two parts (the state's update: as
+ * many as keep fp32's precision). */
+typedef struct snn_linattn_desc {
+    int32_t T, B;            /* tokens, sequences (snn_linattn_step: T = 1) */
+    int32_t heads, kv_heads; /* kv_heads divides heads */
+    int32_t d_k, d_v;        /* multiples of 8, 8 .. 128 */
+    int32_t dtype;           /* q, k, v, o and their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
+    float scale;             /* finite */
+    int64_t q_stride[3];     /* elements, multiples of 8, >= 0: time, sequence, head */
+    int64_t k_stride[3], v_stride[3], o_stride[3];
+} snn_linattn_desc;
+
+/* Scratch bytes of snn_linattn_fwd and snn_linattn_bwd (the larger).  0 for an
+ * invalid descriptor, and a valid answer. */
+size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d);
+
+/* Whole sequences (a prompt, or the forward of a training step).
+ *   decay     fp32 [heads], finite, meant for [0, 1]
+ *   state_in  fp32 [B,heads,d_k,d_v], or NULL for zeros
+ *   state_out fp32 [B,heads,d_k,d_v], or NULL; may be state_in
+ * T == 0 copies the state; heads and B may be 0 (no work). */
+snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void *k,
+                           const void *v, const float *decay, const int32_t *lens,
+                           const float *state_in, void *o, float *state_out, void *ws,
+                           size_t ws_bytes, hipStream_t stream);
+
+/* Backward: with R_t = g R_{t+1} + scale q_t^T do_t the gradient of S_t (that
+ * of the last token's state adds grad_state_out),
+ *     dq_t = scale do_t S_t^T,  dk_t = v_t R_t^T,  dv_t = k_t R_t,
+ *     grad_state_in = g R_0 (grad_state_out itself over no tokens),
+ * dk and dv summed over the query heads that share the key head.  The decay
+ * is a constant, as the neurons' beta is.
+ *   grad_o          strides of o
+ *   grad_state_out  fp32 [B,heads,d_k,d_v], or NULL for zeros
+ *   grad_q, grad_k, grad_v  strides of q, k, v; all required
+ *   grad_state_in   fp32, or NULL to skip; may be grad_state_out */
+snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void *k,
+                           const void *v, const float *decay, const int32_t *lens,
+                           const float *state_in, const void *grad_o,
+                           const float *grad_state_out, void *grad_q, void *grad_k,
+                           void *grad_v, float *grad_state_in, void *ws, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* One token of every running request (d->T = 1, d->B requests).
+ *   slots     device int32 [B], or NULL for request b in slot b: the slot of
+ *             request b in the pools.  A slot outside [0, n_slots) makes the
+ *             request idle: its output is 0 and no state is touched.  Two
+ *             requests must not share a slot.
+ *   state_in, state_out  fp32 [n_slots,heads,d_k,d_v], both required; may be
+ *             the same pool (in place).  Only the requests' slots of state_out
+ *             are written. */
+snn_status snn_linattn_step(const snn_linattn_desc *d, const void *q, const void *k,
+                            const void *v, const float *decay, const int32_t *slots,
+                            int32_t n_slots, const float *state_in, float *state_out, void *o,
+                            hipStream_t stream);
+
+/* The norms before and after a block, its gate and its residual scale, per row
+ * of n channels (x the residual stream, y the block's output):
+ *     u     = y / sqrt(mean(y^2) + eps) w_post     mean over each of `groups`
+ *                                                  equal parts of the row
+ *     x_out = x + scale u act(gate)
+ *     h     = x_out / sqrt(mean(x_out^2) + eps) w_pre   over the whole row,
+ *                                                  the next block's input
+ * with act the identity (SNN_GATE_MUL: a spike or a factor), 1 / (1 + e^-g)
+ * (SNN_GATE_SIGMOID), or g / (1 + e^-g) (SNN_GATE_SILU).  The row tensors are
+ * strided over rows (ld_* elements) and need only their element's alignment.
+ * Arithmetic is fp32, each output rounded once. */
+#define SNN_GATE_NONE 0
+#define SNN_GATE_MUL 1
+#define SNN_GATE_SIGMOID 2
+#define SNN_GATE_SILU 3
+
+typedef struct snn_gate_norm_desc {
+    int32_t rows, n;     /* n 1 .. 16384 */
+    int32_t groups;      /* divides n; n / groups a multiple of 8 unless groups = 1 */
+    int32_t gate;        /* SNN_GATE_* */
+    int32_t x_dtype;     /* x, x_out, their gradients: SNN_F32, or y_dtype */
+    int32_t y_dtype;     /* y, gate, h, their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
+    float eps;           /* > 0 */
+    int32_t reserved;    /* 0 */
+    int64_t ld_x, ld_y, ld_g, ld_h; /* row strides, >= n, of x and x_out; y; gate; h,
+                                       and of their gradients (ld_g: ignored for
+                                       SNN_GATE_NONE) */
+} snn_gate_norm_desc;
+
+/* Scratch bytes of snn_gate_norm_bwd. */
+size_t snn_gate_norm_workspace_bytes(const snn_gate_norm_desc *d);
+
+/* x required.  y NULL: no block's output yet, h = norm(x) alone; gate, scale,
+ * x_out and the checkpoints must then be NULL and the gate SNN_GATE_NONE.
+ * Else x_out is required and gate iff d->gate is not SNN_GATE_NONE.  h NULL:
+ * no norm follows.  w_post, scale, w_pre: fp32 [n], or NULL for ones.
+ * y_ckpt, gate_ckpt (nullable; snn_checkpoint_bytes(rows, n) each, 16-byte
+ * aligned): receive y and the gate as 8-bit checkpoints.  x_out may be x. */
+snn_status snn_gate_norm_fwd(const snn_gate_norm_desc *d, const void *x, const void *y,
+                             const void *gate, const float *w_post, const float *scale,
+                             const float *w_pre, void *x_out, void *h, void *y_ckpt,
+                             void *gate_ckpt, hipStream_t stream);
+
+/* Backward.  x_out: what the forward wrote (x where it was called without y),
+ * NULL where grad_h is.  grad_x_out, grad_h: gradients of x_out and h; either
+ * may be NULL (zero), not both.  y and gate as in the forward, or both NULL
+ * and y_ckpt (and gate_ckpt for a gated block) in their place: the gradient is
+ * then taken at the values the checkpoints stand for, norms included.
+ * grad_x (may be grad_x_out) is required, grad_y where y is, grad_gate where
+ * the gate is; grad_w_post, grad_scale, grad_w_pre (fp32 [n], sums over the
+ * rows in a fixed order) may be NULL, and must be where what they belong to
+ * is absent (w_post, scale: y; w_pre: grad_h).  ws: as queried. */
+snn_status snn_gate_norm_bwd(const snn_gate_norm_desc *d, const void *grad_x_out,
+                             const void *grad_h, const void *x_out, const void *y,
+                             const void *gate, const void *y_ckpt, const void *gate_ckpt,
+                             const float *w_post, const float *scale, const float *w_pre,
+                             void *grad_x, void *grad_y, void *grad_gate, float *grad_w_post,
+                             float *grad_scale, float *grad_w_pre, void *ws, size_t ws_bytes,
+                             hipStream_t stream);
+
+/* Activation checkpoints in 8 bits: rows of n values in blocks of 128 (the
+ * last may be shorter), each with one fp32 scale:
+ *     scale = fl(m fl(1/127)),  code = rint(fl(x fl(127 / m))),  m = max |x|,
+ * and a code stands for fl(code scale): at most m / 254 away (and fp32
+ * rounding).  m < 2^-100 is held as zeros; a block with an infinity or a NaN
+ * reads back as NaN.  The buffer holds int8 codes [rows][n], then from the next
+ * multiple of 256 bytes fp32 scales [rows][ceil(n / 128)]. */
+size_t snn_checkpoint_bytes(int32_t rows, int32_t n); /* 0 for negative sizes */
+snn_status snn_checkpoint_save(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
+                               const void *x, void *ckpt, hipStream_t stream);
+/* x of dtype (SNN_F32 | SNN_F16 | SNN_BF16), each value rounded once. */
+snn_status snn_checkpoint_load(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
+                               const void *ckpt, void *x, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -32,8 +32,9 @@ RESET_DETACHED, RESET_SURROGATE = 0, 1
 GRAD_FULL, GRAD_BCAST, GRAD_FOLD = 0, 1, 2
 LOSS_CE_COUNT, LOSS_MSE_COUNT = 0, 1
 FLAG_FP32_MFMA = 1
-ABI_VERSION = 11
+ABI_VERSION = 12
 DCUR_T_TRANSPOSED, DCUR_T_PLANES = 1, 2
+GATE_NONE, GATE_MUL, GATE_SIGMOID, GATE_SILU = 0, 1, 2, 3
 
 STATUS = {0: "SNN_OK", 1: "SNN_ERR_NULL", 2: "SNN_ERR_SHAPE", 3: "SNN_ERR_DTYPE",
           4: "SNN_ERR_ALIGN", 5: "SNN_ERR_UNSUPPORTED", 6: "SNN_ERR_WORKSPACE",
@@ -44,7 +45,11 @@ EXPORTS = ["snn_abi_version", "snn_status_str", "snn_layer_saved_bytes",
            "snn_loss_workspace_bytes", "snn_loss", "snn_synapse_fwd", "snn_neuron_fwd",
            "snn_neuron_bwd", "snn_synapse_bwd", "snn_adamw", "snn_loss_noalloc",
            "snn_layer_saved_layout", "snn_layer_dcur_t_bytes", "snn_layer_dcur_t_layout",
-           "snn_fused_step_check", "snn_fused_step_workspace_bytes", "snn_fused_step"]
+           "snn_fused_step_check", "snn_fused_step_workspace_bytes", "snn_fused_step",
+           "snn_linattn_workspace_bytes", "snn_linattn_fwd", "snn_linattn_bwd",
+           "snn_linattn_step", "snn_gate_norm_workspace_bytes", "snn_gate_norm_fwd",
+           "snn_gate_norm_bwd", "snn_checkpoint_bytes", "snn_checkpoint_save",
+           "snn_checkpoint_load"]
 
 
 class LayerDesc(ctypes.Structure):
@@ -97,6 +102,22 @@ class AdamwHparams(ctypes.Structure):
                 ("step", ctypes.c_int32)]
 
 
+class LinattnDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3)]
+
+
+class GateNormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("n", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("gate", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("y_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("ld_x", ctypes.c_int64),
+                ("ld_y", ctypes.c_int64), ("ld_g", ctypes.c_int64), ("ld_h", ctypes.c_int64)]
+
+
 class SNNError(RuntimeError):
     def __init__(self, fn, status):
         self.status = status
@@ -118,7 +139,8 @@ def lib():
     P, S = ctypes.c_void_p, ctypes.c_size_t
     D = ctypes.POINTER(LayerDesc)
     G = ctypes.POINTER(GradIn)
-    i32 = ctypes.c_int32
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    LA, GN = ctypes.POINTER(LinattnDesc), ctypes.POINTER(GateNormDesc)
     sig = {
         "snn_abi_version": ([], ctypes.c_int),
         "snn_status_str": ([ctypes.c_int], ctypes.c_char_p),
@@ -141,6 +163,16 @@ def lib():
         "snn_fused_step": ([ctypes.POINTER(FusedDesc)] + [P] * 16 + [S, P], ctypes.c_int),
         "snn_adamw": ([ctypes.POINTER(AdamwTensor), i32, ctypes.POINTER(AdamwHparams), P],
                       ctypes.c_int),
+        "snn_linattn_workspace_bytes": ([LA], S),
+        "snn_linattn_fwd": ([LA] + [P] * 9 + [S, P], ctypes.c_int),
+        "snn_linattn_bwd": ([LA] + [P] * 13 + [S, P], ctypes.c_int),
+        "snn_linattn_step": ([LA] + [P] * 5 + [i32] + [P] * 4, ctypes.c_int),
+        "snn_gate_norm_workspace_bytes": ([GN], S),
+        "snn_gate_norm_fwd": ([GN] + [P] * 11, ctypes.c_int),
+        "snn_gate_norm_bwd": ([GN] + [P] * 17 + [S, P], ctypes.c_int),
+        "snn_checkpoint_bytes": ([i32, i32], S),
+        "snn_checkpoint_save": ([i32, i32, i64, i32, P, P, P], ctypes.c_int),
+        "snn_checkpoint_load": ([i32, i32, i64, i32, P, P, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -413,6 +445,227 @@ def snn_adamw(tensors, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay
         arr[i] = AdamwTensor(_p(p), _p(g), _p(m), _p(v), _p(h), p.numel())
     hp = AdamwHparams(lr, betas[0], betas[1], eps, weight_decay, step)
     _check("snn_adamw", lib().snn_adamw(arr, len(tensors), ctypes.byref(hp), _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# leaky sequence block
+# --------------------------------------------------------------------------
+def linattn_desc(q, k, v, o, scale=None) -> LinattnDesc:
+    """Descriptor of linear attention over q [T,B,heads,d_k], k [T,B,kv_heads,d_k],
+    v [T,B,kv_heads,d_v] and o [T,B,heads,d_v]: tensors of one dtype, each row
+    contiguous, strided over time, sequence and head (scale: 1/sqrt(d_k) if None).
+    Later calls may pass other tensors of the same shapes and strides."""
+    T, B, H, DK = q.shape
+    KV, DV = k.shape[2], v.shape[3]
+    if k.shape != (T, B, KV, DK) or v.shape != (T, B, KV, DV) or o.shape != (T, B, H, DV):
+        raise ValueError(f"linattn_desc: shapes {tuple(q.shape)}, {tuple(k.shape)}, "
+                         f"{tuple(v.shape)}, {tuple(o.shape)} do not go together")
+    if any(t.dtype != q.dtype for t in (k, v, o)):
+        raise ValueError("linattn_desc: q, k, v and o must have one dtype")
+    if any(t.stride(3) != 1 and t.shape[3] > 1 and t.numel() for t in (q, k, v, o)):
+        raise ValueError("linattn_desc: each head's values must be contiguous")
+    S = ctypes.c_int64 * 3
+    return LinattnDesc(T, B, H, KV, DK, DV, _dtype_code(q), DK ** -0.5 if scale is None else scale,
+                       *(S(*t.stride()[:3]) if t.numel() else S() for t in (q, k, v, o)))
+
+
+def _need_heads(fn, what, t, d, heads, width, stride):
+    """A strided argument of the shape, type and strides the descriptor has."""
+    if t is None or isinstance(t, int):
+        return
+    if tuple(t.shape) != (d.T, d.B, heads, width) or _dtype_code(t) != d.dtype or \
+            (t.numel() and (t.stride(3) != 1 or any(
+                n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), stride)))):
+        raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is "
+                         "not what the descriptor says")
+
+
+def _need_linattn(fn, d, q, k, v, o, decay, names=("q", "k", "v", "o")):
+    _need_heads(fn, names[0], q, d, d.heads, d.d_k, d.q_stride)
+    _need_heads(fn, names[1], k, d, d.kv_heads, d.d_k, d.k_stride)
+    _need_heads(fn, names[2], v, d, d.kv_heads, d.d_v, d.v_stride)
+    _need_heads(fn, names[3], o, d, d.heads, d.d_v, d.o_stride)
+    _need_array(fn, decay, F32, d.heads, "decay")
+
+
+def _need_array(fn, t, dtype_code, count, what):
+    """_need for an argument that must also be contiguous and of the type itself."""
+    if t is None or isinstance(t, int):
+        return
+    _need(fn, t, dtype_code, count, what)
+    if not t.is_contiguous() or t.is_floating_point() != (dtype_code == F32):
+        raise ValueError(f"{fn}: {what} must be contiguous and of its type, got {t.dtype}")
+
+
+def snn_linattn_workspace_bytes(desc: LinattnDesc) -> int:
+    return int(lib().snn_linattn_workspace_bytes(ctypes.byref(desc)))
+
+
+def snn_linattn_fwd(desc, q, k, v, decay, lens, state_in, o, state_out, ws, stream=None):
+    """Whole sequences: o and, where given, the state after each (from state_in,
+    or zeros).  lens: int32 [B] lengths, or None."""
+    fn, S = "snn_linattn_fwd", desc.B * desc.heads * desc.d_k * desc.d_v
+    _need_linattn(fn, desc, q, k, v, o, decay)
+    _need_array(fn, lens, I32, desc.B, "lens")
+    _need_array(fn, state_in, F32, S, "state_in")
+    _need_array(fn, state_out, F32, S, "state_out")
+    _check(fn, lib().snn_linattn_fwd(
+        ctypes.byref(desc), _p(q), _p(k), _p(v), _p(decay), _p(lens), _p(state_in), _p(o),
+        _p(state_out), _p(ws), _nbytes(ws), _stream(stream)))
+
+
+def snn_linattn_bwd(desc, q, k, v, decay, lens, state_in, grad_o, grad_state_out, grad_q, grad_k,
+                    grad_v, grad_state_in, ws, stream=None):
+    fn, S = "snn_linattn_bwd", desc.B * desc.heads * desc.d_k * desc.d_v
+    _need_linattn(fn, desc, q, k, v, grad_o, decay, ("q", "k", "v", "grad_o"))
+    _need_linattn(fn, desc, grad_q, grad_k, grad_v, None, None, ("grad_q", "grad_k", "grad_v", ""))
+    _need_array(fn, lens, I32, desc.B, "lens")
+    _need_array(fn, state_in, F32, S, "state_in")
+    _need_array(fn, grad_state_out, F32, S, "grad_state_out")
+    _need_array(fn, grad_state_in, F32, S, "grad_state_in")
+    _check(fn, lib().snn_linattn_bwd(
+        ctypes.byref(desc), _p(q), _p(k), _p(v), _p(decay), _p(lens), _p(state_in), _p(grad_o),
+        _p(grad_state_out), _p(grad_q), _p(grad_k), _p(grad_v), _p(grad_state_in), _p(ws),
+        _nbytes(ws), _stream(stream)))
+
+
+def snn_linattn_step(desc, q, k, v, decay, slots, state_in, state_out, o, stream=None):
+    """One token of every request; states [n_slots, heads, d_k, d_v] in pools
+    (one and the same for an update in place), slots int32 [B] or None."""
+    fn, n_slots = "snn_linattn_step", state_in.shape[0]
+    S = n_slots * desc.heads * desc.d_k * desc.d_v
+    _need_linattn(fn, desc, q, k, v, o, decay)
+    _need_array(fn, slots, I32, desc.B, "slots")
+    _need_array(fn, state_in, F32, S, "state_in")
+    _need_array(fn, state_out, F32, S, "state_out")
+    _check(fn, lib().snn_linattn_step(
+        ctypes.byref(desc), _p(q), _p(k), _p(v), _p(decay), _p(slots), n_slots, _p(state_in),
+        _p(state_out), _p(o), _stream(stream)))
+
+
+_GATE = {"none": GATE_NONE, "mul": GATE_MUL, "sigmoid": GATE_SIGMOID, "silu": GATE_SILU}
+
+
+def _row_stride(t):
+    """Row stride of a tensor [..., n] whose leading dimensions are one row index."""
+    n, st = t.shape, t.stride()
+    if t.numel() == 0:
+        return max(n[-1], 1)
+    if n[-1] > 1 and st[-1] != 1:
+        raise ValueError("row tensors must be contiguous within a row")
+    ld, rows = None, 1
+    for size, s in zip(n[-2::-1], st[-2::-1]):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = s
+        elif s != ld * rows:
+            raise ValueError(f"rows of a tensor of shape {tuple(n)} and strides {st} have no "
+                             "single stride")
+        rows *= size
+    return max(n[-1], 1) if ld is None else ld
+
+
+def gate_norm_desc(x, y=None, gate=None, groups=1, act="none", eps=1e-6, h=None) -> GateNormDesc:
+    """Descriptor of the norms around a block: x [..., n] the residual stream, y
+    the block's output and gate (or None), with act "none", "mul", "sigmoid" or
+    "silu"; y's norm is taken over each of `groups` parts of a row.  Later calls
+    may pass other tensors of the same strides; x_out has x's, h those of the h
+    given here (contiguous rows of y's dtype, or x's without y, if None)."""
+    n = x.shape[-1]
+    rows = x.numel() // n if n else 0
+    for t in (y, gate, h):
+        if t is not None and t.shape != x.shape:
+            raise ValueError(f"gate_norm_desc: shapes {tuple(x.shape)} and {tuple(t.shape)}")
+    yt = _dtype_code(y if y is not None else h if h is not None else x)
+    return GateNormDesc(rows, n, groups, _GATE[act], _dtype_code(x), yt, eps, 0, _row_stride(x),
+                        n if y is None else _row_stride(y),
+                        n if gate is None else _row_stride(gate),
+                        n if h is None else _row_stride(h))
+
+
+def _need_rows(fn, what, t, d, dtype_code, ld):
+    if t is None or isinstance(t, int):
+        return
+    rows = t.numel() // d.n
+    if t.shape[-1] != d.n or rows != d.rows or _dtype_code(t) != dtype_code or \
+            (rows > 1 and _row_stride(t) != ld):
+        raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is "
+                         "not what the descriptor says")
+
+
+def _need_ckpt(fn, what, t, rows, n):
+    if t is None or isinstance(t, int):
+        return
+    if not t.is_contiguous() or _nbytes(t) < snn_checkpoint_bytes(rows, n):
+        raise ValueError(f"{fn}: {what} needs {snn_checkpoint_bytes(rows, n)} contiguous bytes")
+
+
+def snn_gate_norm_workspace_bytes(desc: GateNormDesc) -> int:
+    return int(lib().snn_gate_norm_workspace_bytes(ctypes.byref(desc)))
+
+
+def snn_gate_norm_fwd(desc, x, y, gate, w_post, scale, w_pre, x_out, h, y_ckpt=None,
+                      gate_ckpt=None, stream=None):
+    """x_out = x + scale norm(y) w_post act(gate) and h = norm(x_out) w_pre (y
+    None: h = norm(x) w_pre alone), with y and the gate stored in 8 bits where
+    y_ckpt and gate_ckpt are given."""
+    fn, d = "snn_gate_norm_fwd", desc
+    for what, t in (("x", x), ("x_out", x_out)):
+        _need_rows(fn, what, t, d, d.x_dtype, d.ld_x)
+    for what, t, ld in (("y", y, d.ld_y), ("gate", gate, d.ld_g), ("h", h, d.ld_h)):
+        _need_rows(fn, what, t, d, d.y_dtype, ld)
+    for what, t in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
+        _need_array(fn, t, F32, d.n, what)
+    for what, t in (("y_ckpt", y_ckpt), ("gate_ckpt", gate_ckpt)):
+        _need_ckpt(fn, what, t, d.rows, d.n)
+    _check(fn, lib().snn_gate_norm_fwd(
+        ctypes.byref(d), _p(x), _p(y), _p(gate), _p(w_post), _p(scale), _p(w_pre), _p(x_out),
+        _p(h), _p(y_ckpt), _p(gate_ckpt), _stream(stream)))
+
+
+def snn_gate_norm_bwd(desc, grad_x_out, grad_h, x_out, y, gate, y_ckpt, gate_ckpt, w_post, scale,
+                      w_pre, grad_x, grad_y, grad_gate, grad_w_post, grad_scale, grad_w_pre, ws,
+                      stream=None):
+    """The backward of snn_gate_norm_fwd, from y and gate or from their 8-bit
+    checkpoints."""
+    fn, d = "snn_gate_norm_bwd", desc
+    for what, t in (("grad_x_out", grad_x_out), ("x_out", x_out), ("grad_x", grad_x)):
+        _need_rows(fn, what, t, d, d.x_dtype, d.ld_x)
+    for what, t, ld in (("y", y, d.ld_y), ("grad_y", grad_y, d.ld_y), ("gate", gate, d.ld_g),
+                        ("grad_gate", grad_gate, d.ld_g), ("grad_h", grad_h, d.ld_h)):
+        _need_rows(fn, what, t, d, d.y_dtype, ld)
+    for what, t in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre),
+                    ("grad_w_post", grad_w_post), ("grad_scale", grad_scale),
+                    ("grad_w_pre", grad_w_pre)):
+        _need_array(fn, t, F32, d.n, what)
+    for what, t in (("y_ckpt", y_ckpt), ("gate_ckpt", gate_ckpt)):
+        _need_ckpt(fn, what, t, d.rows, d.n)
+    _check(fn, lib().snn_gate_norm_bwd(
+        ctypes.byref(d), _p(grad_x_out), _p(grad_h), _p(x_out), _p(y), _p(gate), _p(y_ckpt),
+        _p(gate_ckpt), _p(w_post), _p(scale), _p(w_pre), _p(grad_x), _p(grad_y), _p(grad_gate),
+        _p(grad_w_post), _p(grad_scale), _p(grad_w_pre), _p(ws), _nbytes(ws), _stream(stream)))
+
+
+def snn_checkpoint_bytes(rows: int, n: int) -> int:
+    return int(lib().snn_checkpoint_bytes(rows, n))
+
+
+def _checkpoint(fn, x, ckpt, args, stream):
+    n = x.shape[-1]
+    rows = x.numel() // n if n else 0
+    _need_ckpt(fn, "ckpt", ckpt, rows, n)
+    _check(fn, getattr(lib(), fn)(rows, n, _row_stride(x), _dtype_code(x), *args, _stream(stream)))
+
+
+def snn_checkpoint_save(x, ckpt, stream=None):
+    """Stores x [..., n] in 8 bits in ckpt (snn_checkpoint_bytes(rows, n) bytes)."""
+    _checkpoint("snn_checkpoint_save", x, ckpt, (_p(x), _p(ckpt)), stream)
+
+
+def snn_checkpoint_load(ckpt, x, stream=None):
+    """Reads the checkpoint of x's shape back into x (any of its dtypes)."""
+    _checkpoint("snn_checkpoint_load", x, ckpt, (_p(ckpt), _p(x)), stream)
 
 
 # --------------------------------------------------------------------------

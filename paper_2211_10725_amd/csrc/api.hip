@@ -3,6 +3,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <initializer_list>
+
 #include "snn_internal.hpp"
 
 using namespace snn;
@@ -875,6 +877,344 @@ snn_status snn_adamw(const snn_adamw_tensor *tensors, int32_t count,
     if (!any) return SNN_OK;
     (void)hipGetLastError();
     return hip_status(launch_adamw(tensors, count, c, stream));
+}
+
+}  // extern "C"
+
+// ---- leaky sequence block ----------------------------------------------------
+
+namespace {
+
+bool float_dtype(int dt) { return dt == SNN_F32 || dt == SNN_F16 || dt == SNN_BF16; }
+
+snn_status check_linattn(const snn_linattn_desc *d) {
+    if (!d) return SNN_ERR_NULL;
+    if (d->T < 0 || d->B < 0 || d->heads < 0 || d->kv_heads < 0) return SNN_ERR_SHAPE;
+    if (d->heads > 0 && (d->kv_heads < 1 || d->heads % d->kv_heads != 0)) return SNN_ERR_SHAPE;
+    if (d->d_k < 8 || d->d_k > kLaMaxD || d->d_k % 8 != 0 || d->d_v < 8 || d->d_v > kLaMaxD ||
+        d->d_v % 8 != 0)
+        return SNN_ERR_SHAPE;
+    if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
+    if (!finite(d->scale)) return SNN_ERR_SHAPE;
+    // grids of at most 2^31 workgroups, element offsets far inside 63 bits
+    if ((int64_t)d->B * d->heads > ((int64_t)1 << 24) ||
+        (int64_t)d->T * d->B * d->heads > ((int64_t)1 << 34))
+        return SNN_ERR_SHAPE;
+    const int64_t *strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
+    for (const int64_t *st : strides)
+        for (int i = 0; i < 3; ++i)
+            if (st[i] < 0 || st[i] % 8 != 0 || st[i] > ((int64_t)1 << 32)) return SNN_ERR_SHAPE;
+    return SNN_OK;
+}
+
+bool any_misaligned(std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if (!aligned16(p)) return true;
+    return false;
+}
+
+LaOperand operand(const void *p, const int64_t *st, int share) {
+    return LaOperand{p, st[0], st[1], st[2], share};
+}
+
+void set_out(LaRole &r, void *o, const int64_t *st) {
+    r.o = o;
+    r.ot = st[0];
+    r.ob = st[1];
+    r.oh = st[2];
+}
+
+// fp32 gradient of a shared key or value head, one per query head: [T,B,heads,d]
+size_t shared_grad_bytes(const snn_linattn_desc *d, int width) {
+    if (d->heads == d->kv_heads) return 0;
+    return align_up((size_t)d->T * d->B * d->heads * width * sizeof(float));
+}
+
+snn_status check_gate_norm(const snn_gate_norm_desc *d) {
+    if (!d) return SNN_ERR_NULL;
+    if (d->rows < 0 || d->n < 1 || d->n > kGateNormMaxN || d->groups < 1 ||
+        d->n % d->groups != 0 || (d->groups > 1 && (d->n / d->groups) % 8 != 0))
+        return SNN_ERR_SHAPE;
+    if (d->gate < SNN_GATE_NONE || d->gate > SNN_GATE_SILU || d->reserved != 0)
+        return SNN_ERR_UNSUPPORTED;
+    if (!float_dtype(d->y_dtype) || (d->x_dtype != SNN_F32 && d->x_dtype != d->y_dtype))
+        return SNN_ERR_DTYPE;
+    if (!finite(d->eps) || !(d->eps > 0.f)) return SNN_ERR_SHAPE;
+    const int64_t most = (int64_t)1 << 32;
+    for (int64_t ld : {d->ld_x, d->ld_y, d->gate == SNN_GATE_NONE ? d->ld_y : d->ld_g, d->ld_h})
+        if (ld < d->n || ld > most) return SNN_ERR_SHAPE;
+    return SNN_OK;
+}
+
+// whether every pointer has its element's alignment
+bool any_misaligned_rows(int dt, std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if ((uintptr_t)p % dtype_bytes(dt) != 0) return true;
+    return false;
+}
+
+GateNorm gate_norm_args(const snn_gate_norm_desc *d, const float *w_post, const float *scale,
+                        const float *w_pre) {
+    return GateNorm{d->rows, d->n, d->groups, d->gate, d->eps, d->ld_x, d->ld_y, d->ld_g, d->ld_h,
+                    w_post, scale, w_pre};
+}
+
+float *ckpt_scales(const void *ckpt, int64_t rows, int64_t n) {
+    return (float *)((char *)ckpt + ckpt_scale_offset(rows, n));
+}
+
+snn_status check_checkpoint(int32_t rows, int32_t n, int64_t ld, int32_t dtype, const void *x,
+                            const void *ckpt) {
+    if (rows < 0 || n < 0 || ld < n || ld > ((int64_t)1 << 32)) return SNN_ERR_SHAPE;
+    if (rows * ckpt_blocks(n) > INT32_MAX) return SNN_ERR_SHAPE;
+    if (!float_dtype(dtype)) return SNN_ERR_DTYPE;
+    if (rows == 0 || n == 0) return SNN_OK;
+    if (!x || !ckpt) return SNN_ERR_NULL;
+    if (!aligned16(ckpt) || any_misaligned_rows(dtype, {x})) return SNN_ERR_ALIGN;
+    return SNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d) {
+    if (check_linattn(d) != SNN_OK) return 0;
+    return shared_grad_bytes(d, d->d_k) + shared_grad_bytes(d, d->d_v);
+}
+
+snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void *k,
+                           const void *v, const float *decay, const int32_t *lens,
+                           const float *state_in, void *o, float *state_out, void *ws,
+                           size_t ws_bytes, hipStream_t stream) {
+    const snn_status st = check_linattn(d);
+    if (st != SNN_OK) return st;
+    if (d->B == 0 || d->heads == 0) return SNN_OK;
+    if (!decay || (d->T > 0 && (!q || !k || !v || !o))) return SNN_ERR_NULL;
+    if (any_misaligned({q, k, v, decay, lens, state_in, o, state_out, ws})) return SNN_ERR_ALIGN;
+    const size_t need = snn_linattn_workspace_bytes(d);
+    if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    LaCall c{};
+    c.decay = decay;
+    c.lens = lens;
+    c.T = d->T;
+    c.B = d->B;
+    c.H = d->heads;
+    const int share = d->heads / d->kv_heads;
+    LaRole &r = c.role[0];
+    r.q = operand(q, d->q_stride, 1);
+    r.k = operand(k, d->k_stride, share);
+    r.v = operand(v, d->v_stride, share);
+    r.dk = d->d_k;
+    r.dv = d->d_v;
+    set_out(r, o, d->o_stride);
+    r.init = state_in;
+    r.final_state = state_out;
+    r.first = 1;
+    r.rs = d->scale;
+    r.ws = 1.f;
+    (void)hipGetLastError();
+    return hip_status(launch_linattn(c, 1, d->dtype, stream));
+}
+
+snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void *k,
+                           const void *v, const float *decay, const int32_t *lens,
+                           const float *state_in, const void *grad_o,
+                           const float *grad_state_out, void *grad_q, void *grad_k,
+                           void *grad_v, float *grad_state_in, void *ws, size_t ws_bytes,
+                           hipStream_t stream) {
+    const snn_status st = check_linattn(d);
+    if (st != SNN_OK) return st;
+    if (d->B == 0 || d->heads == 0) return SNN_OK;
+    if (!decay || (d->T > 0 && (!q || !k || !v || !grad_o || !grad_q || !grad_k || !grad_v)))
+        return SNN_ERR_NULL;
+    if (any_misaligned({q, k, v, decay, lens, state_in, grad_o, grad_state_out, grad_q, grad_k,
+                        grad_v, grad_state_in, ws}))
+        return SNN_ERR_ALIGN;
+    const size_t need = snn_linattn_workspace_bytes(d);
+    if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    LaCall c{};
+    c.decay = decay;
+    c.lens = lens;
+    c.T = d->T;
+    c.B = d->B;
+    c.H = d->heads;
+    const int share = d->heads / d->kv_heads;
+    const LaOperand oq = operand(q, d->q_stride, 1), ok = operand(k, d->k_stride, share),
+                    ov = operand(v, d->v_stride, share), og = operand(grad_o, d->o_stride, 1);
+    float *pk = (float *)ws, *pv = (float *)((char *)ws + shared_grad_bytes(d, d->d_k));
+    auto shared_out = [&](LaRole &r, void *g, const int64_t *gs, float *part, int width) {
+        if (share == 1) return set_out(r, g, gs);
+        const int64_t st[3] = {(int64_t)d->B * d->heads * width, (int64_t)d->heads * width, width};
+        set_out(r, part, st);
+        r.o_f32 = 1;
+    };
+    LaRole &dq = c.role[0], &dk = c.role[1], &dv = c.role[2];
+    dq.q = og, dq.k = ov, dq.v = ok;
+    dq.dk = d->d_v, dq.dv = d->d_k;
+    set_out(dq, grad_q, d->q_stride);
+    dq.init = state_in;
+    dq.trans = 1;
+    dq.first = 1;
+    dq.rs = d->scale, dq.ws = 1.f;
+    dk.q = ov, dk.k = og, dk.v = oq;
+    dk.dk = d->d_v, dk.dv = d->d_k;
+    shared_out(dk, grad_k, d->k_stride, pk, d->d_k);
+    dk.init = grad_state_out;
+    dk.trans = 1;
+    dk.reverse = 1;
+    dk.rs = 1.f, dk.ws = d->scale;
+    dv.q = ok, dv.k = oq, dv.v = og;
+    dv.dk = d->d_k, dv.dv = d->d_v;
+    shared_out(dv, grad_v, d->v_stride, pv, d->d_v);
+    dv.init = grad_state_out;
+    dv.final_state = grad_state_in;
+    dv.reverse = 1;
+    dv.rs = 1.f, dv.ws = d->scale;
+    (void)hipGetLastError();
+    hipError_t e = launch_linattn(c, 3, d->dtype, stream);
+    if (e == hipSuccess && share > 1 && d->T > 0)
+        e = launch_group_sum(pk, grad_k, d->k_stride, d->T, d->B, d->kv_heads, share, d->d_k,
+                             d->dtype, stream);
+    if (e == hipSuccess && share > 1 && d->T > 0)
+        e = launch_group_sum(pv, grad_v, d->v_stride, d->T, d->B, d->kv_heads, share, d->d_v,
+                             d->dtype, stream);
+    return hip_status(e);
+}
+
+snn_status snn_linattn_step(const snn_linattn_desc *d, const void *q, const void *k,
+                            const void *v, const float *decay, const int32_t *slots,
+                            int32_t n_slots, const float *state_in, float *state_out, void *o,
+                            hipStream_t stream) {
+    const snn_status st = check_linattn(d);
+    if (st != SNN_OK) return st;
+    if (d->T != 1 || n_slots < 0 || (!slots && n_slots < d->B)) return SNN_ERR_SHAPE;
+    if (d->B == 0 || d->heads == 0) return SNN_OK;
+    if (!q || !k || !v || !decay || !state_in || !state_out || !o) return SNN_ERR_NULL;
+    if (any_misaligned({q, k, v, decay, slots, state_in, state_out, o})) return SNN_ERR_ALIGN;
+    const int share = d->heads / d->kv_heads;
+    LaStep c{};
+    c.q = operand(q, d->q_stride, 1);
+    c.k = operand(k, d->k_stride, share);
+    c.v = operand(v, d->v_stride, share);
+    c.dk = d->d_k;
+    c.dv = d->d_v;
+    c.H = d->heads;
+    c.n_slots = n_slots;
+    c.ob = d->o_stride[1];
+    c.oh = d->o_stride[2];
+    c.decay = decay;
+    c.in = state_in;
+    c.slots = slots;
+    c.out = state_out;
+    c.o = o;
+    c.scale = d->scale;
+    (void)hipGetLastError();
+    return hip_status(launch_linattn_step(c, d->B, d->dtype, stream));
+}
+
+size_t snn_gate_norm_workspace_bytes(const snn_gate_norm_desc *d) {
+    return check_gate_norm(d) == SNN_OK ? gate_norm_workspace_bytes(d->rows, d->n) : 0;
+}
+
+snn_status snn_gate_norm_fwd(const snn_gate_norm_desc *d, const void *x, const void *y,
+                             const void *gate, const float *w_post, const float *scale,
+                             const float *w_pre, void *x_out, void *h, void *y_ckpt,
+                             void *gate_ckpt, hipStream_t stream) {
+    const snn_status st = check_gate_norm(d);
+    if (st != SNN_OK) return st;
+    if (d->rows == 0) return SNN_OK;
+    const bool gated = d->gate != SNN_GATE_NONE;
+    if (!y && (gate || gated || w_post || scale || x_out || y_ckpt)) return SNN_ERR_UNSUPPORTED;
+    if ((gate && !gated) || (gate_ckpt && !gated)) return SNN_ERR_UNSUPPORTED;
+    if (!x || (y && !x_out) || (!y && !h) || (gated && !gate)) return SNN_ERR_NULL;
+    if (any_misaligned({w_post, scale, w_pre, y_ckpt, gate_ckpt}) ||
+        any_misaligned_rows(d->x_dtype, {x, x_out}) ||
+        any_misaligned_rows(d->y_dtype, {y, gate, h}))
+        return SNN_ERR_ALIGN;
+    GateNormFwd c{};
+    c.a = gate_norm_args(d, w_post, scale, w_pre);
+    c.x = x;
+    c.y = y;
+    c.g = gate;
+    c.x_out = x_out;
+    c.h = h;
+    if (y_ckpt) c.y8 = (int8_t *)y_ckpt, c.y8s = ckpt_scales(y_ckpt, d->rows, d->n);
+    if (gate_ckpt) c.g8 = (int8_t *)gate_ckpt, c.g8s = ckpt_scales(gate_ckpt, d->rows, d->n);
+    (void)hipGetLastError();
+    return hip_status(launch_gate_norm_fwd(c, d->x_dtype, d->y_dtype, stream));
+}
+
+snn_status snn_gate_norm_bwd(const snn_gate_norm_desc *d, const void *grad_x_out,
+                             const void *grad_h, const void *x_out, const void *y,
+                             const void *gate, const void *y_ckpt, const void *gate_ckpt,
+                             const float *w_post, const float *scale, const float *w_pre,
+                             void *grad_x, void *grad_y, void *grad_gate, float *grad_w_post,
+                             float *grad_scale, float *grad_w_pre, void *ws, size_t ws_bytes,
+                             hipStream_t stream) {
+    const snn_status st = check_gate_norm(d);
+    if (st != SNN_OK) return st;
+    const bool gated = d->gate != SNN_GATE_NONE, block = y || y_ckpt;
+    if (d->rows > 0) {  // without rows their pointers say nothing
+        if ((y && y_ckpt) || (gate && gate_ckpt) || ((gate || gate_ckpt || grad_gate) && !gated) ||
+            (gated && block && ((y && gate_ckpt) || (y_ckpt && gate))) ||
+            (!block && (gated || w_post || scale || grad_y || grad_w_post || grad_scale)) ||
+            (!grad_h && grad_w_pre))
+            return SNN_ERR_UNSUPPORTED;
+        if ((!grad_x_out && !grad_h) || (grad_h && !x_out) || !grad_x || (block && !grad_y) ||
+            (gated && (!grad_gate || (!gate && !gate_ckpt))))
+            return SNN_ERR_NULL;
+    }
+    if (any_misaligned({w_post, scale, w_pre, y_ckpt, gate_ckpt, grad_w_post, grad_scale,
+                        grad_w_pre, ws}) ||
+        any_misaligned_rows(d->x_dtype, {grad_x_out, x_out, grad_x}) ||
+        any_misaligned_rows(d->y_dtype, {grad_h, y, gate, grad_y, grad_gate}))
+        return SNN_ERR_ALIGN;
+    const size_t need = snn_gate_norm_workspace_bytes(d);
+    if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    GateNormBwd c{};
+    c.a = gate_norm_args(d, w_post, scale, w_pre);
+    c.dxo = grad_x_out;
+    c.dh = grad_h;
+    c.xo = x_out;
+    c.y = y;
+    c.g = gate;
+    if (y_ckpt) c.y8 = (const int8_t *)y_ckpt, c.y8s = ckpt_scales(y_ckpt, d->rows, d->n);
+    if (gate_ckpt)
+        c.g8 = (const int8_t *)gate_ckpt, c.g8s = ckpt_scales(gate_ckpt, d->rows, d->n);
+    c.dx = grad_x;
+    c.dy = grad_y;
+    c.dg = grad_gate;
+    c.dw_post = grad_w_post;
+    c.dscale = grad_scale;
+    c.dw_pre = grad_w_pre;
+    c.part = (float *)ws;
+    (void)hipGetLastError();
+    return hip_status(launch_gate_norm_bwd(c, d->x_dtype, d->y_dtype, stream));
+}
+
+size_t snn_checkpoint_bytes(int32_t rows, int32_t n) {
+    if (rows < 0 || n < 0) return 0;
+    return ckpt_scale_offset(rows, n) +
+           align_up((size_t)(rows * ckpt_blocks(n)) * sizeof(float));
+}
+
+snn_status snn_checkpoint_save(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
+                               const void *x, void *ckpt, hipStream_t stream) {
+    const snn_status st = check_checkpoint(rows, n, ld, dtype, x, ckpt);
+    if (st != SNN_OK || rows == 0 || n == 0) return st;
+    (void)hipGetLastError();
+    return hip_status(launch_checkpoint(rows, n, ld, dtype, (void *)x, (int8_t *)ckpt,
+                                        ckpt_scales(ckpt, rows, n), true, stream));
+}
+
+snn_status snn_checkpoint_load(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
+                               const void *ckpt, void *x, hipStream_t stream) {
+    const snn_status st = check_checkpoint(rows, n, ld, dtype, x, ckpt);
+    if (st != SNN_OK || rows == 0 || n == 0) return st;
+    (void)hipGetLastError();
+    return hip_status(launch_checkpoint(rows, n, ld, dtype, x, (int8_t *)ckpt,
+                                        ckpt_scales(ckpt, rows, n), false, stream));
 }
 
 }  // extern "C"

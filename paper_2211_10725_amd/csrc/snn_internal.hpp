@@ -301,4 +301,84 @@ struct FusedStep {
 };
 hipError_t launch_fused_step(const FusedStep &f, void *ws, hipStream_t s);
 
+// ---- linear attention with a decay per head (linattn.hip) ----------------------
+// One operand, element (t, b, h, i) at t st + b sb + (h / share) sh + i.
+struct LaOperand {
+    const void *p;
+    int64_t st, sb, sh;
+    int share;  // query heads that read the same head
+};
+// One recurrence over the tokens n = 0 .. len - 1 (token n from the end where
+// reverse): with X the state that enters token n (X = init before the first),
+//   S = first ? g X + ws k^T v : X + ws k^T v,  o = rs q S,  X' = first ? S : g S.
+struct LaRole {
+    LaOperand q, k, v;
+    int dk, dv;           // sizes of q and k, of v and o
+    void *o;
+    int64_t ot, ob, oh;   // o is strided like the operands, over every query head
+    int o_f32;            // o fp32 whatever the operands' type
+    const float *init;    // [B, H, dk, dv] (trans: [B, H, dv, dk]) or NULL
+    int trans;
+    float *final_state;   // X after the last token, [B, H, dk, dv], or NULL
+    int reverse, first;
+    float rs, ws;
+};
+constexpr int kLaRoles = 3;
+constexpr int kLaMaxD = 128;  // largest head size
+struct LaCall {
+    LaRole role[kLaRoles];
+    const float *decay;
+    const int32_t *lens;
+    int T, B, H;
+};
+hipError_t launch_linattn(const LaCall &c, int roles, int dtype, hipStream_t s);
+// dst (strided [T, B, KV, d] of dtype) = src fp32 [T, B, KV * share, d] summed
+// over each group of `share` heads
+hipError_t launch_group_sum(const float *src, void *dst, const int64_t *stride, int T, int B,
+                            int KV, int share, int d, int dtype, hipStream_t s);
+struct LaStep {
+    LaOperand q, k, v;
+    int dk, dv, H, n_slots;
+    int64_t ob, oh;
+    const float *decay, *in;
+    const int32_t *slots;
+    float *out;
+    void *o;
+    float scale;
+};
+hipError_t launch_linattn_step(const LaStep &c, int B, int dtype, hipStream_t s);
+
+// ---- gated norms and 8-bit checkpoints (gate_norm.hip) --------------------------
+constexpr int kGateNormMaxN = 16384;
+constexpr int kCkptBlock = 128;  // values that share a scale
+__host__ __device__ inline int64_t ckpt_blocks(int64_t n) { return (n + kCkptBlock - 1) / kCkptBlock; }
+inline size_t ckpt_scale_offset(int64_t rows, int64_t n) { return align_up((size_t)(rows * n)); }
+struct GateNorm {
+    int rows, n, groups, gate;
+    float eps;
+    int64_t ld_x, ld_y, ld_g, ld_h;
+    const float *w_post, *scale, *w_pre;
+};
+struct GateNormFwd {
+    GateNorm a;
+    const void *x, *y, *g;
+    void *x_out, *h;
+    int8_t *y8, *g8;   // codes; the scales follow
+    float *y8s, *g8s;
+};
+struct GateNormBwd {
+    GateNorm a;
+    const void *dxo, *dh, *xo, *y, *g;
+    const int8_t *y8, *g8;
+    const float *y8s, *g8s;
+    void *dx, *dy, *dg;
+    float *dw_post, *dscale, *dw_pre;
+    float *part;       // [3][blocks][n] column sums
+};
+hipError_t launch_gate_norm_fwd(const GateNormFwd &c, int xt, int yt, hipStream_t s);
+hipError_t launch_gate_norm_bwd(const GateNormBwd &c, int xt, int yt, hipStream_t s);
+size_t gate_norm_workspace_bytes(int64_t rows, int64_t n);
+hipError_t launch_checkpoint(int64_t rows, int n, int64_t ld, int dtype, void *x, int8_t *codes,
+                             float *scales, bool save, hipStream_t s);
+
 }  // namespace snn
