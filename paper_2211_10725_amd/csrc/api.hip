@@ -897,7 +897,7 @@ snn_status check_linattn(const snn_linattn_desc *d) {
     if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
     if (!finite(d->scale)) return SNN_ERR_SHAPE;
     // grids of at most 2^31 workgroups, element offsets far inside 63 bits
-    if ((int64_t)d->B * d->heads > ((int64_t)1 << 24) ||
+    if (d->T > ((int32_t)1 << 30) || (int64_t)d->B * d->heads > ((int64_t)1 << 24) ||
         (int64_t)d->T * d->B * d->heads > ((int64_t)1 << 34))
         return SNN_ERR_SHAPE;
     const int64_t *strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
@@ -922,6 +922,36 @@ void set_out(LaRole &r, void *o, const int64_t *st) {
     r.ot = st[0];
     r.ob = st[1];
     r.oh = st[2];
+}
+
+// bytes of one role's segment states, 0 where the sequences are not cut
+size_t segment_bytes(const snn_linattn_desc *d, const LaPlan &p) {
+    if (p.segs == 1) return 0;
+    return align_up((size_t)p.segs * d->B * d->heads * d->d_k * d->d_v * sizeof(float));
+}
+
+LaPlan plan_of(const snn_linattn_desc *d, int roles) {
+    return linattn_plan(d->T, (int64_t)d->B * d->heads, roles, std::max(d->d_k, d->d_v));
+}
+
+// the call's common part; ws takes the segments' states of `slots` roles
+LaCall linattn_call(const snn_linattn_desc *d, const float *decay, const int32_t *lens, int roles) {
+    LaCall c{};
+    c.decay = decay;
+    c.lens = lens;
+    c.T = d->T;
+    c.B = d->B;
+    c.H = d->heads;
+    c.roles = roles;
+    const LaPlan p = plan_of(d, roles);
+    c.segs = p.segs;
+    c.seg_len = p.seg_len;
+    return c;
+}
+
+void own_slots(const snn_linattn_desc *d, LaRole &r, void *slots) {
+    r.slot = (float *)slots;
+    r.slot_seg = (int64_t)d->B * d->heads * d->d_k * d->d_v;
 }
 
 // fp32 gradient of a shared key or value head, one per query head: [T,B,heads,d]
@@ -980,7 +1010,9 @@ extern "C" {
 
 size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d) {
     if (check_linattn(d) != SNN_OK) return 0;
-    return shared_grad_bytes(d, d->d_k) + shared_grad_bytes(d, d->d_v);
+    return std::max(segment_bytes(d, plan_of(d, 1)),
+                    2 * segment_bytes(d, plan_of(d, kLaRoles)) + shared_grad_bytes(d, d->d_k) +
+                        shared_grad_bytes(d, d->d_v));
 }
 
 snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void *k,
@@ -994,12 +1026,7 @@ snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void 
     if (any_misaligned({q, k, v, decay, lens, state_in, o, state_out, ws})) return SNN_ERR_ALIGN;
     const size_t need = snn_linattn_workspace_bytes(d);
     if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
-    LaCall c{};
-    c.decay = decay;
-    c.lens = lens;
-    c.T = d->T;
-    c.B = d->B;
-    c.H = d->heads;
+    LaCall c = linattn_call(d, decay, lens, 1);
     const int share = d->heads / d->kv_heads;
     LaRole &r = c.role[0];
     r.q = operand(q, d->q_stride, 1);
@@ -1013,8 +1040,9 @@ snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void 
     r.first = 1;
     r.rs = d->scale;
     r.ws = 1.f;
+    if (c.segs > 1) own_slots(d, r, ws);
     (void)hipGetLastError();
-    return hip_status(launch_linattn(c, 1, d->dtype, stream));
+    return hip_status(launch_linattn(c, d->dtype, stream));
 }
 
 snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void *k,
@@ -1033,16 +1061,13 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
         return SNN_ERR_ALIGN;
     const size_t need = snn_linattn_workspace_bytes(d);
     if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
-    LaCall c{};
-    c.decay = decay;
-    c.lens = lens;
-    c.T = d->T;
-    c.B = d->B;
-    c.H = d->heads;
+    LaCall c = linattn_call(d, decay, lens, kLaRoles);
     const int share = d->heads / d->kv_heads;
+    const size_t slots = segment_bytes(d, plan_of(d, kLaRoles));
     const LaOperand oq = operand(q, d->q_stride, 1), ok = operand(k, d->k_stride, share),
                     ov = operand(v, d->v_stride, share), og = operand(grad_o, d->o_stride, 1);
-    float *pk = (float *)ws, *pv = (float *)((char *)ws + shared_grad_bytes(d, d->d_k));
+    float *pk = (float *)((char *)ws + 2 * slots),
+          *pv = (float *)((char *)pk + shared_grad_bytes(d, d->d_k));
     auto shared_out = [&](LaRole &r, void *g, const int64_t *gs, float *part, int width) {
         if (share == 1) return set_out(r, g, gs);
         const int64_t st[3] = {(int64_t)d->B * d->heads * width, (int64_t)d->heads * width, width};
@@ -1071,8 +1096,13 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
     dv.final_state = grad_state_in;
     dv.reverse = 1;
     dv.rs = 1.f, dv.ws = d->scale;
+    if (c.segs > 1) {  // dk's states are dv's, transposed
+        own_slots(d, dq, ws);
+        own_slots(d, dv, (char *)ws + slots);
+        dk.slot_of = 2;
+    }
     (void)hipGetLastError();
-    hipError_t e = launch_linattn(c, 3, d->dtype, stream);
+    hipError_t e = launch_linattn(c, d->dtype, stream);
     if (e == hipSuccess && share > 1 && d->T > 0)
         e = launch_group_sum(pk, grad_k, d->k_stride, d->T, d->B, d->kv_heads, share, d->d_k,
                              d->dtype, stream);

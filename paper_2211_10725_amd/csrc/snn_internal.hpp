@@ -322,6 +322,12 @@ struct LaRole {
     float *final_state;   // X after the last token, [B, H, dk, dv], or NULL
     int reverse, first;
     float rs, ws;
+    // sequences cut into segments (LaPlan): a role whose states are not another's
+    // transposed owns slots, fp32 [segs][B, H, dk, dv], slot_seg elements apart
+    float *slot;
+    int64_t slot_seg;
+    int slot_of;       // else the role whose slots it reads
+    int64_t init_seg;  // init of consecutive segments, elements apart
 };
 constexpr int kLaRoles = 3;
 constexpr int kLaMaxD = 128;  // largest head size
@@ -330,8 +336,14 @@ struct LaCall {
     const float *decay;
     const int32_t *lens;
     int T, B, H;
+    int roles, segs, seg_len;
 };
-hipError_t launch_linattn(const LaCall &c, int roles, int dtype, hipStream_t s);
+struct LaPlan {
+    int segs, seg_len;
+};
+// heads: sequences by query heads; width: the larger head size
+LaPlan linattn_plan(int T, int64_t heads, int roles, int width);
+hipError_t launch_linattn(const LaCall &c, int dtype, hipStream_t s);
 // dst (strided [T, B, KV, d] of dtype) = src fp32 [T, B, KV * share, d] summed
 // over each group of `share` heads
 hipError_t launch_group_sum(const float *src, void *dst, const int64_t *stride, int T, int B,
