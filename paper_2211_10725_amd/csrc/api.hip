@@ -924,17 +924,10 @@ void set_out(LaRole &r, void *o, const int64_t *st) {
     r.oh = st[2];
 }
 
-// bytes of one role's segment states, 0 where the sequences are not cut
-size_t segment_bytes(const snn_linattn_desc *d, const LaPlan &p) {
-    if (p.segs == 1) return 0;
-    return align_up((size_t)p.segs * d->B * d->heads * d->d_k * d->d_v * sizeof(float));
-}
-
 LaPlan plan_of(const snn_linattn_desc *d, int roles) {
     return linattn_plan(d->T, (int64_t)d->B * d->heads, roles, std::max(d->d_k, d->d_v));
 }
 
-// the call's common part; ws takes the segments' states of `slots` roles
 LaCall linattn_call(const snn_linattn_desc *d, const float *decay, const int32_t *lens, int roles) {
     LaCall c{};
     c.decay = decay;
@@ -947,11 +940,6 @@ LaCall linattn_call(const snn_linattn_desc *d, const float *decay, const int32_t
     c.segs = p.segs;
     c.seg_len = p.seg_len;
     return c;
-}
-
-void own_slots(const snn_linattn_desc *d, LaRole &r, void *slots) {
-    r.slot = (float *)slots;
-    r.slot_seg = (int64_t)d->B * d->heads * d->d_k * d->d_v;
 }
 
 // fp32 gradient of a shared key or value head, one per query head: [T,B,heads,d]
@@ -1010,8 +998,8 @@ extern "C" {
 
 size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d) {
     if (check_linattn(d) != SNN_OK) return 0;
-    return std::max(segment_bytes(d, plan_of(d, 1)),
-                    2 * segment_bytes(d, plan_of(d, kLaRoles)) + shared_grad_bytes(d, d->d_k) +
+    return std::max(plan_of(d, 1).slot_bytes,
+                    2 * plan_of(d, kLaRoles).slot_bytes + shared_grad_bytes(d, d->d_k) +
                         shared_grad_bytes(d, d->d_v));
 }
 
@@ -1040,7 +1028,7 @@ snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void 
     r.first = 1;
     r.rs = d->scale;
     r.ws = 1.f;
-    if (c.segs > 1) own_slots(d, r, ws);
+    r.slot = (float *)ws;
     (void)hipGetLastError();
     return hip_status(launch_linattn(c, d->dtype, stream));
 }
@@ -1063,7 +1051,7 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
     if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
     LaCall c = linattn_call(d, decay, lens, kLaRoles);
     const int share = d->heads / d->kv_heads;
-    const size_t slots = segment_bytes(d, plan_of(d, kLaRoles));
+    const size_t slots = plan_of(d, kLaRoles).slot_bytes;
     const LaOperand oq = operand(q, d->q_stride, 1), ok = operand(k, d->k_stride, share),
                     ov = operand(v, d->v_stride, share), og = operand(grad_o, d->o_stride, 1);
     float *pk = (float *)((char *)ws + 2 * slots),
@@ -1096,11 +1084,10 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
     dv.final_state = grad_state_in;
     dv.reverse = 1;
     dv.rs = 1.f, dv.ws = d->scale;
-    if (c.segs > 1) {  // dk's states are dv's, transposed
-        own_slots(d, dq, ws);
-        own_slots(d, dv, (char *)ws + slots);
-        dk.slot_of = 2;
-    }
+    dq.slot = (float *)ws;
+    dv.slot = (float *)((char *)ws + slots);
+    dk.slot = dv.slot;  // dk's states are dv's, transposed
+    dk.slot_trans = 1;
     (void)hipGetLastError();
     hipError_t e = launch_linattn(c, d->dtype, stream);
     if (e == hipSuccess && share > 1 && d->T > 0)

@@ -81,6 +81,22 @@ __device__ inline void load_weights(const float *w, int64_t e, int m, float (&v)
     if (w && m > 0) load8(w + e, m, v);
 }
 
+template <int TPR, int NV>
+__device__ inline void load_row_weights(const GateNorm &a, int (&m)[NV], int64_t (&e)[NV],
+                                        float (&cw)[NV][8], float (&wr)[NV][8]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float sc[8];
+        e[i] = 8 * (i * TPR + threadIdx.x % TPR);
+        m[i] = (int)min((int64_t)8, max((int64_t)0, a.n - e[i]));
+        load_weights(a.w_post, e[i], m[i], cw[i]);
+        load_weights(a.scale, e[i], m[i], sc);
+        load_weights(a.w_pre, e[i], m[i], wr[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) cw[i][j] *= sc[j];
+    }
+}
+
 // ---- 8-bit checkpoints: 16 consecutive lanes hold a block of 128 values --------
 constexpr float kMinMax = 0x1p-100f;
 
@@ -128,7 +144,7 @@ __device__ inline void row_sum(float (&s)[N], float *red) {
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) s[k] += __shfl_xor(s[k], off, 64);
     if (TPR > 64) {
-        const int w = threadIdx.x >> 6;
+        const int w = threadIdx.x % TPR >> 6;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int k = 0; k < N; ++k) red[w * N + k] = s[k];
@@ -184,21 +200,14 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_fwd_kernel(Gat
     constexpr int RPB = block_threads<TPR>() / TPR;
     __shared__ float red[RPB][16];
     __shared__ float vec[RPB][TPR * NV];
-    const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const int slot = threadIdx.x / TPR;
     const GateNorm a = c.a;
     const int runs = (a.n + 7) / 8, gl = a.groups == 1 ? 0 : a.n / a.groups / 8;
     const float inv_n = 1.f / (float)a.n, inv_d = 1.f / (float)(a.n / a.groups);
     int m[NV];
     int64_t e[NV];
-    float wp[NV][8], sc[NV][8], wr[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        e[i] = 8 * (i * TPR + t);
-        m[i] = (int)min((int64_t)8, max((int64_t)0, a.n - e[i]));
-        load_weights(a.w_post, e[i], m[i], wp[i]);
-        load_weights(a.scale, e[i], m[i], sc[i]);
-        load_weights(a.w_pre, e[i], m[i], wr[i]);
-    }
+    float cw[NV][8], wr[NV][8];  // w_post scale, w_pre
+    load_row_weights<TPR, NV>(a, m, e, cw, wr);
     const int64_t step = (int64_t)gridDim.x * RPB, nb = ckpt_blocks(a.n);
     // every thread of the workgroup takes part in each round's barriers
     for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
@@ -229,7 +238,7 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_fwd_kernel(Gat
                 for (int j = 0; j < 8; ++j) {
                     float act = 1.f, slope;
                     if (c.g) gate_of<false>(a.gate, gv[i][j], act, slope);
-                    xv[i][j] += sc[i][j] * (yv[i][j] * ry * wp[i][j] * act);
+                    xv[i][j] += yv[i][j] * ry * act * cw[i][j];
                 }
                 store8(static_cast<XT *>(c.x_out) + row * a.ld_x + e[i], k, xv[i]);
                 const int64_t blk = row * nb + e[i] / kCkptBlock;
@@ -256,7 +265,7 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_fwd_kernel(Gat
 }
 
 template <typename XT, typename YT, int TPR, int NV>
-__global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_bwd_kernel(GateNormBwd c) {
+__global__ __launch_bounds__(block_threads<TPR>(), 4) void gate_norm_bwd_kernel(GateNormBwd c) {
     constexpr int RPB = block_threads<TPR>() / TPR;
     __shared__ float red[RPB][32];
     __shared__ float vec[RPB][TPR * NV];
@@ -267,16 +276,11 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_bwd_kernel(Gat
     const bool block = c.y || c.y8;
     int m[NV];
     int64_t e[NV];
-    float wp[NV][8], sc[NV][8], wr[NV][8];
-    float a_post[NV][8] = {}, a_scale[NV][8] = {}, a_pre[NV][8] = {};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        e[i] = 8 * (i * TPR + t);
-        m[i] = (int)min((int64_t)8, max((int64_t)0, a.n - e[i]));
-        load_weights(a.w_post, e[i], m[i], wp[i]);
-        load_weights(a.scale, e[i], m[i], sc[i]);
-        load_weights(a.w_pre, e[i], m[i], wr[i]);
-    }
+    float cw[NV][8], wr[NV][8];  // w_post scale, w_pre
+    load_row_weights<TPR, NV>(a, m, e, cw, wr);
+    // sums over this workgroup's rows: of dx act(gate) yhat, which times scale is
+    // w_post's gradient and times w_post scale's, and of dh xhat, w_pre's
+    float a_post[NV][8] = {}, a_pre[NV][8] = {};
     const int64_t step = (int64_t)gridDim.x * RPB, nb = ckpt_blocks(a.n);
     for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
         const int64_t row = r0 + slot;
@@ -337,13 +341,11 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_bwd_kernel(Gat
             for (int j = 0; j < 8; ++j) {
                 float act = 1.f, slope = 0.f;
                 if (a.gate != SNN_GATE_NONE) gate_of<true>(a.gate, gv[i][j], act, slope);
-                const float hat = yv[i][j] * ry[i], u = hat * wp[i][j];
-                const float da = dx[i][j] * sc[i][j], du = da * act;
-                a_scale[i][j] = __builtin_fmaf(dx[i][j], u * act, a_scale[i][j]);
-                a_post[i][j] = __builtin_fmaf(du, hat, a_post[i][j]);
-                gv[i][j] = da * u * slope;
+                const float hat = yv[i][j] * ry[i], d = dx[i][j] * cw[i][j];
+                a_post[i][j] = __builtin_fmaf(dx[i][j] * act, hat, a_post[i][j]);
+                gv[i][j] = d * hat * slope;
                 yv[i][j] = hat;
-                dx[i][j] = du * wp[i][j];
+                dx[i][j] = d * act;
                 s[i] = __builtin_fmaf(hat, dx[i][j], s[i]);
             }
         }
@@ -360,9 +362,9 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_bwd_kernel(Gat
     }
     // the workgroup's column sums, its rows' slots added in order
     __shared__ float col[RPB > 1 ? TPR * NV * 8 : 1];
-    float(*sums[3])[8] = {a_post, a_scale, a_pre};
+    float(*sums[2])[8] = {a_post, a_pre};
 #pragma unroll
-    for (int w = 0; w < 3; ++w) {
+    for (int w = 0; w < 2; ++w) {
         float *part = c.part + ((int64_t)w * gridDim.x + blockIdx.x) * a.n;
         for (int k = 1; k < RPB; ++k) {
             __syncthreads();
@@ -384,23 +386,37 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_bwd_kernel(Gat
     }
 }
 
-// out[w][col] = sum over the workgroups' partial rows, in order within each of
-// the 16 waves' shares, then over the waves
-__global__ __launch_bounds__(1024) void column_sum_kernel(const float *part, int blocks, int n,
-                                                          float *o0, float *o1, float *o2) {
-    float *out = blockIdx.y == 0 ? o0 : blockIdx.y == 1 ? o1 : o2;
-    if (!out) return;  // the whole workgroup
+// Column sums over the workgroups' partial rows, in order within each of the 16
+// waves' shares, then over the waves; w_post's and scale's gradients are the
+// first sum times each other.
+__global__ __launch_bounds__(1024) void column_sum_kernel(GateNormBwd c, int blocks) {
+    const bool pre = blockIdx.y == 1;
+    if (pre ? !c.dw_pre : !c.dw_post && !c.dscale) return;  // the whole workgroup
     __shared__ float sum[16][64];
+    const int n = c.a.n;
     const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane;
-    const float *p = part + (int64_t)blockIdx.y * blocks * n + col;
+    const float *p = c.part + (int64_t)blockIdx.y * blocks * n + col;
+    // 16 loads at a time on their way: one after the other they cost 22 us of
+    // latency for 1024 workgroups
     float s = 0.f;
     if (col < n)
-        for (int b = w; b < blocks; b += 16) s += p[(int64_t)b * n];
+        for (int b = w; b < blocks; b += 256) {
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = b + 16 * i < blocks ? p[(int64_t)(b + 16 * i) * n] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += x[i];
+        }
     sum[w][lane] = s;
     __syncthreads();
     if (w == 0 && col < n) {
         for (int i = 1; i < 16; ++i) s += sum[i][lane];
-        out[col] = s;
+        if (pre) {
+            c.dw_pre[col] = s;
+        } else {
+            if (c.dw_post) c.dw_post[col] = c.a.scale ? s * c.a.scale[col] : s;
+            if (c.dscale) c.dscale[col] = c.a.w_post ? s * c.a.w_post[col] : s;
+        }
     }
 }
 
@@ -423,26 +439,35 @@ __global__ __launch_bounds__(256) void checkpoint_kernel(int64_t blocks, uint32_
     }
 }
 
-int threads_per_row(int n) { return n <= 1024 ? 64 : n <= 4096 ? 256 : 1024; }
+// Threads of a row: the fewest whose runs of 8 cover it, so that a row takes
+// one run per thread (of 512 to 1024, two runs of a wave: the backward's
+// registers then halve the waves that a CU holds); two only past 8192.
+int threads_per_row(int n) {
+    int t = 64;
+    while (t < 1024 && 8 * t < n) t *= 2;
+    return t;
+}
+int rows_per_block(int n) { return std::max(1, 256 / threads_per_row(n)); }
 
-// workgroups of the backward: its partial sums are [3][blocks][n]
+// Workgroups of the backward, as many as are resident at once: its partial sums
+// are [2][blocks][n].
 int bwd_blocks(int64_t rows, int64_t n) {
-    const int64_t rpb = threads_per_row((int)n) == 64 ? 4 : 1;
-    return (int)std::min<int64_t>((rows + rpb - 1) / rpb, 2 * kPlanCus);
+    const int64_t rpb = rows_per_block((int)n);
+    const int64_t most = 4 * kPlanCus * 256 / std::max(256, threads_per_row((int)n));
+    return (int)std::min<int64_t>((rows + rpb - 1) / rpb, most);
 }
 
-// the threads that a row of n channels takes
 #define GATE_NORM_SIZES(KERNEL)                                                                \
-    if (n <= 512) KERNEL<XT, YT, 64, 1><<<grid, 256, 0, s>>>(c);                              \
-    else if (n <= 1024) KERNEL<XT, YT, 64, 2><<<grid, 256, 0, s>>>(c);                        \
-    else if (n <= 2048) KERNEL<XT, YT, 256, 1><<<grid, 256, 0, s>>>(c);                       \
-    else if (n <= 4096) KERNEL<XT, YT, 256, 2><<<grid, 256, 0, s>>>(c);                       \
-    else if (n <= 8192) KERNEL<XT, YT, 1024, 1><<<grid, 1024, 0, s>>>(c);                     \
+    if (n <= 512) KERNEL<XT, YT, 64, 1><<<grid, 256, 0, s>>>(c);                               \
+    else if (n <= 1024) KERNEL<XT, YT, 128, 1><<<grid, 256, 0, s>>>(c);                        \
+    else if (n <= 2048) KERNEL<XT, YT, 256, 1><<<grid, 256, 0, s>>>(c);                        \
+    else if (n <= 4096) KERNEL<XT, YT, 512, 1><<<grid, 512, 0, s>>>(c);                        \
+    else if (n <= 8192) KERNEL<XT, YT, 1024, 1><<<grid, 1024, 0, s>>>(c);                      \
     else KERNEL<XT, YT, 1024, 2><<<grid, 1024, 0, s>>>(c);
 
 template <typename XT, typename YT>
 void run_fwd(const GateNormFwd &c, hipStream_t s) {
-    const int n = c.a.n, rpb = threads_per_row(n) == 64 ? 4 : 1;
+    const int n = c.a.n, rpb = rows_per_block(n);
     const int grid = (int)std::min<int64_t>((c.a.rows + rpb - 1) / rpb, 8 * kPlanCus);
     GATE_NORM_SIZES(gate_norm_fwd_kernel)
 }
@@ -453,8 +478,8 @@ void run_bwd(const GateNormBwd &c, hipStream_t s) {
     if (grid > 0) {
         GATE_NORM_SIZES(gate_norm_bwd_kernel)
     }
-    column_sum_kernel<<<dim3((n + 63) / 64, 3), 1024, 0, s>>>(c.part, grid, n, c.dw_post, c.dscale,
-                                                              c.dw_pre);
+    if (c.dw_post || c.dscale || c.dw_pre)
+        column_sum_kernel<<<dim3((n + 63) / 64, 2), 1024, 0, s>>>(c, grid);
 }
 
 // F is called with the element types of (xt, yt)
@@ -484,7 +509,7 @@ void run_checkpoint(int64_t rows, int n, int64_t ld, void *x, int8_t *codes, flo
 }  // namespace
 
 size_t gate_norm_workspace_bytes(int64_t rows, int64_t n) {
-    return align_up((size_t)3 * bwd_blocks(rows, n) * n * sizeof(float));
+    return align_up((size_t)2 * bwd_blocks(rows, n) * n * sizeof(float));
 }
 
 hipError_t launch_gate_norm_fwd(const GateNormFwd &c, int xt, int yt, hipStream_t s) {

@@ -322,12 +322,10 @@ struct LaRole {
     float *final_state;   // X after the last token, [B, H, dk, dv], or NULL
     int reverse, first;
     float rs, ws;
-    // sequences cut into segments (LaPlan): a role whose states are not another's
-    // transposed owns slots, fp32 [segs][B, H, dk, dv], slot_seg elements apart
+    // sequences cut into segments: the segments' states, LaPlan's slot_bytes;
+    // slot_trans: another role's, whose state is this one's transposed
     float *slot;
-    int64_t slot_seg;
-    int slot_of;       // else the role whose slots it reads
-    int64_t init_seg;  // init of consecutive segments, elements apart
+    int slot_trans;
 };
 constexpr int kLaRoles = 3;
 constexpr int kLaMaxD = 128;  // largest head size
@@ -337,9 +335,12 @@ struct LaCall {
     const int32_t *lens;
     int T, B, H;
     int roles, segs, seg_len;
+    int summed, copied;  // set by the launcher: slots hold the states that enter
+                         // segments, the first one's too
 };
 struct LaPlan {
     int segs, seg_len;
+    size_t slot_bytes;  // of one role's segment states, 0 for one segment
 };
 // heads: sequences by query heads; width: the larger head size
 LaPlan linattn_plan(int T, int64_t heads, int roles, int width);
@@ -357,6 +358,7 @@ struct LaStep {
     float *out;
     void *o;
     float scale;
+    int cols, slices;  // set by the launcher: columns of v per workgroup
 };
 hipError_t launch_linattn_step(const LaStep &c, int B, int dtype, hipStream_t s);
 
@@ -385,7 +387,7 @@ struct GateNormBwd {
     const float *y8s, *g8s;
     void *dx, *dy, *dg;
     float *dw_post, *dscale, *dw_pre;
-    float *part;       // [3][blocks][n] column sums
+    float *part;       // [2][blocks][n] column sums
 };
 hipError_t launch_gate_norm_fwd(const GateNormFwd &c, int xt, int yt, hipStream_t s);
 hipError_t launch_gate_norm_bwd(const GateNormBwd &c, int xt, int yt, hipStream_t s);
