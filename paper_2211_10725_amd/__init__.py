@@ -202,6 +202,10 @@ def _nbytes(t):
 def _stream(stream):
     if stream is None:
         import torch
+        if torch.cuda.is_initialized():
+            # the current stream's handle itself: a Stream object around it costs
+            # several microseconds, more than a small call's kernel
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -469,32 +473,46 @@ def linattn_desc(q, k, v, o, scale=None) -> LinattnDesc:
                        *(S(*t.stride()[:3]) if t.numel() else S() for t in (q, k, v, o)))
 
 
-def _need_heads(fn, what, t, d, heads, width, stride):
-    """A strided argument of the shape, type and strides the descriptor has."""
+def _need_heads(fn, what, t, dtype, shape, stride):
+    """A strided argument of the shape, type and strides the descriptor has
+    (dimensions of one element have any stride)."""
     if t is None or isinstance(t, int):
         return
-    if tuple(t.shape) != (d.T, d.B, heads, width) or _dtype_code(t) != d.dtype or \
-            (t.numel() and (t.stride(3) != 1 or any(
-                n > 1 and a != b for n, a, b in zip(t.shape, t.stride(), stride)))):
-        raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is "
-                         "not what the descriptor says")
+    if t.dtype is dtype and t.shape == shape:
+        st = t.stride()
+        if st[3] == 1 and list(st[:3]) == stride[:]:
+            return
+        if not t.numel() or st[3] == 1 and all(n == 1 or a == b
+                                               for n, a, b in zip(shape, st, stride)):
+            return
+    raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is not "
+                     "what the descriptor says")
 
 
-def _need_linattn(fn, d, q, k, v, o, decay, names=("q", "k", "v", "o")):
-    _need_heads(fn, names[0], q, d, d.heads, d.d_k, d.q_stride)
-    _need_heads(fn, names[1], k, d, d.kv_heads, d.d_k, d.k_stride)
-    _need_heads(fn, names[2], v, d, d.kv_heads, d.d_v, d.v_stride)
-    _need_heads(fn, names[3], o, d, d.heads, d.d_v, d.o_stride)
-    _need_array(fn, decay, F32, d.heads, "decay")
+def _torch_dtype(code):
+    import torch
+    return torch.float32 if code == F32 else torch.float16 if code == F16 else torch.bfloat16
+
+
+def _need_linattn(fn, d, q, k, v, o, decay, prefix=""):
+    dt, T, B, H, KV, DK, DV = (_torch_dtype(d.dtype), d.T, d.B, d.heads, d.kv_heads, d.d_k,
+                               d.d_v)
+    _need_heads(fn, prefix + "q", q, dt, (T, B, H, DK), d.q_stride)
+    _need_heads(fn, prefix + "k", k, dt, (T, B, KV, DK), d.k_stride)
+    _need_heads(fn, prefix + "v", v, dt, (T, B, KV, DV), d.v_stride)
+    _need_heads(fn, "o or its gradient", o, dt, (T, B, H, DV), d.o_stride)
+    _need_array(fn, decay, F32, H, "decay")
 
 
 def _need_array(fn, t, dtype_code, count, what):
     """_need for an argument that must also be contiguous and of the type itself."""
     if t is None or isinstance(t, int):
         return
-    _need(fn, t, dtype_code, count, what)
-    if not t.is_contiguous() or t.is_floating_point() != (dtype_code == F32):
-        raise ValueError(f"{fn}: {what} must be contiguous and of its type, got {t.dtype}")
+    import torch
+    dt = torch.float32 if dtype_code == F32 else torch.int32
+    if t.dtype is not dt or t.numel() < count or not t.is_contiguous():
+        raise ValueError(f"{fn}: {what} needs {count} contiguous elements of {dt}, got "
+                         f"{t.numel()} of {t.dtype}")
 
 
 def snn_linattn_workspace_bytes(desc: LinattnDesc) -> int:
@@ -517,8 +535,8 @@ def snn_linattn_fwd(desc, q, k, v, decay, lens, state_in, o, state_out, ws, stre
 def snn_linattn_bwd(desc, q, k, v, decay, lens, state_in, grad_o, grad_state_out, grad_q, grad_k,
                     grad_v, grad_state_in, ws, stream=None):
     fn, S = "snn_linattn_bwd", desc.B * desc.heads * desc.d_k * desc.d_v
-    _need_linattn(fn, desc, q, k, v, grad_o, decay, ("q", "k", "v", "grad_o"))
-    _need_linattn(fn, desc, grad_q, grad_k, grad_v, None, None, ("grad_q", "grad_k", "grad_v", ""))
+    _need_linattn(fn, desc, q, k, v, grad_o, decay)
+    _need_linattn(fn, desc, grad_q, grad_k, grad_v, None, None, "grad_")
     _need_array(fn, lens, I32, desc.B, "lens")
     _need_array(fn, state_in, F32, S, "state_in")
     _need_array(fn, grad_state_out, F32, S, "grad_state_out")
@@ -584,14 +602,17 @@ def gate_norm_desc(x, y=None, gate=None, groups=1, act="none", eps=1e-6, h=None)
                         n if h is None else _row_stride(h))
 
 
-def _need_rows(fn, what, t, d, dtype_code, ld):
+def _need_rows(fn, what, t, d, dtype, ld):
     if t is None or isinstance(t, int):
         return
-    rows = t.numel() // d.n
-    if t.shape[-1] != d.n or rows != d.rows or _dtype_code(t) != dtype_code or \
-            (rows > 1 and _row_stride(t) != ld):
-        raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is "
-                         "not what the descriptor says")
+    n, rows, shape = d.n, d.rows, t.shape
+    if t.dtype is dtype and shape[-1] == n and t.numel() == rows * n:
+        if len(shape) == 2 and t.stride() == (ld, 1):
+            return
+        if rows <= 1 or _row_stride(t) == ld:
+            return
+    raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is not "
+                     "what the descriptor says")
 
 
 def _need_ckpt(fn, what, t, rows, n):
@@ -611,14 +632,17 @@ def snn_gate_norm_fwd(desc, x, y, gate, w_post, scale, w_pre, x_out, h, y_ckpt=N
     None: h = norm(x) w_pre alone), with y and the gate stored in 8 bits where
     y_ckpt and gate_ckpt are given."""
     fn, d = "snn_gate_norm_fwd", desc
-    for what, t in (("x", x), ("x_out", x_out)):
-        _need_rows(fn, what, t, d, d.x_dtype, d.ld_x)
-    for what, t, ld in (("y", y, d.ld_y), ("gate", gate, d.ld_g), ("h", h, d.ld_h)):
-        _need_rows(fn, what, t, d, d.y_dtype, ld)
-    for what, t in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre)):
-        _need_array(fn, t, F32, d.n, what)
-    for what, t in (("y_ckpt", y_ckpt), ("gate_ckpt", gate_ckpt)):
-        _need_ckpt(fn, what, t, d.rows, d.n)
+    xt, yt, n = _torch_dtype(d.x_dtype), _torch_dtype(d.y_dtype), d.n
+    _need_rows(fn, "x", x, d, xt, d.ld_x)
+    _need_rows(fn, "x_out", x_out, d, xt, d.ld_x)
+    _need_rows(fn, "y", y, d, yt, d.ld_y)
+    _need_rows(fn, "gate", gate, d, yt, d.ld_g)
+    _need_rows(fn, "h", h, d, yt, d.ld_h)
+    _need_array(fn, w_post, F32, n, "w_post")
+    _need_array(fn, scale, F32, n, "scale")
+    _need_array(fn, w_pre, F32, n, "w_pre")
+    _need_ckpt(fn, "y_ckpt", y_ckpt, d.rows, n)
+    _need_ckpt(fn, "gate_ckpt", gate_ckpt, d.rows, n)
     _check(fn, lib().snn_gate_norm_fwd(
         ctypes.byref(d), _p(x), _p(y), _p(gate), _p(w_post), _p(scale), _p(w_pre), _p(x_out),
         _p(h), _p(y_ckpt), _p(gate_ckpt), _stream(stream)))
@@ -630,11 +654,12 @@ def snn_gate_norm_bwd(desc, grad_x_out, grad_h, x_out, y, gate, y_ckpt, gate_ckp
     """The backward of snn_gate_norm_fwd, from y and gate or from their 8-bit
     checkpoints."""
     fn, d = "snn_gate_norm_bwd", desc
+    xt, yt = _torch_dtype(d.x_dtype), _torch_dtype(d.y_dtype)
     for what, t in (("grad_x_out", grad_x_out), ("x_out", x_out), ("grad_x", grad_x)):
-        _need_rows(fn, what, t, d, d.x_dtype, d.ld_x)
+        _need_rows(fn, what, t, d, xt, d.ld_x)
     for what, t, ld in (("y", y, d.ld_y), ("grad_y", grad_y, d.ld_y), ("gate", gate, d.ld_g),
                         ("grad_gate", grad_gate, d.ld_g), ("grad_h", grad_h, d.ld_h)):
-        _need_rows(fn, what, t, d, d.y_dtype, ld)
+        _need_rows(fn, what, t, d, yt, ld)
     for what, t in (("w_post", w_post), ("scale", scale), ("w_pre", w_pre),
                     ("grad_w_post", grad_w_post), ("grad_scale", grad_scale),
                     ("grad_w_pre", grad_w_pre)):
