@@ -562,7 +562,7 @@ typedef struct snn_gate_norm_desc {
     int32_t x_dtype;     /* x, x_out, their gradients: SNN_F32, or y_dtype */
     int32_t y_dtype;     /* y, gate, h, their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
     float eps;           /* > 0 */
-    int32_t reserved;    /* 0 */
+    int32_t ckpt_block;  /* block of the 8-bit checkpoints: 8, 16, 32, 64 or 128 */
     int64_t ld_x, ld_y, ld_g, ld_h; /* row strides, >= n, of x and x_out; y; gate; h,
                                        and of their gradients (ld_g: ignored for
                                        SNN_GATE_NONE) */
@@ -575,8 +575,9 @@ size_t snn_gate_norm_workspace_bytes(const snn_gate_norm_desc *d);
  * x_out and the checkpoints must then be NULL and the gate SNN_GATE_NONE.
  * Else x_out is required and gate iff d->gate is not SNN_GATE_NONE.  h NULL:
  * no norm follows.  w_post, scale, w_pre: fp32 [n], or NULL for ones.
- * y_ckpt, gate_ckpt (nullable; snn_checkpoint_bytes(rows, n) each, 16-byte
- * aligned): receive y and the gate as 8-bit checkpoints.  x_out may be x. */
+ * y_ckpt, gate_ckpt (nullable; snn_checkpoint_bytes(rows, n, ckpt_block) each,
+ * 16-byte aligned): receive y and the gate as 8-bit checkpoints.  x_out may be
+ * x. */
 snn_status snn_gate_norm_fwd(const snn_gate_norm_desc *d, const void *x, const void *y,
                              const void *gate, const float *w_post, const float *scale,
                              const float *w_pre, void *x_out, void *h, void *y_ckpt,
@@ -599,19 +600,21 @@ snn_status snn_gate_norm_bwd(const snn_gate_norm_desc *d, const void *grad_x_out
                              float *grad_scale, float *grad_w_pre, void *ws, size_t ws_bytes,
                              hipStream_t stream);
 
-/* Activation checkpoints in 8 bits: rows of n values in blocks of 128 (the
- * last may be shorter), each with one fp32 scale:
+/* Activation checkpoints in 8 bits: rows of n values in blocks of `block` (8,
+ * 16, 32, 64 or 128; a row's last may be shorter), each with one fp32 scale:
  *     scale = fl(m fl(1/127)),  code = rint(fl(x fl(127 / m))),  m = max |x|,
  * and a code stands for fl(code scale): at most m / 254 away (and fp32
  * rounding).  m < 2^-100 is held as zeros; a block with an infinity or a NaN
- * reads back as NaN.  The buffer holds int8 codes [rows][n], then from the next
- * multiple of 256 bytes fp32 scales [rows][ceil(n / 128)]. */
-size_t snn_checkpoint_bytes(int32_t rows, int32_t n); /* 0 for negative sizes */
-snn_status snn_checkpoint_save(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
-                               const void *x, void *ckpt, hipStream_t stream);
+ * reads back as NaN.  Values that are small beside others of their block lose
+ * digits: where a norm divides by the root mean square of a group (a head), a
+ * block should lie within one group.  The buffer holds int8 codes [rows][n],
+ * then from the next multiple of 256 bytes fp32 scales [rows][ceil(n / block)]. */
+size_t snn_checkpoint_bytes(int32_t rows, int32_t n, int32_t block); /* 0: bad sizes */
+snn_status snn_checkpoint_save(int32_t rows, int32_t n, int32_t block, int64_t ld,
+                               int32_t dtype, const void *x, void *ckpt, hipStream_t stream);
 /* x of dtype (SNN_F32 | SNN_F16 | SNN_BF16), each value rounded once. */
-snn_status snn_checkpoint_load(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
-                               const void *ckpt, void *x, hipStream_t stream);
+snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t ld,
+                               int32_t dtype, const void *ckpt, void *x, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -114,7 +114,7 @@ class GateNormDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("n", ctypes.c_int32), ("groups", ctypes.c_int32),
                 ("gate", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
                 ("y_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
-                ("reserved", ctypes.c_int32), ("ld_x", ctypes.c_int64),
+                ("ckpt_block", ctypes.c_int32), ("ld_x", ctypes.c_int64),
                 ("ld_y", ctypes.c_int64), ("ld_g", ctypes.c_int64), ("ld_h", ctypes.c_int64)]
 
 
@@ -170,9 +170,9 @@ def lib():
         "snn_gate_norm_workspace_bytes": ([GN], S),
         "snn_gate_norm_fwd": ([GN] + [P] * 11, ctypes.c_int),
         "snn_gate_norm_bwd": ([GN] + [P] * 17 + [S, P], ctypes.c_int),
-        "snn_checkpoint_bytes": ([i32, i32], S),
-        "snn_checkpoint_save": ([i32, i32, i64, i32, P, P, P], ctypes.c_int),
-        "snn_checkpoint_load": ([i32, i32, i64, i32, P, P, P], ctypes.c_int),
+        "snn_checkpoint_bytes": ([i32, i32, i32], S),
+        "snn_checkpoint_save": ([i32, i32, i32, i64, i32, P, P, P], ctypes.c_int),
+        "snn_checkpoint_load": ([i32, i32, i32, i64, i32, P, P, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -584,19 +584,23 @@ def _row_stride(t):
     return max(n[-1], 1) if ld is None else ld
 
 
-def gate_norm_desc(x, y=None, gate=None, groups=1, act="none", eps=1e-6, h=None) -> GateNormDesc:
+def gate_norm_desc(x, y=None, gate=None, groups=1, act="none", eps=1e-6, h=None,
+                   ckpt_block=128) -> GateNormDesc:
     """Descriptor of the norms around a block: x [..., n] the residual stream, y
     the block's output and gate (or None), with act "none", "mul", "sigmoid" or
     "silu"; y's norm is taken over each of `groups` parts of a row.  Later calls
     may pass other tensors of the same strides; x_out has x's, h those of the h
-    given here (contiguous rows of y's dtype, or x's without y, if None)."""
+    given here (contiguous rows of y's dtype, or x's without y, if None).  ckpt_block:
+    values that share a scale in 8-bit checkpoints of y and the gate; a block
+    should lie within one group."""
     n = x.shape[-1]
     rows = x.numel() // n if n else 0
     for t in (y, gate, h):
         if t is not None and t.shape != x.shape:
             raise ValueError(f"gate_norm_desc: shapes {tuple(x.shape)} and {tuple(t.shape)}")
     yt = _dtype_code(y if y is not None else h if h is not None else x)
-    return GateNormDesc(rows, n, groups, _GATE[act], _dtype_code(x), yt, eps, 0, _row_stride(x),
+    return GateNormDesc(rows, n, groups, _GATE[act], _dtype_code(x), yt, eps, ckpt_block,
+                        _row_stride(x),
                         n if y is None else _row_stride(y),
                         n if gate is None else _row_stride(gate),
                         n if h is None else _row_stride(h))
@@ -615,11 +619,12 @@ def _need_rows(fn, what, t, d, dtype, ld):
                      "what the descriptor says")
 
 
-def _need_ckpt(fn, what, t, rows, n):
+def _need_ckpt(fn, what, t, rows, n, block):
     if t is None or isinstance(t, int):
         return
-    if not t.is_contiguous() or _nbytes(t) < snn_checkpoint_bytes(rows, n):
-        raise ValueError(f"{fn}: {what} needs {snn_checkpoint_bytes(rows, n)} contiguous bytes")
+    need = snn_checkpoint_bytes(rows, n, block)
+    if not t.is_contiguous() or _nbytes(t) < need:
+        raise ValueError(f"{fn}: {what} needs {need} contiguous bytes")
 
 
 def snn_gate_norm_workspace_bytes(desc: GateNormDesc) -> int:
@@ -641,8 +646,8 @@ def snn_gate_norm_fwd(desc, x, y, gate, w_post, scale, w_pre, x_out, h, y_ckpt=N
     _need_array(fn, w_post, F32, n, "w_post")
     _need_array(fn, scale, F32, n, "scale")
     _need_array(fn, w_pre, F32, n, "w_pre")
-    _need_ckpt(fn, "y_ckpt", y_ckpt, d.rows, n)
-    _need_ckpt(fn, "gate_ckpt", gate_ckpt, d.rows, n)
+    _need_ckpt(fn, "y_ckpt", y_ckpt, d.rows, n, d.ckpt_block)
+    _need_ckpt(fn, "gate_ckpt", gate_ckpt, d.rows, n, d.ckpt_block)
     _check(fn, lib().snn_gate_norm_fwd(
         ctypes.byref(d), _p(x), _p(y), _p(gate), _p(w_post), _p(scale), _p(w_pre), _p(x_out),
         _p(h), _p(y_ckpt), _p(gate_ckpt), _stream(stream)))
@@ -665,32 +670,34 @@ def snn_gate_norm_bwd(desc, grad_x_out, grad_h, x_out, y, gate, y_ckpt, gate_ckp
                     ("grad_w_pre", grad_w_pre)):
         _need_array(fn, t, F32, d.n, what)
     for what, t in (("y_ckpt", y_ckpt), ("gate_ckpt", gate_ckpt)):
-        _need_ckpt(fn, what, t, d.rows, d.n)
+        _need_ckpt(fn, what, t, d.rows, d.n, d.ckpt_block)
     _check(fn, lib().snn_gate_norm_bwd(
         ctypes.byref(d), _p(grad_x_out), _p(grad_h), _p(x_out), _p(y), _p(gate), _p(y_ckpt),
         _p(gate_ckpt), _p(w_post), _p(scale), _p(w_pre), _p(grad_x), _p(grad_y), _p(grad_gate),
         _p(grad_w_post), _p(grad_scale), _p(grad_w_pre), _p(ws), _nbytes(ws), _stream(stream)))
 
 
-def snn_checkpoint_bytes(rows: int, n: int) -> int:
-    return int(lib().snn_checkpoint_bytes(rows, n))
+def snn_checkpoint_bytes(rows: int, n: int, block: int = 128) -> int:
+    return int(lib().snn_checkpoint_bytes(rows, n, block))
 
 
-def _checkpoint(fn, x, ckpt, args, stream):
+def _checkpoint(fn, x, ckpt, block, args, stream):
     n = x.shape[-1]
     rows = x.numel() // n if n else 0
-    _need_ckpt(fn, "ckpt", ckpt, rows, n)
-    _check(fn, getattr(lib(), fn)(rows, n, _row_stride(x), _dtype_code(x), *args, _stream(stream)))
+    _need_ckpt(fn, "ckpt", ckpt, rows, n, block)
+    _check(fn, getattr(lib(), fn)(rows, n, block, _row_stride(x), _dtype_code(x), *args,
+                                  _stream(stream)))
 
 
-def snn_checkpoint_save(x, ckpt, stream=None):
-    """Stores x [..., n] in 8 bits in ckpt (snn_checkpoint_bytes(rows, n) bytes)."""
-    _checkpoint("snn_checkpoint_save", x, ckpt, (_p(x), _p(ckpt)), stream)
+def snn_checkpoint_save(x, ckpt, block=128, stream=None):
+    """Stores x [..., n] in 8 bits in ckpt (snn_checkpoint_bytes(rows, n, block)
+    bytes), `block` values to a scale."""
+    _checkpoint("snn_checkpoint_save", x, ckpt, block, (_p(x), _p(ckpt)), stream)
 
 
-def snn_checkpoint_load(ckpt, x, stream=None):
+def snn_checkpoint_load(ckpt, x, block=128, stream=None):
     """Reads the checkpoint of x's shape back into x (any of its dtypes)."""
-    _checkpoint("snn_checkpoint_load", x, ckpt, (_p(ckpt), _p(x)), stream)
+    _checkpoint("snn_checkpoint_load", x, ckpt, block, (_p(ckpt), _p(x)), stream)
 
 
 # --------------------------------------------------------------------------

@@ -948,13 +948,17 @@ size_t shared_grad_bytes(const snn_linattn_desc *d, int width) {
     return align_up((size_t)d->T * d->B * d->heads * width * sizeof(float));
 }
 
+bool ckpt_block_valid(int block) {
+    return block >= 8 && block <= 128 && (block & (block - 1)) == 0;
+}
+
 snn_status check_gate_norm(const snn_gate_norm_desc *d) {
     if (!d) return SNN_ERR_NULL;
     if (d->rows < 0 || d->n < 1 || d->n > kGateNormMaxN || d->groups < 1 ||
         d->n % d->groups != 0 || (d->groups > 1 && (d->n / d->groups) % 8 != 0))
         return SNN_ERR_SHAPE;
-    if (d->gate < SNN_GATE_NONE || d->gate > SNN_GATE_SILU || d->reserved != 0)
-        return SNN_ERR_UNSUPPORTED;
+    if (d->gate < SNN_GATE_NONE || d->gate > SNN_GATE_SILU) return SNN_ERR_UNSUPPORTED;
+    if (!ckpt_block_valid(d->ckpt_block)) return SNN_ERR_SHAPE;
     if (!float_dtype(d->y_dtype) || (d->x_dtype != SNN_F32 && d->x_dtype != d->y_dtype))
         return SNN_ERR_DTYPE;
     if (!finite(d->eps) || !(d->eps > 0.f)) return SNN_ERR_SHAPE;
@@ -973,7 +977,7 @@ bool any_misaligned_rows(int dt, std::initializer_list<const void *> ps) {
 
 GateNorm gate_norm_args(const snn_gate_norm_desc *d, const float *w_post, const float *scale,
                         const float *w_pre) {
-    return GateNorm{d->rows, d->n, d->groups, d->gate, d->eps, d->ld_x, d->ld_y, d->ld_g, d->ld_h,
+    return GateNorm{d->rows, d->n, d->groups, d->gate, d->ckpt_block, d->eps, d->ld_x, d->ld_y, d->ld_g, d->ld_h,
                     w_post, scale, w_pre};
 }
 
@@ -981,10 +985,11 @@ float *ckpt_scales(const void *ckpt, int64_t rows, int64_t n) {
     return (float *)((char *)ckpt + ckpt_scale_offset(rows, n));
 }
 
-snn_status check_checkpoint(int32_t rows, int32_t n, int64_t ld, int32_t dtype, const void *x,
-                            const void *ckpt) {
-    if (rows < 0 || n < 0 || ld < n || ld > ((int64_t)1 << 32)) return SNN_ERR_SHAPE;
-    if (rows * ckpt_blocks(n) > INT32_MAX) return SNN_ERR_SHAPE;
+snn_status check_checkpoint(int32_t rows, int32_t n, int32_t block, int64_t ld, int32_t dtype,
+                            const void *x, const void *ckpt) {
+    if (rows < 0 || n < 0 || ld < n || ld > ((int64_t)1 << 32) || !ckpt_block_valid(block))
+        return SNN_ERR_SHAPE;
+    if (rows * ckpt_blocks(n, 128) > INT32_MAX) return SNN_ERR_SHAPE;
     if (!float_dtype(dtype)) return SNN_ERR_DTYPE;
     if (rows == 0 || n == 0) return SNN_OK;
     if (!x || !ckpt) return SNN_ERR_NULL;
@@ -1210,27 +1215,27 @@ snn_status snn_gate_norm_bwd(const snn_gate_norm_desc *d, const void *grad_x_out
     return hip_status(launch_gate_norm_bwd(c, d->x_dtype, d->y_dtype, stream));
 }
 
-size_t snn_checkpoint_bytes(int32_t rows, int32_t n) {
-    if (rows < 0 || n < 0) return 0;
+size_t snn_checkpoint_bytes(int32_t rows, int32_t n, int32_t block) {
+    if (rows < 0 || n < 0 || !ckpt_block_valid(block)) return 0;
     return ckpt_scale_offset(rows, n) +
-           align_up((size_t)(rows * ckpt_blocks(n)) * sizeof(float));
+           align_up((size_t)(rows * ckpt_blocks(n, block)) * sizeof(float));
 }
 
-snn_status snn_checkpoint_save(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
+snn_status snn_checkpoint_save(int32_t rows, int32_t n, int32_t block, int64_t ld, int32_t dtype,
                                const void *x, void *ckpt, hipStream_t stream) {
-    const snn_status st = check_checkpoint(rows, n, ld, dtype, x, ckpt);
+    const snn_status st = check_checkpoint(rows, n, block, ld, dtype, x, ckpt);
     if (st != SNN_OK || rows == 0 || n == 0) return st;
     (void)hipGetLastError();
-    return hip_status(launch_checkpoint(rows, n, ld, dtype, (void *)x, (int8_t *)ckpt,
+    return hip_status(launch_checkpoint(rows, n, block, ld, dtype, (void *)x, (int8_t *)ckpt,
                                         ckpt_scales(ckpt, rows, n), true, stream));
 }
 
-snn_status snn_checkpoint_load(int32_t rows, int32_t n, int64_t ld, int32_t dtype,
+snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t ld, int32_t dtype,
                                const void *ckpt, void *x, hipStream_t stream) {
-    const snn_status st = check_checkpoint(rows, n, ld, dtype, x, ckpt);
+    const snn_status st = check_checkpoint(rows, n, block, ld, dtype, x, ckpt);
     if (st != SNN_OK || rows == 0 || n == 0) return st;
     (void)hipGetLastError();
-    return hip_status(launch_checkpoint(rows, n, ld, dtype, x, (int8_t *)ckpt,
+    return hip_status(launch_checkpoint(rows, n, block, ld, dtype, x, (int8_t *)ckpt,
                                         ckpt_scales(ckpt, rows, n), false, stream));
 }
 

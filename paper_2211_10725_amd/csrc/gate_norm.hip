@@ -157,15 +157,16 @@ __device__ inline void load_row_weights(const GateNorm &a, int (&m)[NV], int64_t
     }
 }
 
-// ---- 8-bit checkpoints: 16 consecutive lanes hold a block of 128 values --------
+// ---- 8-bit checkpoints: `lanes` consecutive lanes (1 .. 16) hold a block of values --
 constexpr float kMinMax = 0x1p-100f;
 
-__device__ inline void encode8(const float (&v)[8], int8_t *code, float *scale, int m) {
+__device__ inline void encode8(const float (&v)[8], int8_t *code, float *scale, int m,
+                               int lanes) {
     uint32_t top = 0;  // |x| as bits: NaN above infinity above every number
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-#pragma unroll
-    for (int off = 1; off < 16; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
+    for (int off = 1; off < lanes; off <<= 1)
+        top = max(top, (uint32_t)__shfl_xor((int)top, off, 64));
     const float t = __uint_as_float(top);
     const bool fine = top < 0x7f800000u, some = fine && t >= kMinMax;
     const float up = some ? 127.f / t : 0.f;
@@ -179,7 +180,7 @@ __device__ inline void encode8(const float (&v)[8], int8_t *code, float *scale, 
         for (int j = 0; j < 8; ++j)
             if (j < m) code[j] = c[j];
     }
-    if ((threadIdx.x & 15) == 0 && m > 0)
+    if ((threadIdx.x & (lanes - 1)) == 0 && m > 0)
         *scale = !fine ? __builtin_nanf("") : some ? t * (float)(1.0 / 127.0) : 0.f;
 }
 __device__ inline void decode8(const int8_t *code, float scale, int m, float (&v)[8]) {
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_fwd_kernel(Gat
     int64_t e[NV];
     float cw[NV][8], wr[NV][8];  // w_post scale, w_pre
     load_row_weights<TPR, NV>(a, m, e, cw, wr);
-    const int64_t step = (int64_t)gridDim.x * RPB, nb = ckpt_blocks(a.n);
+    const int64_t step = (int64_t)gridDim.x * RPB, nb = ckpt_blocks(a.n, a.block);
     // every thread of the workgroup takes part in each round's barriers
     for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
         const int64_t row = r0 + slot;
@@ -301,9 +302,9 @@ __global__ __launch_bounds__(block_threads<TPR>()) void gate_norm_fwd_kernel(Gat
                     xv[i][j] += yv[i][j] * ry * act * cw[i][j];
                 }
                 store8(static_cast<XT *>(c.x_out) + row * a.ld_x + e[i], k, xv[i]);
-                const int64_t blk = row * nb + e[i] / kCkptBlock;
-                if (c.y8) encode8(yv[i], c.y8 + row * a.n + e[i], c.y8s + blk, k);
-                if (c.g8) encode8(gv[i], c.g8 + row * a.n + e[i], c.g8s + blk, k);
+                const int64_t blk = row * nb + e[i] / a.block;
+                if (c.y8) encode8(yv[i], c.y8 + row * a.n + e[i], c.y8s + blk, k, a.block / 8);
+                if (c.g8) encode8(gv[i], c.g8 + row * a.n + e[i], c.g8s + blk, k, a.block / 8);
             }
         }
         if (!c.h) continue;
@@ -342,7 +343,7 @@ gate_norm_bwd_kernel(GateNormBwd c) {
     // sums over this workgroup's rows: of dx act(gate) yhat, which times scale is
     // w_post's gradient and times w_post scale's, and of dh xhat, w_pre's
     float a_post[NV][8] = {}, a_pre[NV][8] = {};
-    const int64_t step = (int64_t)gridDim.x * RPB, nb = ckpt_blocks(a.n);
+    const int64_t step = (int64_t)gridDim.x * RPB, nb = ckpt_blocks(a.n, a.block);
     for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
         const int64_t row = r0 + slot;
         const bool live = row < a.rows;
@@ -354,7 +355,7 @@ gate_norm_bwd_kernel(GateNormBwd c) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int k = live ? m[i] : 0;
-            const int64_t at = row * a.n + e[i], blk = row * nb + e[i] / kCkptBlock;
+            const int64_t at = row * a.n + e[i], blk = row * nb + e[i] / a.block;
             rdx[i].load(static_cast<const XT *>(c.dxo) + row * a.ld_x + e[i], c.dxo ? k : 0);
             if (c.dh) {
                 rdh[i].load(static_cast<const YT *>(c.dh) + row * a.ld_h + e[i], k);
@@ -506,19 +507,21 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(GateNormBwd c, int blo
     }
 }
 
+// 16 lanes take 128 values of a row
 template <typename T, bool SAVE>
-__global__ __launch_bounds__(256) void checkpoint_kernel(int64_t blocks, uint32_t nb, int n,
-                                                         int64_t ld, T *x, int8_t *codes,
-                                                         float *scales) {
-    const int64_t b = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const bool live = b < blocks;
-    const int64_t row = live ? (uint32_t)b / nb : 0;
-    const int e = live ? (int)((uint32_t)b % nb) * kCkptBlock + 8 * (threadIdx.x & 15) : 0;
+__global__ __launch_bounds__(256) void checkpoint_kernel(int64_t units, uint32_t per_row, int n,
+                                                         int block, int64_t ld, T *x,
+                                                         int8_t *codes, float *scales) {
+    const int64_t u = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const bool live = u < units;
+    const int64_t row = live ? (uint32_t)u / per_row : 0;
+    const int e = live ? (int)((uint32_t)u % per_row) * 128 + 8 * (threadIdx.x & 15) : 0;
     const int m = live ? min(8, max(0, n - e)) : 0;
+    const int64_t b = row * ckpt_blocks(n, block) + e / block;
     float v[8];
     if (SAVE) {
         load8(x + row * ld + e, m, v);
-        encode8(v, codes + row * n + e, scales + b, m);
+        encode8(v, codes + row * n + e, scales + b, m, block / 8);
     } else if (m > 0) {
         decode8(codes + row * n + e, scales[b], m, v);
         store8(x + row * ld + e, m, v);
@@ -584,16 +587,16 @@ hipError_t by_types(const C &c, int xt, int yt, hipStream_t s, void (*f32)(const
 }
 
 template <typename T>
-void run_checkpoint(int64_t rows, int n, int64_t ld, void *x, int8_t *codes, float *scales,
-                    bool save, hipStream_t s) {
-    const int64_t nb = ckpt_blocks(n), blocks = rows * nb;
-    const int grid = (int)((blocks + 15) / 16);
+void run_checkpoint(int64_t rows, int n, int block, int64_t ld, void *x, int8_t *codes,
+                    float *scales, bool save, hipStream_t s) {
+    const int64_t per_row = ckpt_blocks(n, 128), units = rows * per_row;
+    const int grid = (int)((units + 15) / 16);
     if (save)
-        checkpoint_kernel<T, true><<<grid, 256, 0, s>>>(blocks, (uint32_t)nb, n, ld, (T *)x,
-                                                        codes, scales);
+        checkpoint_kernel<T, true><<<grid, 256, 0, s>>>(units, (uint32_t)per_row, n, block, ld,
+                                                        (T *)x, codes, scales);
     else
-        checkpoint_kernel<T, false><<<grid, 256, 0, s>>>(blocks, (uint32_t)nb, n, ld, (T *)x,
-                                                         codes, scales);
+        checkpoint_kernel<T, false><<<grid, 256, 0, s>>>(units, (uint32_t)per_row, n, block, ld,
+                                                         (T *)x, codes, scales);
 }
 
 }  // namespace
@@ -614,12 +617,12 @@ hipError_t launch_gate_norm_bwd(const GateNormBwd &c, int xt, int yt, hipStream_
                                  run_bwd<bf16_t, bf16_t>);
 }
 
-hipError_t launch_checkpoint(int64_t rows, int n, int64_t ld, int dtype, void *x, int8_t *codes,
-                             float *scales, bool save, hipStream_t s) {
+hipError_t launch_checkpoint(int64_t rows, int n, int block, int64_t ld, int dtype, void *x,
+                             int8_t *codes, float *scales, bool save, hipStream_t s) {
     switch (dtype) {
-        case SNN_F32: run_checkpoint<float>(rows, n, ld, x, codes, scales, save, s); break;
-        case SNN_F16: run_checkpoint<half_t>(rows, n, ld, x, codes, scales, save, s); break;
-        default: run_checkpoint<bf16_t>(rows, n, ld, x, codes, scales, save, s); break;
+        case SNN_F32: run_checkpoint<float>(rows, n, block, ld, x, codes, scales, save, s); break;
+        case SNN_F16: run_checkpoint<half_t>(rows, n, block, ld, x, codes, scales, save, s); break;
+        default: run_checkpoint<bf16_t>(rows, n, block, ld, x, codes, scales, save, s); break;
     }
     return hipGetLastError();
 }

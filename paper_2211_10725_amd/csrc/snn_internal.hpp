@@ -364,11 +364,13 @@ hipError_t launch_linattn_step(const LaStep &c, int B, int dtype, hipStream_t s)
 
 // ---- gated norms and 8-bit checkpoints (gate_norm.hip) --------------------------
 constexpr int kGateNormMaxN = 16384;
-constexpr int kCkptBlock = 128;  // values that share a scale
-__host__ __device__ inline int64_t ckpt_blocks(int64_t n) { return (n + kCkptBlock - 1) / kCkptBlock; }
+// blocks of a row, `block` values that share a scale each
+__host__ __device__ inline int64_t ckpt_blocks(int64_t n, int block) {
+    return (n + block - 1) / block;
+}
 inline size_t ckpt_scale_offset(int64_t rows, int64_t n) { return align_up((size_t)(rows * n)); }
 struct GateNorm {
-    int rows, n, groups, gate;
+    int rows, n, groups, gate, block;
     float eps;
     int64_t ld_x, ld_y, ld_g, ld_h;
     const float *w_post, *scale, *w_pre;
@@ -392,7 +394,7 @@ struct GateNormBwd {
 hipError_t launch_gate_norm_fwd(const GateNormFwd &c, int xt, int yt, hipStream_t s);
 hipError_t launch_gate_norm_bwd(const GateNormBwd &c, int xt, int yt, hipStream_t s);
 size_t gate_norm_workspace_bytes(int64_t rows, int64_t n);
-hipError_t launch_checkpoint(int64_t rows, int n, int64_t ld, int dtype, void *x, int8_t *codes,
-                             float *scales, bool save, hipStream_t s);
+hipError_t launch_checkpoint(int64_t rows, int n, int block, int64_t ld, int dtype, void *x,
+                             int8_t *codes, float *scales, bool save, hipStream_t s);
 
 }  // namespace snn

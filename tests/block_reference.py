@@ -55,18 +55,18 @@ def linattn_grads(q, k, v, decay, lens, init, scale, go, gs):
     return dq, dk, dv, R
 
 
-def quantised(x):
+def quantised(x, block=128):
     """What an 8-bit checkpoint of fp32 x [rows, n] stands for (its own fp32 steps)."""
     x = np.asarray(x, np.float32)
     out = np.zeros_like(x)
-    for a in range(0, x.shape[1], 128):
-        b = x[:, a:a + 128]
+    for a in range(0, x.shape[1], block):
+        b = x[:, a:a + block]
         with np.errstate(all="ignore"):
             top = np.abs(b).max(1, keepdims=True)
             fine = np.isfinite(b).all(1, keepdims=True)
             code = np.rint(b * (np.float32(127) / top))
             val = np.where(top >= np.float32(2.0 ** -100), code * (top * np.float32(1 / 127)), 0)
-        out[:, a:a + 128] = np.where(fine, val, np.nan)
+        out[:, a:a + block] = np.where(fine, val, np.nan)
     return out
 
 

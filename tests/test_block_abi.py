@@ -123,14 +123,14 @@ def test_gate_norm_descriptor():
     d = _gn()
     assert _gfwd(None) == NULL and _gfwd(d) == ALIGN
     for bad in (dict(rows=-1), dict(n=0), dict(n=16385, groups=1), dict(groups=0), dict(groups=5),
-                dict(groups=24), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
+                dict(groups=24), dict(ckpt_block=0),
+                dict(ckpt_block=48), dict(ckpt_block=256), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
                 dict(ld_x=95), dict(ld_y=0), dict(ld_g=95), dict(ld_h=-96), dict(ld_x=1 << 33)):
         assert _gfwd(_changed(d, **bad)) == SHAPE, bad
         assert snn.lib().snn_gate_norm_workspace_bytes(_changed(d, **bad)) == 0
     for bad in (dict(x_dtype=snn.F16), dict(y_dtype=snn.U8), dict(x_dtype=snn.U8)):
         assert _gfwd(_changed(d, **bad)) == DTYPE
     assert _gfwd(_changed(d, gate=4)) == UNSUPPORTED
-    assert _gfwd(_changed(d, reserved=1)) == UNSUPPORTED
     assert _gfwd(_changed(d, rows=0)) == OK
 
 
@@ -184,17 +184,20 @@ def test_gate_norm_binding_checks_tensors():
 
 def test_checkpoint():
     L = snn.lib()
-    assert L.snn_checkpoint_bytes(-1, 5) == 0 and L.snn_checkpoint_bytes(3, -1) == 0
-    assert L.snn_checkpoint_bytes(2, 129) == 512 + 256           # codes, then 4 scales
+    assert L.snn_checkpoint_bytes(-1, 5, 128) == 0 and L.snn_checkpoint_bytes(3, -1, 128) == 0
+    assert L.snn_checkpoint_bytes(2, 129, 128) == 512 + 256      # codes, then 4 scales
+    assert L.snn_checkpoint_bytes(2, 1024, 8) == 2048 + 1024     # 256 scales
+    assert all(L.snn_checkpoint_bytes(2, 129, b) == 0 for b in (0, 4, 24, 256, -8))
     for fn in (L.snn_checkpoint_save, L.snn_checkpoint_load):
-        assert fn(-1, 8, 8, snn.F32, 16, 16, None) == SHAPE
-        assert fn(3, 8, 7, snn.F32, 16, 16, None) == SHAPE
-        assert fn(1 << 30, 1 << 20, 1 << 20, snn.F32, 16, 16, None) == SHAPE
-        assert fn(3, 8, 8, snn.U8, 16, 16, None) == DTYPE
-        assert fn(3, 8, 8, snn.F32, None, 16, None) == NULL
-        assert fn(3, 8, 8, snn.F32, 16, None, None) == NULL
-        assert fn(0, 8, 8, snn.F32, None, None, None) == OK
-    assert L.snn_checkpoint_save(3, 8, 8, snn.F32, 18, 16, None) == ALIGN
-    assert L.snn_checkpoint_load(3, 8, 8, snn.F16, 24, 16, None) == ALIGN
+        assert fn(-1, 8, 128, 8, snn.F32, 16, 16, None) == SHAPE
+        assert fn(3, 8, 128, 7, snn.F32, 16, 16, None) == SHAPE
+        assert fn(3, 8, 96, 8, snn.F32, 16, 16, None) == SHAPE
+        assert fn(1 << 30, 1 << 20, 128, 1 << 20, snn.F32, 16, 16, None) == SHAPE
+        assert fn(3, 8, 64, 8, snn.U8, 16, 16, None) == DTYPE
+        assert fn(3, 8, 64, 8, snn.F32, None, 16, None) == NULL
+        assert fn(3, 8, 64, 8, snn.F32, 16, None, None) == NULL
+        assert fn(0, 8, 64, 8, snn.F32, None, None, None) == OK
+    assert L.snn_checkpoint_save(3, 8, 128, 8, snn.F32, 18, 16, None) == ALIGN
+    assert L.snn_checkpoint_load(3, 8, 128, 8, snn.F16, 24, 16, None) == ALIGN
     with pytest.raises(ValueError):
-        snn.snn_checkpoint_save(torch.empty(4, 40), torch.empty(100, dtype=torch.uint8), 0)
+        snn.snn_checkpoint_save(torch.empty(4, 40), torch.empty(100, dtype=torch.uint8))

@@ -46,7 +46,7 @@ def _near(got, want, absolute, dt, rows=0, what=""):
 
 class Case:
     def __init__(self, rows, n, groups=1, act="silu", x="f32", y="f32", pad=0, off=0, seed=0,
-                 weights=True, ckpt=False):
+                 weights=True, ckpt=0):
         rng = np.random.default_rng(seed)
         self.xt, self.yt, self.n, self.rows = x, y, n, rows
         self.groups, self.act, self.ckpt = groups, act, ckpt
@@ -59,10 +59,11 @@ class Case:
         self.gh = _rand(rng, (rows, n), y, **more)
         self.w = [_rand(rng, (1, n), "f32", 0.3, 1.0)[0].contiguous() if weights else None
                   for _ in range(3)]
-        self.d = snn.gate_norm_desc(self.x, self.y, self.g, groups, act, EPS, self.h)
+        self.d = snn.gate_norm_desc(self.x, self.y, self.g, groups, act, EPS, self.h,
+                                    ckpt_block=ckpt or 128)
         self.y8 = self.g8 = None
         if ckpt:
-            size = snn.snn_checkpoint_bytes(rows, n)
+            size = snn.snn_checkpoint_bytes(rows, n, ckpt)
             self.y8 = torch.empty(size, dtype=torch.uint8, device="cuda")
             self.g8 = torch.empty(size, dtype=torch.uint8, device="cuda") if self.g is not None \
                 else None
@@ -93,8 +94,8 @@ class Case:
                               dx, dy, dg, *dw, ws)
         y, g = _np(self.y), _np(self.g) if self.g is not None else None
         if self.ckpt:
-            y = ref.quantised(y).astype(np.float64)
-            g = ref.quantised(g).astype(np.float64) if g is not None else None
+            y = ref.quantised(y, self.ckpt).astype(np.float64)
+            g = ref.quantised(g, self.ckpt).astype(np.float64) if g is not None else None
         w_post, scale, w_pre = self.weights()
         want = ref.gate_norm_grads(_np(self.gx), _np(self.gh), _np(self.xo), y, g, self.groups,
                                    self.act, self.d.eps, w_post, scale, w_pre)
@@ -157,15 +158,16 @@ def test_gates_slices_and_absent_weights(act, types):
 @pytest.mark.parametrize("n,groups", [(64, 1), (100, 1), (384, 3), (1001, 1), (2048, 16),
                                       (5000, 1)])
 def test_backward_from_8_bit_checkpoints(n, groups, types):
-    for act in ("silu", "none"):
-        c = Case(40, n, groups, act, *types, ckpt=True, seed=n)
+    for act, block in (("silu", 128), ("none", 128), ("silu", 32), ("mul", 8)):
+        c = Case(40, n, groups, act, *types, ckpt=block, seed=n)
         c.fwd()
         for t, kept in ((c.y, c.y8), (c.g, c.g8)):
             if t is None:
                 continue
             back = torch.empty((40, n), device="cuda")
-            snn.snn_checkpoint_load(kept, back)
-            assert np.array_equal(back.cpu().numpy(), ref.quantised(t.float().cpu().numpy()))
+            snn.snn_checkpoint_load(kept, back, block)
+            assert np.array_equal(back.cpu().numpy(),
+                                  ref.quantised(t.float().cpu().numpy(), block))
         c.bwd()
 
 
@@ -287,30 +289,31 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("block", [128, 64, 16, 8])
 @pytest.mark.parametrize("rows,n", [(1, 1), (3, 127), (5, 128), (4, 129), (17, 1000), (300, 4104),
                                     (2000, 50)])
-def test_checkpoint_values(rows, n, dt):
+def test_checkpoint_values(rows, n, block, dt):
     rng = np.random.default_rng(n)
     wide = _rand(rng, (rows, n), dt, pad=5, off=2)
     scales = torch.as_tensor(10.0 ** rng.integers(-4, 4, (rows, 1)), device="cuda")
     wide.copy_(wide.float() * scales)
     for x in (wide, wide.contiguous()):
-        kept = torch.full((snn.snn_checkpoint_bytes(rows, n) + 64,), 77, dtype=torch.uint8,
-                          device="cuda")
-        snn.snn_checkpoint_save(x, kept)
+        kept = torch.full((snn.snn_checkpoint_bytes(rows, n, block) + 64,), 77,
+                          dtype=torch.uint8, device="cuda")
+        snn.snn_checkpoint_save(x, kept, block)
         assert (kept[-64:] == 77).all()
-        want = ref.quantised(x.float().cpu().numpy())
+        want = ref.quantised(x.float().cpu().numpy(), block)
         back = torch.full((rows, n), float("nan"), device="cuda")
-        snn.snn_checkpoint_load(kept, back)
+        snn.snn_checkpoint_load(kept, back, block)
         assert np.array_equal(back.cpu().numpy(), want)
         out = _nan_like(x)
-        snn.snn_checkpoint_load(kept, out)
+        snn.snn_checkpoint_load(kept, out, block)
         assert torch.equal(out.cpu(), torch.as_tensor(want).to(TYPES[dt]))
     # at most half a step of the block's scale from the value itself
     x32 = x.float().cpu().numpy()
-    for a in range(0, n, 128):
-        top = np.abs(x32[:, a:a + 128]).max(1, keepdims=True)
-        assert (np.abs(want[:, a:a + 128] - x32[:, a:a + 128]) <= top / 254 * (1 + 1e-4)).all()
+    for a in range(0, n, block):
+        top = np.abs(x32[:, a:a + block]).max(1, keepdims=True)
+        assert (np.abs(want[:, a:a + block] - x32[:, a:a + block]) <= top / 254 * (1 + 1e-4)).all()
 
 
 def test_checkpoint_of_zeros_tiny_and_bad_values():
@@ -345,7 +348,7 @@ def test_checkpoint_offsets_past_32_bits():
 
 
 def test_graph_replays():
-    c = Case(200, 768, 6, "silu", "f32", "f16", ckpt=True)
+    c = Case(200, 768, 6, "silu", "f32", "f16", ckpt=128)
     c.fwd(), c.bwd()
     want = {k: v.clone() for k, v in c.got.items()}
     want["xo"], want["h"] = c.xo.clone(), c.h.clone()
