@@ -73,6 +73,15 @@ __device__ inline float wave_max(float x) {
 #undef SNN_DPP_MAX
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
+// m = max(m, |a|, |b|), NaN ignored: one instruction, where fmaxf would first quiet
+// each operand
+__device__ inline void grow(float &m, float a, float b) {
+    asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(a), "v"(b));
+}
+__device__ inline void grow_finite(float &m, float a) {
+    a = __builtin_fabsf(a);
+    if (a < __builtin_inff()) m = fmaxf(m, a);
+}
 // The exponent e for which x 2^e lies in [2^14, 2^15), within [-120, 120]
 __device__ inline int scale_to_half(float x) {
     return min(120, max(-120, 14 + 127 - (int)((__float_as_uint(x) >> 23) & 255u)));
@@ -342,26 +351,24 @@ struct State {
     }
     // largest finite magnitude of the wave's part
     __device__ inline float largest() const {
-        float m = 0.f;
+        float m[4] = {};
+#pragma unroll
+        for (int a = 0; a < kTiles; ++a)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                grow(m[2 * p], s[a][p][0], s[a][p][1]);
+                grow(m[2 * p + 1], s[a][p][2], s[a][p][3]);
+            }
+        const float t = wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+        if (t < __builtin_inff()) return t;
+        m[0] = 0.f;
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
             for (int p = 0; p < 2; ++p)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) m = fmaxf(m, __builtin_fabsf(s[a][p][r]));
-        m = wave_max(m);
-        if (m < __builtin_inff()) return m;
-        m = 0.f;
-#pragma unroll
-        for (int a = 0; a < kTiles; ++a)
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = __builtin_fabsf(s[a][p][r]);
-                    if (x < __builtin_inff()) m = fmaxf(m, x);
-                }
-        return wave_max(m);
+                for (int r = 0; r < 4; ++r) grow_finite(m[0], s[a][p][r]);
+        return wave_max(m[0]);
     }
 };
 
@@ -518,11 +525,11 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                     near[x] = score[16 + l - 4 * g - x];
                     far[x] = score[32 + l - 4 * g - x];
                 }
-                float most = 0.f;
+                float most[2] = {};
 #pragma unroll
                 for (int t = 0; t < kTT; ++t)
 #pragma unroll
-                    for (int s = 0; s <= t; ++s)
+                    for (int s = 0; s <= t; ++s) {
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             float e = P[t][s][x];
@@ -530,14 +537,29 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                             else if (s + 1 == t) e *= far[x];
                             else e *= far[x] * tile[t - s - 1];
                             P[t][s][x] = e;
-                            if constexpr (kNorm) {
-                                const float a = __builtin_fabsf(e);
-                                most = fmaxf(most, a < __builtin_inff() ? a : 0.f);
-                            }
                         }
+                        if constexpr (kNorm) {
+                            grow(most[0], P[t][s][0], P[t][s][1]);
+                            grow(most[1], P[t][s][2], P[t][s][3]);
+                        }
+                    }
                 int exp_p = 0;
-                // at most 60: what smaller scores lose is far below an fp16 output's least step
-                if constexpr (kNorm) exp_p = min(60, scale_to_half(wave_max(most)));
+                // at most 60: what smaller scores lose is far below an fp16 output's least
+                // step
+                if constexpr (kNorm) {
+                    float m = wave_max(fmaxf(most[0], most[1]));
+                    if (!(m < __builtin_inff())) {  // of an infinite q or k: the finite ones'
+                        m = 0.f;
+#pragma unroll
+                        for (int t = 0; t < kTT; ++t)
+#pragma unroll
+                            for (int s = 0; s <= t; ++s)
+#pragma unroll
+                                for (int x = 0; x < 4; ++x) grow_finite(m, P[t][s][x]);
+                        m = wave_max(m);
+                    }
+                    exp_p = min(60, scale_to_half(m));
+                }
                 const float fp = pow2(exp_p), back = pow2(-exp_p);
 #pragma unroll
                 for (int t = 0; t < kTT; ++t) {
@@ -588,22 +610,29 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] *= wt[32 * u + 16 * (j >> 2) + (j & 3)];
             };
+            float w[kNorm ? kU : 1][2][8];
             if constexpr (kNorm) {
-                float most = 0.f;
+                float m[2] = {};
 #pragma unroll
                 for (int u = 0; u < kU; ++u)
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        float x[8];
-                        weighted(u, p, x);
+                        weighted(u, p, w[u][p]);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float a = __builtin_fabsf(x[j]);
-                            most = fmaxf(most, a < __builtin_inff() ? a : 0.f);
-                        }
+                        for (int j = 0; j < 8; j += 2) grow(m[p], w[u][p][j], w[u][p][j + 1]);
                     }
+                float most = wave_max(fmaxf(m[0], m[1]));
+                if (!(most < __builtin_inff())) {
+                    most = 0.f;
+#pragma unroll
+                    for (int u = 0; u < kU; ++u)
+#pragma unroll
+                        for (int p = 0; p < 2; ++p)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) grow_finite(most, w[u][p][j]);
+                    most = wave_max(most);
+                }
                 // the scale of this chunk's v g^j, unless the state would leave 2^61
-                most = wave_max(most);
                 int e = most > 0.f ? scale_to_half(most) : exp_s;
                 const float left_s = largest * __builtin_fabsf(gc);
                 if (left_s > 0.f)
@@ -621,10 +650,12 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
                     float x[8];
-                    weighted(u, p, x);
-                    if constexpr (kNorm)
+                    if constexpr (kNorm) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] *= fv;
+                        for (int j = 0; j < 8; ++j) x[j] = w[u][p][j] * fv;
+                    } else {
+                        weighted(u, p, x);
+                    }
 #pragma unroll
                     for (int m = 0; m < kParts; ++m) part[p][m] = take_part<T>(x);
                 }

@@ -229,6 +229,31 @@ def test_later_tokens_never_reach_earlier_outputs(what, value, dt):
 
 
 @pytest.mark.parametrize("dt", list(TYPES))
+def test_infinities_leave_other_columns_and_tokens_as_they_were(dt):
+    """Values far above fp16's range inside (scores and states to 1e6), cut into
+    segments: an infinity in one column of v, and one in a late k, change nothing
+    of the other columns and of the tokens before."""
+    c = Case(1100, 1, 1, 1, 64, 64, dt, std=40.0, decay=[0.9])
+    c.scale = 1e-4
+    c.d = snn.linattn_desc(c.q, c.k, c.v, c.o, c.scale)
+    wo, ws = ref.linattn(*c.arrays())
+    ao, as_ = ref.linattn(*c.arrays(np.abs))
+    keep = [i for i in range(64) if i != 9]
+    old = c.v[40, 0, 0, 9].item()
+    c.v[40, 0, 0, 9] = float("inf")
+    o, s = c.fwd()
+    c.tol(_np(o)[..., keep], wo[..., keep], ao[..., keep])
+    c.tol(_np(s)[..., keep], ws[..., keep], as_[..., keep], fp32=True)
+    c.v[40, 0, 0, 9] = old
+    c.k[1090, 0, 0, 3] = float("inf")
+    o, s = c.fwd()
+    c.tol(_np(o[:1090]), wo[:1090], ao[:1090])
+    assert not torch.isfinite(o[1090:]).any()
+    rows = [i for i in range(64) if i != 3]
+    c.tol(_np(s)[:, :, rows], ws[:, :, rows], as_[:, :, rows], fp32=True)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
 def test_state_carries_over_calls_and_in_place(dt):
     c = Case(130, 2, 2, 1, 64, 64, dt)
     whole, end = (x.clone() for x in c.fwd())
