@@ -503,7 +503,7 @@ size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d);
  *   decay     fp32 [heads], finite, meant for [0, 1]
  *   state_in  fp32 [B,heads,d_k,d_v], or NULL for zeros
  *   state_out fp32 [B,heads,d_k,d_v], or NULL; may be state_in
- * T == 0 copies the state; heads and B may be 0 (no work). */
+ * o overlaps no input.  T == 0 copies the state; heads and B may be 0 (no work). */
 snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void *k,
                            const void *v, const float *decay, const int32_t *lens,
                            const float *state_in, void *o, float *state_out, void *ws,
@@ -518,7 +518,9 @@ snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void 
  *   grad_o          strides of o
  *   grad_state_out  fp32 [B,heads,d_k,d_v], or NULL for zeros
  *   grad_q, grad_k, grad_v  strides of q, k, v; all required
- *   grad_state_in   fp32, or NULL to skip; may be grad_state_out */
+ *   grad_state_in   fp32, or NULL to skip; not grad_state_out (which other
+ *                   heads' workgroups may still read: SNN_ERR_UNSUPPORTED)
+ * No output may overlap an input or another output. */
 snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void *k,
                            const void *v, const float *decay, const int32_t *lens,
                            const float *state_in, const void *grad_o,

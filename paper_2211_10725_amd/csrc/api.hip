@@ -1049,6 +1049,8 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
     if (d->B == 0 || d->heads == 0) return SNN_OK;
     if (!decay || (d->T > 0 && (!q || !k || !v || !grad_o || !grad_q || !grad_k || !grad_v)))
         return SNN_ERR_NULL;
+    // grad_k's heads read the state's gradient while grad_v's may have written theirs
+    if (grad_state_in && grad_state_in == grad_state_out) return SNN_ERR_UNSUPPORTED;
     if (any_misaligned({q, k, v, decay, lens, state_in, grad_o, grad_state_out, grad_q, grad_k,
                         grad_v, grad_state_in, ws}))
         return SNN_ERR_ALIGN;

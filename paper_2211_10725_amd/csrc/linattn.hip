@@ -394,12 +394,6 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     const int begin = seg * c.seg_len, end = (int)min((int64_t)begin + c.seg_len, (int64_t)len);
     const int dk = r.dk, dv = r.dv;
     const float decay = c.decay[h];
-    for (int i = tid; i <= C; i += G::kThreads) pw[i] = decay_power(decay, i);
-    for (int i = tid; i < 2 * C; i += G::kThreads)
-        weight[i] = i < C ? r.ws * decay_power(decay, max(C - r.first - i, 0)) : 0.f;
-    if (tid < 48) score[tid] = r.rs * r.ws * decay_power(decay, max(tid - 16, 0));
-    if (tid < 2) flag[tid] = 0;
-
     Source<T, D> sq, sk, sv;
     const int last = r.reverse ? len - 1 : -1;  // len 0: no token is read
     if (OUT) sq.init(r.q, b, h, dk, last, begin);
@@ -409,6 +403,12 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     if (OUT) sq.load(end - begin, q4);
     sk.load(end - begin, k4);
     sv.load(end - begin, v4);
+
+    for (int i = tid; i <= C; i += G::kThreads) pw[i] = decay_power(decay, i);
+    for (int i = tid; i < 2 * C; i += G::kThreads)
+        weight[i] = i < C ? r.ws * decay_power(decay, max(C - r.first - i, 0)) : 0.f;
+    if (tid < 48) score[tid] = r.rs * r.ws * decay_power(decay, max(tid - 16, 0));
+    if (tid < 2) flag[tid] = 0;
 
     State<T, D> S;
     const int64_t at = (int64_t)bh * dk * dv;

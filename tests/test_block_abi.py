@@ -66,6 +66,8 @@ def test_linattn_pointers_and_workspace():
         assert call(ctypes.byref(d), *ptr[:i], None, *ptr[i + 1:], 16, 1 << 62, None) == NULL, i
     ptr[-1] = 16
     assert call(ctypes.byref(d), *ptr, 16, need - 1, None) == WORKSPACE
+    ptr[7] = 16  # the state's gradient in place
+    assert call(ctypes.byref(d), *ptr, 16, need, None) == UNSUPPORTED
 
 
 def test_linattn_step():

@@ -274,6 +274,23 @@ def test_state_carries_over_calls_and_in_place(dt):
     c.tol(_np(end), ws_, as_, fp32=True)
 
 
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,d", [(300, 64), (700, 64), (1500, 128)])
+def test_state_in_place_over_many_segments(T, d, dt):
+    """One head: the tokens are cut (2, 5 and 11 times), with the state given, in
+    place, apart and absent."""
+    c = Case(T, 1, 1, 1, d, d, dt, lens=[T - 70])
+    o, s = (x.clone() for x in c.fwd())
+    c.check_fwd()
+    state = c.s0.clone()
+    c.fwd(state_out=state, s0=state)
+    assert torch.equal(c.o, o) and torch.equal(state, s)
+    c.check_bwd()
+    z = Case(T, 1, 1, 1, d, d, dt, state=False)
+    z.check_fwd()
+    z.check_bwd()
+
+
 def test_no_tokens_and_no_sequences():
     for T, B, H, KV in ((0, 2, 2, 2), (5, 0, 2, 2)):
         c = Case(T, B, H, KV, 64, 64, "bf16")
