@@ -538,9 +538,10 @@ int threads_per_row(int n) {
 }
 int rows_per_block(int n) { return std::max(1, 256 / threads_per_row(n)); }
 
-// Workgroups of the backward, as many as are resident at once: its partial sums
-// are [2][blocks][n].
-int bwd_blocks(int64_t rows, int64_t n) {
+// Workgroups, as many as are resident at once (four of 256 threads per compute
+// unit; 16384 rows of 2048 there and back 255 us, with half as many 290, with 1.5
+// times 288).  The backward's partial sums are [2][blocks][n].
+int row_blocks(int64_t rows, int64_t n) {
     const int64_t rpb = rows_per_block((int)n);
     const int64_t most = 4 * kPlanCus * 256 / std::max(256, threads_per_row((int)n));
     return (int)std::min<int64_t>((rows + rpb - 1) / rpb, most);
@@ -556,14 +557,13 @@ int bwd_blocks(int64_t rows, int64_t n) {
 
 template <typename XT, typename YT>
 void run_fwd(const GateNormFwd &c, hipStream_t s) {
-    const int n = c.a.n, rpb = rows_per_block(n);
-    const int grid = (int)std::min<int64_t>((c.a.rows + rpb - 1) / rpb, 8 * kPlanCus);
+    const int n = c.a.n, grid = row_blocks(c.a.rows, n);
     GATE_NORM_SIZES(gate_norm_fwd_kernel, XT, YT)
 }
 
 template <typename XT, typename YT>
 void run_bwd(const GateNormBwd &c, hipStream_t s) {
-    const int n = c.a.n, grid = bwd_blocks(c.a.rows, n);
+    const int n = c.a.n, grid = row_blocks(c.a.rows, n);
     if (grid > 0) {
         if (c.y8) {
             GATE_NORM_SIZES(gate_norm_bwd_kernel, XT, YT, true)
@@ -602,7 +602,7 @@ void run_checkpoint(int64_t rows, int n, int block, int64_t ld, void *x, int8_t 
 }  // namespace
 
 size_t gate_norm_workspace_bytes(int64_t rows, int64_t n) {
-    return align_up((size_t)2 * bwd_blocks(rows, n) * n * sizeof(float));
+    return align_up((size_t)2 * row_blocks(rows, n) * n * sizeof(float));
 }
 
 hipError_t launch_gate_norm_fwd(const GateNormFwd &c, int xt, int yt, hipStream_t s) {
