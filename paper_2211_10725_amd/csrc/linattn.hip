@@ -954,15 +954,16 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
 
 }  // namespace
 
-// Segments that fill the device: two workgroups of 128 head values for each
-// compute unit, or three of 64, as near as whole segments come to it; a segment
-// has 128 tokens or more.  Bf16 training of 128 heads of 128 (2048 tokens): the
-// forward in 4 segments 130 us, in 2 149; the backward's three roles uncut 276, in
-// 2 283.  1000 tokens of 128 heads of 64 (fp16): 6 segments 50 us, 3 60.
+// As many segments as the workgroups resident at once have room for: two of 128
+// head values on a compute unit, four of 64; a segment has 128 tokens or more.
+// Bf16 training of 128 heads of 128 (2048 tokens): the forward in 4 segments 130
+// us, in 2 149; the backward's 384 heads and roles uncut 276, in 2 283 (and with a
+// short segment for the 128 slots left 282).  Fp32 of 256 heads of 64 (512
+// tokens): the forward in 4 segments 70 us, in 3 85.
 LaPlan linattn_plan(int T, int64_t heads, int roles, int width) {
-    const int64_t want = (width > 64 ? 2 : 3) * kPlanCus;
-    const int64_t have = std::max<int64_t>(heads * roles, 1);
-    const int64_t segs = std::min<int64_t>((want + have / 2) / have, T / 128);
+    const int64_t slots = (width > 64 ? 2 : 4) * kPlanCus;
+    const int64_t segs =
+        std::min<int64_t>(slots / std::max<int64_t>(heads * roles, 1), T / 128);
     LaPlan p;
     p.segs = 1;
     p.seg_len = std::max(T, 1);
