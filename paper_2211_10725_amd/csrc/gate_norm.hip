@@ -11,6 +11,10 @@
 // Workgroups take rows in turn with the weights in registers, and the
 // backward's column sums too: one partial row per workgroup, added in
 // workgroup order by a second kernel.
+//
+// Bound by HBM.  16384 rows of 2048 (bf16 block, fp32 residual stream, 16 heads):
+// forward 93 us, 5.0 TB/s, as a large copy; backward 155 to 164, 4.5 to 4.8 TB/s.
+// 8192 rows of 4096 (fp16) with 8-bit checkpoints: 119 and 166.
 #include "snn_internal.hpp"
 
 namespace snn {
