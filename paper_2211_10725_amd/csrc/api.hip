@@ -914,7 +914,7 @@ bool any_misaligned(std::initializer_list<const void *> ps) {
 }
 
 LaOperand operand(const void *p, const int64_t *st, int share) {
-    return LaOperand{p, st[0], st[1], st[2], share};
+    return LaOperand{p, st[0], st[1], st[2], 1.0 / share};
 }
 
 void set_out(LaRole &r, void *o, const int64_t *st) {

@@ -69,6 +69,12 @@ __device__ inline float decay_power(float g, int e) {
     return (float)r;
 }
 
+// n / d of uniform 0 <= n < 2^31 by 1 / d in fp64, which is exact: n + 1/2 is never
+// within an error of a multiple of d.  An integer division takes ten times the
+// instructions.
+__device__ inline int divided(int n, double by) {
+    return __builtin_amdgcn_readfirstlane((int)((n + 0.5) * by));
+}
 __device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
 // largest of 64 lanes' values >= 0, the same in every lane
@@ -203,7 +209,7 @@ struct Source {
         typedef Geo<T, D> G;
         const int run = threadIdx.x % G::kRuns, row = threadIdx.x / G::kRuns;
         step = last >= 0 ? -x.st : x.st;
-        lane = static_cast<const T *>(x.p) + b * x.sb + (int64_t)(h / x.share) * x.sh +
+        lane = static_cast<const T *>(x.p) + b * x.sb + (int64_t)divided(h, x.by_share) * x.sh +
                (last >= 0 ? last * x.st : 0) + (begin + row) * step + run * G::kRun;
         live = run * G::kRun < width;
         whole = width == D;
@@ -288,31 +294,50 @@ struct State {
     }
     __device__ static inline int row(int a) { return row(a, threadIdx.x & 63); }
     __device__ static inline int col(int p) { return col(p, threadIdx.x >> 6, threadIdx.x & 63); }
+    // from and to [dk][dv] (trans: [dv][dk]) in memory; what is out of range is
+    // read as row 0, column 0 and dropped, so that no branch holds a load back
     __device__ inline void load(const float *from, bool trans, int dk, int dv) {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (!from || row(a) >= dk || col(p) >= dv) continue;
-                if (trans) {
-                    s[a][p] = *reinterpret_cast<const f32x4 *>(from + (int64_t)col(p) * dk + row(a));
-                } else {
+            for (int p = 0; p < 2; ++p) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (!from) return;
+        if (trans) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        s[a][p][r] = from[(int64_t)(row(a) + r) * dv + col(p)];
+            for (int a = 0; a < kTiles; ++a)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const bool in = row(a) < dk && col(p) < dv;
+                    s[a][p] = *reinterpret_cast<const f32x4 *>(
+                        from + (in ? col(p) * dk + row(a) : 0));
                 }
-            }
+        } else {
+#pragma unroll
+            for (int a = 0; a < kTiles; ++a)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const float *x = from + (row(a) < dk && col(p) < dv ? row(a) * dv + col(p) : 0);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[a][p][r] = x[r * dv];
+                }
+        }
+        if (dk < D || dv < D)
+#pragma unroll
+            for (int a = 0; a < kTiles; ++a)
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+                    if (row(a) >= dk || col(p) >= dv) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __device__ inline void store(float *to, int dk, int dv) const {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
             for (int p = 0; p < 2; ++p)
-                if (row(a) < dk && col(p) < dv)
+                if (row(a) < dk && col(p) < dv) {
+                    float *x = to + row(a) * dv + col(p);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        to[(int64_t)(row(a) + r) * dv + col(p)] = s[a][p][r];
+                    for (int r = 0; r < 4; ++r) x[r * dv] = s[a][p][r];
+                }
     }
     // Segment states between launches: a wave's tiles as they lie in its registers,
     // 16 bytes per lane.
@@ -398,9 +423,13 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     __shared__ int flag[2];
 
     const int item = xcd_local_item();
-    const LaRole &r = c.role[item % c.roles];
-    const int seg = item / c.roles % c.segs, bh = item / c.roles / c.segs;
-    const int b = bh / c.H, h = bh % c.H;
+    const int unit = divided(item, c.by_roles), bh = divided(unit, c.by_segs);
+    const int seg = unit - bh * c.segs, b = divided(bh, c.by_heads), h = bh - b * c.H;
+    const LaRole r = c.role[item - unit * c.roles];
+    // every line of the arguments on its way at once
+    asm volatile("" ::"s"(r.q.p), "s"(r.k.st), "s"(r.v.p), "s"(r.v.by_share), "s"(r.o),
+                 "s"(r.o_f32), "s"(r.final_state), "s"(r.rs), "s"(r.slot), "s"(r.slot_trans),
+                 "s"(c.decay), "s"(c.T), "s"(c.segs));
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 15, g = lane >> 4;
     const int len = c.lens ? min(max(c.lens[b], 0), c.T) : c.T;
     const int begin = seg * c.seg_len, end = (int)min((int64_t)begin + c.seg_len, (int64_t)len);
@@ -416,10 +445,8 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     sk.load(end - begin, k4);
     sv.load(end - begin, v4);
 
-    for (int i = tid; i <= C; i += G::kThreads) pw[i] = decay_power(decay, i);
-    for (int i = tid; i < 2 * C; i += G::kThreads)
-        weight[i] = i < C ? r.ws * decay_power(decay, max(C - r.first - i, 0)) : 0.f;
-    if (tid < 48) score[tid] = r.rs * r.ws * decay_power(decay, max(tid - 16, 0));
+    static_assert(C < G::kThreads);
+    if (tid <= C) pw[tid] = decay_power(decay, tid);
     if (tid < 2) flag[tid] = 0;
 
     State<T, D> S;
@@ -449,6 +476,9 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     const int64_t obytes = ostep * (o_f32 ? 4 : sizeof(T));
 
     __syncthreads();
+    for (int i = tid; i < 2 * C; i += G::kThreads)
+        weight[i] = i < C ? r.ws * pw[max(C - r.first - i, 0)] : 0.f;
+    if (tid < 48) score[tid] = r.rs * r.ws * pw[max(tid - 16, 0)];
     float tile[kTT];  // decays from tile to tile of 16 tokens
 #pragma unroll
     for (int t = 0; t < kTT; ++t)
@@ -858,7 +888,7 @@ __global__ __launch_bounds__(256) void group_sum_kernel(const float *src, T *dst
 template <typename T>
 __device__ inline float load_value(const LaOperand &x, int t, int b, int h, int i) {
     return (float)static_cast<const T *>(
-        x.p)[t * x.st + b * x.sb + (int64_t)(h / x.share) * x.sh + i];
+        x.p)[t * x.st + b * x.sb + (int64_t)divided(h, x.by_share) * x.sh + i];
 }
 
 // One token of every request.  The state is read and written once, 16 bytes per
@@ -873,8 +903,8 @@ template <typename T>
 __global__ __launch_bounds__(kStepThreads) void linattn_step_kernel(LaStep c) {
     __shared__ float qs[kLaMaxD], ks[kLaMaxD], part[kStepThreads * 4];
     const int tid = threadIdx.x;
-    const int slice = blockIdx.x % c.slices, bh = blockIdx.x / c.slices;
-    const int h = bh % c.H, b = bh / c.H;
+    const int bh = divided(blockIdx.x, c.by_slices), slice = blockIdx.x - bh * c.slices;
+    const int b = divided(bh, c.by_heads), h = bh - b * c.H;
     const int slot = c.slots ? c.slots[b] : b;
     const int col0 = slice * c.cols, cols = min(c.cols, c.dv - col0);
     T *o = static_cast<T *>(c.o) + b * c.ob + h * c.oh + col0;
@@ -933,9 +963,16 @@ __global__ __launch_bounds__(kStepThreads) void linattn_step_kernel(LaStep c) {
     }
 }
 
+void set_divisors(LaCall &c) {
+    c.by_roles = 1.0 / c.roles;
+    c.by_segs = 1.0 / c.segs;
+    c.by_heads = 1.0 / c.H;
+}
+
 template <typename T, int D>
 hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
     LaCall out = c;
+    set_divisors(out);
     if (c.segs > 1) {
         // the roles that own slots
         LaCall own = c;
@@ -943,6 +980,7 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
         for (int i = 0; i < c.roles; ++i)
             if (!c.role[i].slot_trans) own.role[own.roles++] = c.role[i];
         own.segs = c.segs - 1;
+        set_divisors(own);
         linattn_kernel<T, D, false><<<own.roles * c.B * c.H * own.segs, 2 * D, 0, s>>>(own);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -1031,6 +1069,8 @@ hipError_t launch_linattn_step(const LaStep &call, int B, int dtype, hipStream_t
     c.cols = c.dv;
     while (c.cols % 64 == 0 && (int64_t)B * c.H * (c.dv / c.cols) < 4 * kPlanCus) c.cols /= 2;
     c.slices = c.dv / c.cols;
+    c.by_slices = 1.0 / c.slices;
+    c.by_heads = 1.0 / c.H;
     const int grid = B * c.H * c.slices;
     switch (dtype) {
         case SNN_F32: linattn_step_kernel<float><<<grid, kStepThreads, 0, s>>>(c); break;

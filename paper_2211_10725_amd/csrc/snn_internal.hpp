@@ -302,11 +302,11 @@ struct FusedStep {
 hipError_t launch_fused_step(const FusedStep &f, void *ws, hipStream_t s);
 
 // ---- linear attention with a decay per head (linattn.hip) ----------------------
-// One operand, element (t, b, h, i) at t st + b sb + (h / share) sh + i.
+// One operand, element (t, b, h, i) at t st + b sb + floor(h / share) sh + i.
 struct LaOperand {
     const void *p;
     int64_t st, sb, sh;
-    int share;  // query heads that read the same head
+    double by_share;  // one over the query heads that read the same head
 };
 // One recurrence over the tokens n = 0 .. len - 1 (token n from the end where
 // reverse): with X the state that enters token n (X = init before the first),
@@ -335,6 +335,7 @@ struct LaCall {
     const int32_t *lens;
     int T, B, H;
     int roles, segs, seg_len;
+    double by_roles, by_segs, by_heads;  // set by the launcher: one over each
     int summed, copied;  // set by the launcher: slots hold the states that enter
                          // segments, the first one's too
 };
@@ -359,6 +360,7 @@ struct LaStep {
     void *o;
     float scale;
     int cols, slices;  // set by the launcher: columns of v per workgroup
+    double by_slices, by_heads;
 };
 hipError_t launch_linattn_step(const LaStep &c, int B, int dtype, hipStream_t s);
 
