@@ -925,7 +925,8 @@ void set_out(LaRole &r, void *o, const int64_t *st) {
 }
 
 LaPlan plan_of(const snn_linattn_desc *d, int roles) {
-    return linattn_plan(d->T, (int64_t)d->B * d->heads, roles, std::max(d->d_k, d->d_v));
+    return linattn_plan(d->T, (int64_t)d->B * d->heads, roles, std::max(d->d_k, d->d_v),
+                        d->dtype);
 }
 
 LaCall linattn_call(const snn_linattn_desc *d, const float *decay, const int32_t *lens, int roles) {

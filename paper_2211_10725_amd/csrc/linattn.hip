@@ -1007,22 +1007,29 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
 
 }  // namespace
 
-// As many segments as the workgroups resident at once have room for: two of 128
-// head values on a compute unit, four of 64; a segment has 128 tokens or more.
-// Bf16 training of 128 heads of 128 (2048 tokens): the forward in 4 segments 130
-// us, in 2 149; the backward's 384 heads and roles uncut 276, in 2 283 (and with a
-// short segment for the 128 slots left 282).  Fp32 of 256 heads of 64 (512
-// tokens): the forward in 4 segments 70 us, in 3 85.
-LaPlan linattn_plan(int T, int64_t heads, int roles, int width) {
+// As many segments of 128 tokens or more as the workgroups resident at once have room
+// for: two of 128 head values on a compute unit, four of 64.  Bf16 training of 128
+// heads of 128 (2048 tokens): the forward in 4 segments 130 us, in 2 149; the
+// backward's 384 heads and roles uncut 276, in 2 283 (and with a short segment for the
+// 128 slots left 282).  Fp32 of 256 heads of 64 (512 tokens): the forward in 4
+// segments 70 us, in 3 85.
+// While each has a compute unit to itself, shorter ones too: a chunk of 32 tokens in
+// fp32 (30 heads of 128 there and back, 101 tokens: 63 us, uncut 74; 8 heads, 1000
+// tokens: 107, in seven 169), 64 tokens in 16 bits from three on (the same in bf16,
+// 1000 tokens: 62 against 67; 128 tokens in two 35, uncut 30).
+LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype) {
     const int64_t slots = (width > 64 ? 2 : 4) * kPlanCus;
-    const int64_t segs =
-        std::min<int64_t>(slots / std::max<int64_t>(heads * roles, 1), T / 128);
+    const int64_t units = std::max<int64_t>(heads * roles, 1);
+    const int least = dtype == SNN_F32 ? 32 : 64, most = (T - 1) / least + 1;
+    int64_t segs = std::min<int64_t>(slots / units, T / 128);
+    if (dtype == SNN_F32 || most > 2)
+        segs = std::max(segs, std::min<int64_t>(kPlanCus / units, most));
     LaPlan p;
     p.segs = 1;
     p.seg_len = std::max(T, 1);
     p.slot_bytes = 0;
     if (segs > 1) {
-        p.seg_len = (int)(((T + segs - 1) / segs + 63) / 64 * 64);
+        p.seg_len = (int)(((T + segs - 1) / segs + least - 1) / least * least);
         p.segs = (T + p.seg_len - 1) / p.seg_len;
         if (p.segs > 1) {
             const size_t d = width > 64 ? 128 : 64;

@@ -344,7 +344,7 @@ struct LaPlan {
     size_t slot_bytes;  // of one role's segment states, 0 for one segment
 };
 // heads: sequences by query heads; width: the larger head size
-LaPlan linattn_plan(int T, int64_t heads, int roles, int width);
+LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype);
 hipError_t launch_linattn(const LaCall &c, int dtype, hipStream_t s);
 // dst (strided [T, B, KV, d] of dtype) = src fp32 [T, B, KV * share, d] summed
 // over each group of `share` heads
