@@ -487,6 +487,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
         tile[t] = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(pw[16 * t])));
     const float row = r.rs * pw[l] * (r.first ? decay : 1.f);
 
+    const bool keep = r.final_state && seg + 1 == c.segs;  // the last chunk's state is used
     int par = 0;
     for (int n = begin; n < end; par ^= 1) {
         int count = min(C, end - n);
@@ -647,6 +648,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
 #pragma unroll
                     for (int p = 0; p < 2; ++p) vf[u][p] = read_columns<T, D>(tv, u, wave, p);
             }
+            if (OUT && left <= 0 && !keep) break;
             // the state's update
             const float *wt = weight + (C - count) + 4 * g;
             auto weighted = [&](int u, int p, float (&x)[8]) {
@@ -783,6 +785,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                                     O[t][p];
                 }
             }
+            if (OUT && left <= 0 && !keep) break;
             S.scale(gc);
 #pragma unroll
             for (int s = 0; s < kTT; ++s)
@@ -817,7 +820,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                 z[0] = z[1] = u32x4{0, 0, 0, 0};
             }
         }
-        if (r.final_state && seg + 1 == c.segs) S.store(r.final_state + at, dk, dv);
+        if (keep) S.store(r.final_state + at, dk, dv);
     } else {
         S.store_slot(slot + (seg + 1) * slot_seg);
     }
