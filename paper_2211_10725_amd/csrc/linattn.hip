@@ -10,10 +10,10 @@
 // all of it on the matrix cores:
 //   o_i = rs (sum_{j<=i} g^{i-j} ws (q_i.k_j) v_j + g^{i+first} q_i X)
 //   X'  = g^C X + sum_j g^{C-first-j} ws k_j^T v_j
-// A wave owns 32 columns of v and the state's columns with them, in registers,
-// so waves exchange nothing but the staged tiles of q, k and v; each computes
-// the chunk's scores q.k for itself (12 % of its matrix instructions at d = 128,
-// 18 % at 64).  Every product is arranged so that a result lies in the registers
+// A wave owns 32 columns of v (fp32 often 16) and the state's columns with them, in
+// registers, so waves exchange nothing but the staged tiles of q, k and v; each
+// computes the chunk's scores q.k for itself (in 16 bits 12 % of its matrix
+// instructions at d = 128, 18 % at 64; in fp32 of 64 39 %).  Every product is arranged so that a result lies in the registers
 // as the next product's operand: scores and output are taken transposed (s x t,
 // dv x t), and the 16 rows of a result tile are the k values 4 g + r that lane
 // group g holds of an operand, in whatever order, as long as both operands agree.
@@ -42,7 +42,7 @@
 // the matrix cores are busy in 42 %, waves wait in 25 %.  Of the vector
 // instructions half decay and split the state, a quarter split v g^j.  fp32 is
 // bound by the fp32 matrix instructions: 512 tokens of 256 heads of 64, forward
-// and backward, 219 us, of which they take about half.
+// and backward, 195 us, of which they take more than half.
 #include <type_traits>
 
 #include "snn_internal.hpp"
@@ -168,16 +168,26 @@ __device__ inline void unpack(const u32x4 &p, float (&x)[8]) {
 }
 
 // ---- geometry ----------------------------------------------------------------------
-// D: head sizes up to 64 or 128, padded with zeros.  A wave has 32 columns, so
-// D / 32 waves make a workgroup; each thread stages four 16-byte runs of every
-// tile.
-template <typename T, int D>
+// D: head sizes up to 64 or 128, padded with zeros.  N: columns of a wave, one tile
+// or a pair, so D / N waves make a workgroup.
+//
+// 16-bit types take 32: what a wave does for the scores, it does for more columns.
+// fp32 takes 16 at d = 64, where the registers then hold four waves of a SIMD instead
+// of two (512 tokens of 256 heads there and back 195 us against 213, of 64 heads 73
+// against 93).  At 128 they do not: 16 while each workgroup has a compute unit to
+// itself (101 tokens of 30 heads there and back 55 us against 61), else 32 (512 tokens
+// of 256 heads 512 us against 596).
+template <typename T, int D, int N>
 struct Geo {
     static constexpr bool kHalf = sizeof(T) == 2;
     // Tokens of a chunk: 64 where the registers hold that, else 32 (at d = 128 64 spill,
     // and 512 x 16 tokens and heads took 174 us against 142).
     static constexpr int C = kHalf && D == 64 ? 64 : 32;
-    static constexpr int kWaves = D / 32, kThreads = 64 * kWaves;
+    static constexpr int kPairs = N / 16, kWaves = D / N, kThreads = 64 * kWaves;
+    static constexpr int kEu = kHalf || D > 64 ? 2 : 4;  // waves of a SIMD at least
+    // fp32: tiles of the head that a product takes together, for independent sums (at
+    // 128 others run meanwhile, and one leaves less padding)
+    static constexpr int kStep = D > 64 ? 1 : 2;
     static constexpr int kRun = 16 / sizeof(T);       // values of a 16-byte run
     static constexpr int kRuns = D / kRun;            // runs of a row
     static constexpr int kRows = kThreads / kRuns;    // rows that the threads stage at once
@@ -201,14 +211,14 @@ struct Geo {
 
 // Rows of one operand for this workgroup's sequence and head: token n of the
 // recurrence lies at base + n step.
-template <typename T, int D>
+template <typename T, int D, int N>
 struct Source {
     const T *lane;  // this thread's run in the first row it stages of the next chunk
     int64_t step;
     bool live;      // the run lies within the head
     bool whole;     // the head fills the row
     __device__ inline void init(const LaOperand &x, int b, int h, int width, int last, int begin) {
-        typedef Geo<T, D> G;
+        typedef Geo<T, D, N> G;
         const int run = threadIdx.x % G::kRuns, row = threadIdx.x / G::kRuns;
         step = last >= 0 ? -x.st : x.st;
         lane = static_cast<const T *>(x.p) + b * x.sb + (int64_t)divided(h, x.by_share) * x.sh +
@@ -217,8 +227,8 @@ struct Source {
         whole = width == D;
     }
     // the next `count` tokens, zeros past them and past the head
-    __device__ inline void load(int count, u32x4 (&v)[Geo<T, D>::kVec]) const {
-        typedef Geo<T, D> G;
+    __device__ inline void load(int count, u32x4 (&v)[Geo<T, D, N>::kVec]) const {
+        typedef Geo<T, D, N> G;
         if (whole && count >= G::C) {
 #pragma unroll
             for (int i = 0; i < G::kVec; ++i)
@@ -234,8 +244,8 @@ struct Source {
         }
     }
     __device__ inline void advance(int tokens) { lane += tokens * step; }
-    __device__ static inline void stage(T *tile, const u32x4 (&v)[Geo<T, D>::kVec]) {
-        typedef Geo<T, D> G;
+    __device__ static inline void stage(T *tile, const u32x4 (&v)[Geo<T, D, N>::kVec]) {
+        typedef Geo<T, D, N> G;
         const int run = threadIdx.x % G::kRuns, row = threadIdx.x / G::kRuns;
 #pragma unroll
         for (int i = 0; i < G::kVec; ++i)
@@ -269,7 +279,7 @@ __device__ inline bool not_finite(const u32x4 (&v)[N]) {
 // of 32: a lane's results of both pairs are 8 neighbours in memory.
 template <typename T, int D>
 __device__ inline u32x4 read_columns(const T *tile, int u, int block, int p) {
-    typedef Geo<T, D> G;
+    typedef Geo<T, D, 32> G;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int lane = threadIdx.x & 63, g = lane >> 4, L = lane & 15;
     const int row = 32 * u + 4 * g + (L >> 2);
@@ -282,17 +292,17 @@ __device__ inline u32x4 read_columns(const T *tile, int u, int block, int p) {
 
 // The state's columns of one wave: tile (a, p) holds rows row(a) + r and column
 // col(p), r = 0 .. 3.
-template <typename T, int D>
+template <typename T, int D, int N>
 struct State {
-    static constexpr int kTiles = D / 16;
-    f32x4 s[kTiles][2];
+    static constexpr int kTiles = D / 16, kPairs = N / 16;
+    f32x4 s[kTiles][kPairs];
     __device__ static inline int row(int a, int lane) {
         const int g = lane >> 4;
         return sizeof(T) == 2 ? 32 * (a >> 1) + 8 * g + 4 * (a & 1) : 16 * a + 4 * g;
     }
     __device__ static inline int col(int p, int w, int lane) {
         const int i = lane & 15;
-        return 32 * w + (sizeof(T) == 2 ? 8 * (i >> 2) + 4 * p + (i & 3) : 16 * p + i);
+        return N * w + (sizeof(T) == 2 ? 8 * (i >> 2) + 4 * p + (i & 3) : 16 * p + i);
     }
     __device__ static inline int row(int a) { return row(a, threadIdx.x & 63); }
     __device__ static inline int col(int p) { return col(p, threadIdx.x >> 6, threadIdx.x & 63); }
@@ -302,13 +312,13 @@ struct State {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int p = 0; p < kPairs; ++p) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (!from) return;
         if (trans) {
 #pragma unroll
             for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int p = 0; p < kPairs; ++p) {
                     const bool in = row(a) < dk && col(p) < dv;
                     s[a][p] = *reinterpret_cast<const f32x4 *>(
                         from + (in ? col(p) * dk + row(a) : 0));
@@ -317,7 +327,7 @@ struct State {
 #pragma unroll
             for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int p = 0; p < kPairs; ++p) {
                     const float *x = from + (row(a) < dk && col(p) < dv ? row(a) * dv + col(p) : 0);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[a][p][r] = x[r * dv];
@@ -327,14 +337,14 @@ struct State {
 #pragma unroll
             for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                for (int p = 0; p < kPairs; ++p)
                     if (row(a) >= dk || col(p) >= dv) s[a][p] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __device__ inline void store(float *to, int dk, int dv) const {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+            for (int p = 0; p < kPairs; ++p)
                 if (row(a) < dk && col(p) < dv) {
                     float *x = to + row(a) * dv + col(p);
 #pragma unroll
@@ -346,35 +356,36 @@ struct State {
     static constexpr int kSlot = D * D;
     __device__ static inline f32x4 *own(float *slot, int a, int p) {
         return reinterpret_cast<f32x4 *>(slot) +
-               (((threadIdx.x >> 6) * kTiles + a) * 2 + p) * 64 + (threadIdx.x & 63);
+               (((threadIdx.x >> 6) * kTiles + a) * kPairs + p) * 64 + (threadIdx.x & 63);
     }
     __device__ inline void store_slot(float *slot) const {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) *own(slot, a, p) = s[a][p];
+            for (int p = 0; p < kPairs; ++p) *own(slot, a, p) = s[a][p];
     }
     // s = f s + the slot (trans: of a role whose state is this one transposed)
     __device__ inline void add_slot(float f, float *slot, bool trans) {
         if (trans) {
-            // row col(p) and columns row(a) .. + 3 of the slot's state: tile 2 w + p, column
-            // block a / 2, half a % 2, lanes 16 (l / 4) + 4 g .. + 3
+            // row col(p) and columns row(a) .. + 3 of the slot's state: row tile kPairs w + p,
+            // column tile a, lanes 16 (l / 4) + 4 g .. + 3
             const int w = threadIdx.x >> 6, g = (threadIdx.x & 63) >> 4, l = threadIdx.x & 15;
-            const float *from = slot + 1024 * w + 64 * (l >> 2) + 16 * g + (l & 3);
+            const float *from = slot + 256 * kPairs * kPairs * w + 64 * (l >> 2) + 16 * g + (l & 3);
 #pragma unroll
             for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                for (int p = 0; p < kPairs; ++p)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         s[a][p][r] = __builtin_fmaf(
                             f, s[a][p][r],
-                            from[512 * kTiles * (a >> 1) + 512 * p + 256 * (a & 1) + 4 * r]);
+                            from[256 * (kTiles * (a / kPairs * kPairs) + kPairs * p + a % kPairs) +
+                                 4 * r]);
         } else {
 #pragma unroll
             for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int p = 0; p < kPairs; ++p) {
                     const f32x4 x = *own(slot, a, p);
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
@@ -386,7 +397,7 @@ struct State {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) s[a][p] *= f;
+            for (int p = 0; p < kPairs; ++p) s[a][p] *= f;
     }
     // largest finite magnitude of the wave's part
     __device__ inline float largest() const {
@@ -394,7 +405,7 @@ struct State {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
+            for (int p = 0; p < kPairs; ++p) {
                 grow(m[2 * p], s[a][p][0], s[a][p][1]);
                 grow(m[2 * p + 1], s[a][p][2], s[a][p][3]);
             }
@@ -404,7 +415,7 @@ struct State {
 #pragma unroll
         for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+            for (int p = 0; p < kPairs; ++p)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) grow_finite(m[0], s[a][p][r]);
         return wave_max(m[0]);
@@ -413,9 +424,10 @@ struct State {
 
 // One workgroup: one role, sequence, head and segment.  OUT: outputs (and the
 // final state); else the segment's own state alone, into its slot.
-template <typename T, int D, bool OUT>
-__global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
-    typedef Geo<T, D> G;
+template <typename T, int D, int N, bool OUT>
+__global__ __launch_bounds__((Geo<T, D, N>::kThreads), (Geo<T, D, N>::kEu))
+void linattn_kernel(LaCall c) {
+    typedef Geo<T, D, N> G;
     constexpr int C = G::C, kTT = C / 16, kU = C / 32;  // tiles of 16 tokens
     constexpr bool kHalf = G::kHalf, kNorm = std::is_same_v<T, half_t>;
     __shared__ __attribute__((aligned(16))) T tq[OUT ? G::kTile : 8], tk[G::kTile], tv[G::kTile];
@@ -437,7 +449,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     const int begin = seg * c.seg_len, end = (int)min((int64_t)begin + c.seg_len, (int64_t)len);
     const int dk = r.dk, dv = r.dv;
     const float decay = c.decay[h];
-    Source<T, D> sq, sk, sv;
+    Source<T, D, N> sq, sk, sv;
     const int last = r.reverse ? len - 1 : -1;  // len 0: no token is read
     if (OUT) sq.init(r.q, b, h, dk, last, begin);
     sk.init(r.k, b, h, dk, last, begin);
@@ -451,12 +463,12 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     if (tid <= C) pw[tid] = decay_power(decay, tid);
     if (tid < 2) flag[tid] = 0;
 
-    State<T, D> S;
+    State<T, D, N> S;
     const int64_t at = (int64_t)bh * dk * dv;
     // the state that enters this segment: the first one's is given; another's is in
     // its slot, or (few segments) the sum of those before it
-    const int64_t slot_seg = (int64_t)c.B * c.H * State<T, D>::kSlot;
-    float *slot = r.slot + (int64_t)bh * State<T, D>::kSlot;
+    const int64_t slot_seg = (int64_t)c.B * c.H * State<T, D, N>::kSlot;
+    float *slot = r.slot + (int64_t)bh * State<T, D, N>::kSlot;
     const bool ready = c.summed && (seg > 0 || c.copied);
     S.load(OUT && r.init && !ready ? r.init + at : nullptr, r.trans, dk, dv);
     if (OUT && c.segs > 1) {
@@ -471,7 +483,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     // this lane's token and columns of the output, and their step over tokens
     const int64_t ostep = r.reverse ? -r.ot : r.ot;
     const bool o_f32 = r.o_f32;
-    const int ocol = 32 * wave + (kHalf ? 8 * g : 4 * g);
+    const int ocol = N * wave + (kHalf ? 8 : 4) * g;
     char *out = static_cast<char *>(r.o) +
                 (b * r.ob + h * r.oh + (r.reverse ? (len - 1) * r.ot : 0) + (begin + l) * ostep +
                  ocol) * (int64_t)(o_f32 ? 4 : sizeof(T));
@@ -492,9 +504,9 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
     for (int n = begin; n < end; par ^= 1) {
         int count = min(C, end - n);
         __syncthreads();  // the previous chunk's reads are done
-        if (OUT) Source<T, D>::stage(tq, q4);
-        Source<T, D>::stage(tk, k4);
-        Source<T, D>::stage(tv, v4);
+        if (OUT) Source<T, D, N>::stage(tq, q4);
+        Source<T, D, N>::stage(tk, k4);
+        Source<T, D, N>::stage(tv, v4);
         if (OUT && __any(not_finite<T, G::kVec>(v4)) && lane == 0) flag[par] = 1;
         __syncthreads();
         if (OUT && flag[par]) {  // the whole workgroup: one token alone
@@ -706,7 +718,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                     for (int m = 0; m < kParts; ++m) part[p][m] = take_part<T>(x);
                 }
 #pragma unroll
-                for (int a = 0; a < State<T, D>::kTiles; ++a) {
+                for (int a = 0; a < State<T, D, N>::kTiles; ++a) {
                     const u32x4 kt = read_columns<T, D>(tk, u, a >> 1, a & 1);
 #pragma unroll
                     for (int m = kParts - 1; m >= 0; --m)
@@ -714,30 +726,33 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                         for (int p = 0; p < 2; ++p) S.s[a][p] = mfma<T>(kt, part[p][m], S.s[a][p]);
                 }
             }
-        } else if (32 * wave < dv) {
+        } else if (N * wave < dv) {
             const float *fq = reinterpret_cast<const float *>(tq),
                         *fk = reinterpret_cast<const float *>(tk),
                         *fv = reinterpret_cast<const float *>(tv);
-            f32x4 vf[kTT][2];
+            f32x4 vf[kTT][G::kPairs];
+            auto read_v = [&] {
 #pragma unroll
-            for (int s = 0; s < kTT; ++s)
+                for (int s = 0; s < kTT; ++s)
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                    for (int p = 0; p < G::kPairs; ++p)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        vf[s][p][x] = fv[(16 * s + 4 * g + x) * G::kStride + 32 * wave + 16 * p + l];
+                        for (int x = 0; x < 4; ++x)
+                            vf[s][p][x] =
+                                fv[(16 * s + 4 * g + x) * G::kStride + N * wave + 16 * p + l];
+            };
             if constexpr (OUT) {
-                f32x4 O[kTT][2], P[kTT][kTT];
+                f32x4 O[kTT][G::kPairs], P[kTT][kTT];
 #pragma unroll
                 for (int t = 0; t < kTT; ++t) {
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) O[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int p = 0; p < G::kPairs; ++p) O[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int s = 0; s <= t; ++s) P[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
                 }
 #pragma unroll
-                for (int a = 0; a < State<T, D>::kTiles; ++a) {
-                    if (16 * a >= dk) break;  // nothing but padding from here
+                for (int a = 0; a < State<T, D, N>::kTiles; ++a) {
+                    if (a % G::kStep == 0 && 16 * a >= dk) break;  // nothing but padding from here
                     f32x4 qf[kTT], kf[kTT];
 #pragma unroll
                     for (int t = 0; t < kTT; ++t) {
@@ -753,10 +768,11 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                             for (int s = 0; s <= t; ++s)
                                 P[t][s] = mfma(kf[s][x], qf[t][x], P[t][s]);
 #pragma unroll
-                            for (int p = 0; p < 2; ++p)
+                            for (int p = 0; p < G::kPairs; ++p)
                                 O[t][p] = mfma(S.s[a][p][x], qf[t][x], O[t][p]);
                         }
                 }
+                read_v();
                 float near[4], far[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -766,7 +782,7 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
 #pragma unroll
                 for (int t = 0; t < kTT; ++t) {
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) O[t][p] *= row * tile[t];
+                    for (int p = 0; p < G::kPairs; ++p) O[t][p] *= row * tile[t];
 #pragma unroll
                     for (int s = 0; s <= t; ++s)
 #pragma unroll
@@ -775,33 +791,43 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
                             if (s == t) e = l - 4 * g - x >= 0 ? e * near[x] : 0.f;
                             else e *= far[x];
 #pragma unroll
-                            for (int p = 0; p < 2; ++p) O[t][p] = mfma(vf[s][p][x], e, O[t][p]);
+                            for (int p = 0; p < G::kPairs; ++p)
+                                O[t][p] = mfma(vf[s][p][x], e, O[t][p]);
                         }
                     if (16 * t + l < count)
 #pragma unroll
-                        for (int p = 0; p < 2; ++p)
+                        for (int p = 0; p < G::kPairs; ++p)
                             if (ocol + 16 * p < dv)
                                 *reinterpret_cast<f32x4 *>(out + 16 * t * obytes + 64 * p) =
                                     O[t][p];
                 }
             }
+            if (!OUT) read_v();
             if (OUT && left <= 0 && !keep) break;
             S.scale(gc);
 #pragma unroll
             for (int s = 0; s < kTT; ++s)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int row = 16 * s + 4 * g + x;
-                    const float w = weight[row + C - count];
+                    const float w = weight[16 * s + 4 * g + x + C - count];
 #pragma unroll
-                    for (int a = 0; a < State<T, D>::kTiles; ++a) {
-                        if (16 * a >= dk) break;
-                        const float kt = fk[row * G::kStride + 16 * a + l];
-#pragma unroll
-                        for (int p = 0; p < 2; ++p)
-                            S.s[a][p] = mfma(kt, vf[s][p][x] * w, S.s[a][p]);
-                    }
+                    for (int p = 0; p < G::kPairs; ++p) vf[s][p][x] *= w;
                 }
+#pragma unroll
+            for (int a0 = 0; a0 < State<T, D, N>::kTiles; a0 += G::kStep) {
+                if (16 * a0 >= dk) break;
+#pragma unroll
+                for (int s = 0; s < kTT; ++s)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int a = a0; a < a0 + G::kStep; ++a) {
+                            const float kt = fk[(16 * s + 4 * g + x) * G::kStride + 16 * a + l];
+#pragma unroll
+                            for (int p = 0; p < G::kPairs; ++p)
+                                S.s[a][p] = mfma(kt, vf[s][p][x], S.s[a][p]);
+                        }
+            }
         }
         n = next;
         out += count * obytes;
@@ -829,14 +855,15 @@ __global__ __launch_bounds__(2 * D, 2) void linattn_kernel(LaCall c) {
 // Segments' own states into the states they start from, in place: slot s + 1
 // holds segment s's own, slot 0 receives the initial one where it is read from
 // there.
-template <typename T, int D>
+template <typename T, int D, int N>
 __global__ __launch_bounds__(256) void segment_states_kernel(LaCall c) {
-    typedef State<T, D> St;
+    typedef State<T, D, N> St;
     const LaRole &r = c.role[blockIdx.z];
     // four rows of a column per thread, in the slots' order
     const int bh = blockIdx.y, e = blockIdx.x * 256 + threadIdx.x;
-    const int tile = e >> 6, lane = e & 63, p = tile & 1, a = (tile >> 1) % St::kTiles;
-    const int i = St::row(a, lane), j = St::col(p, tile / 2 / St::kTiles, lane);
+    const int tile = e >> 6, lane = e & 63, p = tile % St::kPairs,
+              a = tile / St::kPairs % St::kTiles;
+    const int i = St::row(a, lane), j = St::col(p, tile / St::kPairs / St::kTiles, lane);
     const int len = c.lens ? min(max(c.lens[bh / c.H], 0), c.T) : c.T;
     const float g = c.decay[bh % c.H], full = decay_power(g, c.seg_len);
     const int64_t slot_seg = (int64_t)c.B * c.H * (St::kSlot / 4);
@@ -974,7 +1001,7 @@ void set_divisors(LaCall &c) {
     c.by_heads = 1.0 / c.H;
 }
 
-template <typename T, int D>
+template <typename T, int D, int N>
 hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
     LaCall out = c;
     set_divisors(out);
@@ -986,7 +1013,8 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
             if (!c.role[i].slot_trans) own.role[own.roles++] = c.role[i];
         own.segs = c.segs - 1;
         set_divisors(own);
-        linattn_kernel<T, D, false><<<own.roles * c.B * c.H * own.segs, 2 * D, 0, s>>>(own);
+        linattn_kernel<T, D, N, false>
+            <<<own.roles * c.B * c.H * own.segs, Geo<T, D, N>::kThreads, 0, s>>>(own);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         // a final state written over the initial one must not reach the first
@@ -998,13 +1026,14 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
             LaCall sum = out;
             sum.roles = own.roles;
             for (int i = 0; i < own.roles; ++i) sum.role[i] = own.role[i];
-            segment_states_kernel<T, D>
+            segment_states_kernel<T, D, N>
                 <<<dim3(D * D / 1024, c.B * c.H, own.roles), 256, 0, s>>>(sum);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
     }
-    linattn_kernel<T, D, true><<<c.roles * c.B * c.H * c.segs, 2 * D, 0, s>>>(out);
+    linattn_kernel<T, D, N, true>
+        <<<c.roles * c.B * c.H * c.segs, Geo<T, D, N>::kThreads, 0, s>>>(out);
     return hipGetLastError();
 }
 
@@ -1019,12 +1048,15 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
 // While each has a compute unit to itself, shorter ones too: a chunk of 32 tokens in
 // fp32 (30 heads of 128 there and back, 101 tokens: 63 us, uncut 74; 8 heads, 1000
 // tokens: 107, in seven 169), 64 tokens in 16 bits from three on (the same in bf16,
-// 1000 tokens: 62 against 67; 128 tokens in two 35, uncut 30).
+// 1000 tokens: 62 against 67; 128 tokens in two 35, uncut 30).  And where a second
+// segment would put two fp32 workgroups of 128 on a compute unit, none is cut (192
+// heads, 512 tokens: 147 us, in two 156).
 LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype) {
     const int64_t slots = (width > 64 ? 2 : 4) * kPlanCus;
     const int64_t units = std::max<int64_t>(heads * roles, 1);
     const int least = dtype == SNN_F32 ? 32 : 64, most = (T - 1) / least + 1;
     int64_t segs = std::min<int64_t>(slots / units, T / 128);
+    if (dtype == SNN_F32 && width > 64 && 2 * units > kPlanCus && units <= kPlanCus) segs = 1;
     if (dtype == SNN_F32 || most > 2)
         segs = std::max(segs, std::min<int64_t>(kPlanCus / units, most));
     LaPlan p;
@@ -1045,10 +1077,17 @@ LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype) {
 hipError_t launch_linattn(const LaCall &c, int dtype, hipStream_t s) {
     const bool wide = std::max(c.role[0].dk, c.role[0].dv) > 64;
     switch (dtype) {
-        case SNN_F32: return wide ? launch_chunks<float, 128>(c, s) : launch_chunks<float, 64>(c, s);
+        case SNN_F32:
+            if (!wide) return launch_chunks<float, 64, 16>(c, s);
+            return (int64_t)c.roles * c.B * c.H * c.segs <= kPlanCus
+                       ? launch_chunks<float, 128, 16>(c, s)
+                       : launch_chunks<float, 128, 32>(c, s);
         case SNN_F16:
-            return wide ? launch_chunks<half_t, 128>(c, s) : launch_chunks<half_t, 64>(c, s);
-        default: return wide ? launch_chunks<bf16_t, 128>(c, s) : launch_chunks<bf16_t, 64>(c, s);
+            return wide ? launch_chunks<half_t, 128, 32>(c, s)
+                        : launch_chunks<half_t, 64, 32>(c, s);
+        default:
+            return wide ? launch_chunks<bf16_t, 128, 32>(c, s)
+                        : launch_chunks<bf16_t, 64, 32>(c, s);
     }
 }
 

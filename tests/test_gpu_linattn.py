@@ -277,8 +277,8 @@ def test_state_carries_over_calls_and_in_place(dt):
 @pytest.mark.parametrize("dt", list(TYPES))
 @pytest.mark.parametrize("T,d", [(300, 64), (700, 64), (1500, 128)])
 def test_state_in_place_over_many_segments(T, d, dt):
-    """One head: the tokens are cut (2, 5 and 11 times), with the state given, in
-    place, apart and absent."""
+    """One head: the tokens are cut into segments, with the state given, in place,
+    apart and absent."""
     c = Case(T, 1, 1, 1, d, d, dt, lens=[T - 70])
     o, s = (x.clone() for x in c.fwd())
     c.check_fwd()
@@ -289,6 +289,17 @@ def test_state_in_place_over_many_segments(T, d, dt):
     z = Case(T, 1, 1, 1, d, d, dt, state=False)
     z.check_fwd()
     z.check_bwd()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,B,H,KV,dk,dv", [(20, 65, 4, 2, 128, 72), (640, 33, 2, 1, 72, 40),
+                                            (1152, 15, 2, 2, 72, 72), (1152, 5, 2, 1, 40, 72),
+                                            (40, 150, 7, 7, 16, 24)])
+def test_more_workgroups_than_compute_units(T, B, H, KV, dk, dv, dt):
+    """Many heads, uncut and in segments of a few hundred tokens."""
+    c = Case(T, B, H, KV, dk, dv, dt, lens=[T - (b % 3) * T // 2 for b in range(B)])
+    c.check_fwd()
+    c.check_bwd()
 
 
 def test_no_tokens_and_no_sequences():
