@@ -6,17 +6,18 @@
 // state R^T; dv: time reversed, q' = k, k' = q, v' = do, state R), so one
 // kernel computes forward and backward; a launch runs up to kLaRoles of them.
 //
-// Whole sequences go in chunks of C tokens (64 or 32) with the state between them,
+// Whole sequences go in chunks of C = 32 tokens with the state between them,
 // all of it on the matrix cores:
 //   o_i = rs (sum_{j<=i} g^{i-j} ws (q_i.k_j) v_j + g^{i+first} q_i X)
 //   X'  = g^C X + sum_j g^{C-first-j} ws k_j^T v_j
-// A wave owns 32 columns of v (fp32 often 16) and the state's columns with them, in
-// registers, so waves exchange nothing but the staged tiles of q, k and v; each
-// computes the chunk's scores q.k for itself (in 16 bits 12 % of its matrix
-// instructions at d = 128, 18 % at 64; in fp32 of 64 39 %).  Every product is arranged so that a result lies in the registers
-// as the next product's operand: scores and output are taken transposed (s x t,
-// dv x t), and the 16 rows of a result tile are the k values 4 g + r that lane
-// group g holds of an operand, in whatever order, as long as both operands agree.
+// A wave owns 16 or 32 columns of v and the state's columns with them, in registers,
+// so waves exchange nothing but the staged tiles of q, k and v; each computes the
+// chunk's scores q.k for itself (12 % of its matrix instructions at d = 128 with 32
+// columns, 20 % at 64; in fp32 25 and 39 %).  Every product is arranged so that a
+// result lies in the registers as the next product's operand: scores and output are
+// taken transposed (s x t, dv x t), and the 16 rows of a result tile are the k values
+// 4 g + r that lane group g holds of an operand, in whatever order, as long as both
+// operands agree.
 //
 // 16-bit operands multiply exactly into fp32.  What is fp32 and becomes an
 // operand is split: scores and state into two 16-bit parts (2^-16 of a term,
@@ -171,20 +172,22 @@ __device__ inline void unpack(const u32x4 &p, float (&x)[8]) {
 // D: head sizes up to 64 or 128, padded with zeros.  N: columns of a wave, one tile
 // or a pair, so D / N waves make a workgroup.
 //
-// 16-bit types take 32: what a wave does for the scores, it does for more columns.
-// fp32 takes 16 at d = 64, where the registers then hold four waves of a SIMD instead
-// of two (512 tokens of 256 heads there and back 195 us against 213, of 64 heads 73
-// against 93).  At 128 they do not: 16 while each workgroup has a compute unit to
-// itself (101 tokens of 30 heads there and back 55 us against 61), else 32 (512 tokens
-// of 256 heads 512 us against 596).
+// Of 64, a wave takes 16: the registers then hold four waves of a SIMD, with chunks of
+// 32 tokens, instead of two with 32 columns and chunks of 64 (2000 tokens of 128 heads
+// there and back: bf16 145 us against 169, fp16 172 against 175; 512 tokens of 256
+// fp32 heads 195 against 213).  Of 128 they do not: 16 while each workgroup has a
+// compute unit to itself (101 tokens of 8 heads there and back: bf16 27 us against 30;
+// of 30 fp32 heads 55 against 61), else 32, which compute the scores half as often
+// (2000 tokens of 128 bf16 heads 316 against 344, 512 of 256 fp32 heads 512 against
+// 596).
 template <typename T, int D, int N>
 struct Geo {
     static constexpr bool kHalf = sizeof(T) == 2;
-    // Tokens of a chunk: 64 where the registers hold that, else 32 (at d = 128 64 spill,
-    // and 512 x 16 tokens and heads took 174 us against 142).
-    static constexpr int C = kHalf && D == 64 ? 64 : 32;
+    // Tokens of a chunk (64 spill at d = 128: 512 x 16 tokens and heads took 174 us
+    // against 142).
+    static constexpr int C = 32;
     static constexpr int kPairs = N / 16, kWaves = D / N, kThreads = 64 * kWaves;
-    static constexpr int kEu = kHalf || D > 64 ? 2 : 4;  // waves of a SIMD at least
+    static constexpr int kEu = D > 64 ? 2 : 4;  // waves of a SIMD at least
     // fp32: tiles of the head that a product takes together, for independent sums (at
     // 128 others run meanwhile, and one leaves less padding)
     static constexpr int kStep = D > 64 ? 1 : 2;
@@ -192,7 +195,6 @@ struct Geo {
     static constexpr int kRuns = D / kRun;            // runs of a row
     static constexpr int kRows = kThreads / kRuns;    // rows that the threads stage at once
     static constexpr int kVec = C / kRows;            // runs a thread stages
-    static_assert(kHalf || C == 32);  // fp32 scores: two tiles of tokens
     // 16-bit rows: run c of row r lies at slot c ^ swz(r), so that the 16 rows that
     // a fragment's lanes read at one run, and the 4 rows by 4 runs of a transposing
     // read, fall on distinct banks.  fp32 rows: 4 values of padding, which spread
@@ -271,19 +273,19 @@ __device__ inline bool not_finite(const u32x4 (&v)[N]) {
     return (bad & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u)) != 0;
 }
 
-// 8 values of column `col` (of 16 lanes' columns each) in rows 32 u + 4 g .. + 3
-// and 32 u + 16 + 4 g .. + 3 of a row-major tile: within 16 lanes, the
-// transposing read hands lane i element e of lane 4 e + i / 4's 4-value run
-// (position i % 4), so lane L points at row 4 g + L / 4 and the run of lanes
-// 4 (L % 4) .. + 3.  Pair p of 16 columns holds columns 8 (i / 4) + 4 p + i % 4
-// of 32: a lane's results of both pairs are 8 neighbours in memory.
+// 8 values of one column of column tile c, rows 4 g .. + 3 and 16 + 4 g .. + 3 of a
+// row-major tile: within 16 lanes, the transposing read hands lane i element e of
+// lane 4 e + i / 4's 4-value run (position i % 4), so lane L points at row 4 g + L / 4
+// and the run of lanes 4 (L % 4) .. + 3.  Of 32 columns the even tile holds
+// 8 (i / 4) + i % 4, the odd one those + 4: a lane's results of both are 8 neighbours
+// in memory.
 template <typename T, int D>
-__device__ inline u32x4 read_columns(const T *tile, int u, int block, int p) {
+__device__ inline u32x4 read_columns(const T *tile, int c) {
     typedef Geo<T, D, 32> G;
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int lane = threadIdx.x & 63, g = lane >> 4, L = lane & 15;
-    const int row = 32 * u + 4 * g + (L >> 2);
-    const T *a = tile + G::at(row, 4 * block + (L & 3)) + 4 * p;
+    const int row = 4 * g + (L >> 2);
+    const T *a = tile + G::at(row, 4 * (c >> 1) + (L & 3)) + 4 * (c & 1);
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)a);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(a + 16 * G::kStride));
     const u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
@@ -301,8 +303,8 @@ struct State {
         return sizeof(T) == 2 ? 32 * (a >> 1) + 8 * g + 4 * (a & 1) : 16 * a + 4 * g;
     }
     __device__ static inline int col(int p, int w, int lane) {
-        const int i = lane & 15;
-        return N * w + (sizeof(T) == 2 ? 8 * (i >> 2) + 4 * p + (i & 3) : 16 * p + i);
+        const int i = lane & 15, c = kPairs * w + p;
+        return sizeof(T) == 2 ? 32 * (c >> 1) + 8 * (i >> 2) + 4 * (c & 1) + (i & 3) : 16 * c + i;
     }
     __device__ static inline int row(int a) { return row(a, threadIdx.x & 63); }
     __device__ static inline int col(int p) { return col(p, threadIdx.x >> 6, threadIdx.x & 63); }
@@ -428,7 +430,8 @@ template <typename T, int D, int N, bool OUT>
 __global__ __launch_bounds__((Geo<T, D, N>::kThreads), (Geo<T, D, N>::kEu))
 void linattn_kernel(LaCall c) {
     typedef Geo<T, D, N> G;
-    constexpr int C = G::C, kTT = C / 16, kU = C / 32;  // tiles of 16 tokens
+    constexpr int C = G::C, kTT = C / 16;  // tiles of 16 tokens
+    static_assert(kTT == 2);
     constexpr bool kHalf = G::kHalf, kNorm = std::is_same_v<T, half_t>;
     __shared__ __attribute__((aligned(16))) T tq[OUT ? G::kTile : 8], tk[G::kTile], tv[G::kTile];
     __shared__ float pw[C + 1];       // decay^i
@@ -483,7 +486,8 @@ void linattn_kernel(LaCall c) {
     // this lane's token and columns of the output, and their step over tokens
     const int64_t ostep = r.reverse ? -r.ot : r.ot;
     const bool o_f32 = r.o_f32;
-    const int ocol = N * wave + (kHalf ? 8 : 4) * g;
+    const int tile0 = G::kPairs * wave;  // its first tile of 16 columns
+    const int ocol = kHalf ? 32 * (tile0 >> 1) + 4 * (tile0 & 1) + 8 * g : N * wave + 4 * g;
     char *out = static_cast<char *>(r.o) +
                 (b * r.ob + h * r.oh + (r.reverse ? (len - 1) * r.ot : 0) + (begin + l) * ostep +
                  ocol) * (int64_t)(o_f32 ? 4 : sizeof(T));
@@ -528,13 +532,13 @@ void linattn_kernel(LaCall c) {
         if constexpr (kNorm) largest = S.largest();
 
         if constexpr (kHalf) {
-            u32x4 vf[kU][2];
+            u32x4 vf[G::kPairs];
             if constexpr (OUT) {
-                f32x4 O[kTT][2], P[kTT][kTT];
+                f32x4 O[kTT][G::kPairs], P[kTT][kTT];
 #pragma unroll
                 for (int t = 0; t < kTT; ++t) {
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) O[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int p = 0; p < G::kPairs; ++p) O[t][p] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int s = 0; s <= t; ++s) P[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
                 }
@@ -555,7 +559,7 @@ void linattn_kernel(LaCall c) {
 #pragma unroll
                         for (int s = 0; s <= t; ++s) P[t][s] = mfma<T>(kf[s], qf[t], P[t][s]);
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
+                    for (int p = 0; p < G::kPairs; ++p) {
                         float x[8];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -571,9 +575,7 @@ void linattn_kernel(LaCall c) {
                     }
                 }
 #pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) vf[u][p] = read_columns<T, D>(tv, u, wave, p);
+                for (int p = 0; p < G::kPairs; ++p) vf[p] = read_columns<T, D>(tv, tile0 + p);
                 // scores: decayed, those of later tokens zero.  A tile's row is s = 4 g + x,
                 // its column t = l, of the same 16 tokens or the 16 before
                 float near[4], far[4];
@@ -591,8 +593,7 @@ void linattn_kernel(LaCall c) {
                         for (int x = 0; x < 4; ++x) {
                             float e = P[t][s][x];
                             if (s == t) e = l - 4 * g - x >= 0 ? e * near[x] : 0.f;
-                            else if (s + 1 == t) e *= far[x];
-                            else e *= far[x] * tile[t - s - 1];
+                            else e *= far[x];
                             P[t][s][x] = e;
                         }
                         if constexpr (kNorm) {
@@ -623,71 +624,71 @@ void linattn_kernel(LaCall c) {
                     float f = row * tile[t];
                     if constexpr (kNorm) f = __builtin_ldexpf(f, exp_p - exp_x - exp_s);
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) O[t][p] *= f;
+                    for (int p = 0; p < G::kPairs; ++p) O[t][p] *= f;
+                    float x[8];
 #pragma unroll
-                    for (int u = 0; u <= t / 2; ++u) {
-                        float x[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int s = 2 * u + (j >> 2);
-                            x[j] = s <= t ? P[t][s <= t ? s : 0][j & 3] : 0.f;
-                            if constexpr (kNorm) x[j] *= fp;
-                        }
-                        const u32x4 hi = take_part<T>(x), lo = pack<T>(x);
-#pragma unroll
-                        for (int p = 0; p < 2; ++p) {
-                            O[t][p] = mfma<T>(vf[u][p], lo, O[t][p]);
-                            O[t][p] = mfma<T>(vf[u][p], hi, O[t][p]);
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        const int s = j >> 2;
+                        x[j] = s <= t ? P[t][s <= t ? s : 0][j & 3] : 0.f;
+                        if constexpr (kNorm) x[j] *= fp;
                     }
-                    // token 16 t + l, columns 8 g .. 8 g + 7 of the wave's 32
+                    const u32x4 hi = take_part<T>(x), lo = pack<T>(x);
+#pragma unroll
+                    for (int p = 0; p < G::kPairs; ++p) {
+                        O[t][p] = mfma<T>(vf[p], lo, O[t][p]);
+                        O[t][p] = mfma<T>(vf[p], hi, O[t][p]);
+                    }
+                    // token 16 t + l, columns 8 g .. 8 g + 7 of 32 or four of them
                     if (16 * t + l < count && ocol < dv) {
                         char *to = out + 16 * t * obytes;
-                        if constexpr (kNorm) O[t][0] *= back, O[t][1] *= back;
+                        if constexpr (kNorm)
+#pragma unroll
+                            for (int p = 0; p < G::kPairs; ++p) O[t][p] *= back;
                         if (o_f32) {
-                            reinterpret_cast<f32x4 *>(to)[0] = O[t][0];
-                            reinterpret_cast<f32x4 *>(to)[1] = O[t][1];
+#pragma unroll
+                            for (int p = 0; p < G::kPairs; ++p)
+                                reinterpret_cast<f32x4 *>(to)[p] = O[t][p];
                         } else {
-                            const float x[8] = {O[t][0][0], O[t][0][1], O[t][0][2], O[t][0][3],
-                                                O[t][1][0], O[t][1][1], O[t][1][2], O[t][1][3]};
-                            *reinterpret_cast<u32x4 *>(to) = pack<T>(x);
+                            u32x2 half[G::kPairs];
+#pragma unroll
+                            for (int p = 0; p < G::kPairs; ++p)
+                                half[p] = u32x2{pack2<T>(O[t][p][0], O[t][p][1]),
+                                                pack2<T>(O[t][p][2], O[t][p][3])};
+                            if constexpr (G::kPairs == 2)
+                                *reinterpret_cast<u32x4 *>(to) =
+                                    u32x4{half[0][0], half[0][1], half[1][0], half[1][1]};
+                            else *reinterpret_cast<u32x2 *>(to) = half[0];
                         }
                     }
                 }
             } else {
 #pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) vf[u][p] = read_columns<T, D>(tv, u, wave, p);
+                for (int p = 0; p < G::kPairs; ++p) vf[p] = read_columns<T, D>(tv, tile0 + p);
             }
             if (OUT && left <= 0 && !keep) break;
             // the state's update
             const float *wt = weight + (C - count) + 4 * g;
-            auto weighted = [&](int u, int p, float (&x)[8]) {
-                unpack<T>(vf[u][p], x);
+            auto weighted = [&](int p, float (&x)[8]) {
+                unpack<T>(vf[p], x);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] *= wt[32 * u + 16 * (j >> 2) + (j & 3)];
+                for (int j = 0; j < 8; ++j) x[j] *= wt[16 * (j >> 2) + (j & 3)];
             };
-            float w[kNorm ? kU : 1][2][8];
+            float w[G::kPairs][8];
             if constexpr (kNorm) {
                 float m[2] = {};
 #pragma unroll
-                for (int u = 0; u < kU; ++u)
+                for (int p = 0; p < G::kPairs; ++p) {
+                    weighted(p, w[p]);
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        weighted(u, p, w[u][p]);
-#pragma unroll
-                        for (int j = 0; j < 8; j += 2) grow(m[p], w[u][p][j], w[u][p][j + 1]);
-                    }
+                    for (int j = 0; j < 8; j += 2) grow(m[p], w[p][j], w[p][j + 1]);
+                }
                 float most = wave_max(fmaxf(m[0], m[1]));
                 if (!(most < __builtin_inff())) {
                     most = 0.f;
 #pragma unroll
-                    for (int u = 0; u < kU; ++u)
+                    for (int p = 0; p < G::kPairs; ++p)
 #pragma unroll
-                        for (int p = 0; p < 2; ++p)
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) grow_finite(most, w[u][p][j]);
+                        for (int j = 0; j < 8; ++j) grow_finite(most, w[p][j]);
                     most = wave_max(most);
                 }
                 // the scale of this chunk's v g^j, unless the state would leave 2^61
@@ -702,29 +703,27 @@ void linattn_kernel(LaCall c) {
             }
             constexpr int kParts = kNorm ? 2 : 3;
             const float fv = pow2(exp_s);
+            u32x4 part[G::kPairs][kParts];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                u32x4 part[2][kParts];
+            for (int p = 0; p < G::kPairs; ++p) {
+                float x[8];
+                if constexpr (kNorm) {
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    float x[8];
-                    if constexpr (kNorm) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = w[u][p][j] * fv;
-                    } else {
-                        weighted(u, p, x);
-                    }
-#pragma unroll
-                    for (int m = 0; m < kParts; ++m) part[p][m] = take_part<T>(x);
+                    for (int j = 0; j < 8; ++j) x[j] = w[p][j] * fv;
+                } else {
+                    weighted(p, x);
                 }
 #pragma unroll
-                for (int a = 0; a < State<T, D, N>::kTiles; ++a) {
-                    const u32x4 kt = read_columns<T, D>(tk, u, a >> 1, a & 1);
+                for (int m = 0; m < kParts; ++m) part[p][m] = take_part<T>(x);
+            }
 #pragma unroll
-                    for (int m = kParts - 1; m >= 0; --m)
+            for (int a = 0; a < State<T, D, N>::kTiles; ++a) {
+                const u32x4 kt = read_columns<T, D>(tk, a);
 #pragma unroll
-                        for (int p = 0; p < 2; ++p) S.s[a][p] = mfma<T>(kt, part[p][m], S.s[a][p]);
-                }
+                for (int m = kParts - 1; m >= 0; --m)
+#pragma unroll
+                    for (int p = 0; p < G::kPairs; ++p)
+                        S.s[a][p] = mfma<T>(kt, part[p][m], S.s[a][p]);
             }
         } else if (N * wave < dv) {
             const float *fq = reinterpret_cast<const float *>(tq),
@@ -1074,20 +1073,18 @@ LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype) {
     return p;
 }
 
+template <typename T>
+static hipError_t launch_width(const LaCall &c, hipStream_t s) {
+    if (std::max(c.role[0].dk, c.role[0].dv) <= 64) return launch_chunks<T, 64, 16>(c, s);
+    return (int64_t)c.roles * c.B * c.H * c.segs <= kPlanCus ? launch_chunks<T, 128, 16>(c, s)
+                                                             : launch_chunks<T, 128, 32>(c, s);
+}
+
 hipError_t launch_linattn(const LaCall &c, int dtype, hipStream_t s) {
-    const bool wide = std::max(c.role[0].dk, c.role[0].dv) > 64;
     switch (dtype) {
-        case SNN_F32:
-            if (!wide) return launch_chunks<float, 64, 16>(c, s);
-            return (int64_t)c.roles * c.B * c.H * c.segs <= kPlanCus
-                       ? launch_chunks<float, 128, 16>(c, s)
-                       : launch_chunks<float, 128, 32>(c, s);
-        case SNN_F16:
-            return wide ? launch_chunks<half_t, 128, 32>(c, s)
-                        : launch_chunks<half_t, 64, 32>(c, s);
-        default:
-            return wide ? launch_chunks<bf16_t, 128, 32>(c, s)
-                        : launch_chunks<bf16_t, 64, 32>(c, s);
+        case SNN_F32: return launch_width<float>(c, s);
+        case SNN_F16: return launch_width<half_t>(c, s);
+        default: return launch_width<bf16_t>(c, s);
     }
 }
 
