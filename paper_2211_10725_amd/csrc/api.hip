@@ -1099,11 +1099,10 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
     (void)hipGetLastError();
     hipError_t e = launch_linattn(c, d->dtype, stream);
     if (e == hipSuccess && share > 1 && d->T > 0)
-        e = launch_group_sum(pk, grad_k, d->k_stride, d->T, d->B, d->kv_heads, share, d->d_k,
-                             d->dtype, stream);
-    if (e == hipSuccess && share > 1 && d->T > 0)
-        e = launch_group_sum(pv, grad_v, d->v_stride, d->T, d->B, d->kv_heads, share, d->d_v,
-                             d->dtype, stream);
+        e = launch_group_sum(
+            {pk, grad_k, d->k_stride[0], d->k_stride[1], d->k_stride[2], d->d_k},
+            {pv, grad_v, d->v_stride[0], d->v_stride[1], d->v_stride[2], d->d_v}, d->T, d->B,
+            d->kv_heads, share, d->dtype, stream);
     return hip_status(e);
 }
 

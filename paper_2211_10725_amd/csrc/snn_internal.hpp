@@ -348,8 +348,14 @@ LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype);
 hipError_t launch_linattn(const LaCall &c, int dtype, hipStream_t s);
 // dst (strided [T, B, KV, d] of dtype) = src fp32 [T, B, KV * share, d] summed
 // over each group of `share` heads
-hipError_t launch_group_sum(const float *src, void *dst, const int64_t *stride, int T, int B,
-                            int KV, int share, int d, int dtype, hipStream_t s);
+struct LaGroupSum {
+    const float *src;
+    void *dst;
+    int64_t st, sb, sh;
+    int d;
+};
+hipError_t launch_group_sum(const LaGroupSum &a, const LaGroupSum &b, int T, int B, int KV,
+                            int share, int dtype, hipStream_t s);
 struct LaStep {
     LaOperand q, k, v;
     int dk, dv, H, n_slots;
