@@ -37,13 +37,14 @@
 // segment's workgroup adds those before it itself), a last computes the outputs
 // from each segment's state.
 //
-// Measured: 32768 tokens of 16 heads of 128 (bf16) 223 us in 73 + 14 + 141 (own
-// states, their sums, outputs), 2.4 TB/s of the least traffic; the outputs' kernel
-// moves 4 TB/s.  Counters there: vector instructions issue in 67 % of its time,
-// the matrix cores are busy in 42 %, waves wait in 25 %.  Of the vector
-// instructions half decay and split the state, a quarter split v g^j.  fp32 is
-// bound by the fp32 matrix instructions: 512 tokens of 256 heads of 64, forward
-// and backward, 195 us, of which they take more than half.
+// Measured: 32768 tokens of 16 heads of 128 (bf16) 221 us, traced as 71 + 14 + 141
+// (own states, their sums, outputs), 2.4 TB/s of the least traffic; the outputs'
+// kernel moves 4 TB/s.  Counters there: the matrix cores are busy in 51 % of its
+// time, vector instructions take 31 %, and the two waves of a SIMD wait for memory
+// or LDS in 29 % of theirs.  fp32 is bound by the fp32 matrix instructions: 512
+// tokens of 256 heads of 64, forward and backward, 193 us; they take 63 % of the
+// forward's outputs and 74 % of the backward.  fp16 of 64 (8 x 1000 tokens of 16
+// heads, 34 us) is bound by the vector unit: 59 %, matrix cores 14 %.
 #include <type_traits>
 
 #include "snn_internal.hpp"
