@@ -61,8 +61,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Up to this many segments each adds the states of those before it by itself
 // rather than in a launch between (2000 tokens in 8 segments, 64 bf16 heads of 128:
-// 62 against 71 us, 128 fp16 heads of 64: 60 against 64; in 16 segments, 64 bf16
-// heads of 64, it would be the slower, 45 against 44).
+// 69 against 74 us, 128 fp16 heads of 64: 57 against 61).  Beyond that a prompt still
+// gains (in 16, 64 bf16 heads of 64: 34 against 37) and training loses (12 heads of
+// 128, 4096 tokens: 130 against 115).
 constexpr int kSumHere = 8;
 
 // decay^e, e >= 0, by repeated squaring in fp64 (0^0 = 1)
@@ -1050,9 +1051,9 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
 // 128 slots left 282).  Fp32 of 256 heads of 64 (512 tokens): the forward in 4
 // segments 70 us, in 3 85.
 // While each has a compute unit to itself, shorter ones too: a chunk of 32 tokens in
-// fp32 (30 heads of 128 there and back, 101 tokens: 63 us, uncut 74; 8 heads, 1000
-// tokens: 107, in seven 169), 64 tokens in 16 bits from three on (the same in bf16,
-// 1000 tokens: 62 against 67; 128 tokens in two 35, uncut 30).  And where a second
+// fp32 (30 heads of 128 there and back, 101 tokens: 53 us, uncut 74; 8 heads, 1000
+// tokens: 98, in seven 135), 64 tokens in 16 bits from three on (the same in bf16,
+// 1000 tokens: 58 against 59; 30 heads, 128 tokens in two 31, uncut 26).  And where a second
 // segment would put two fp32 workgroups of 128 on a compute unit, none is cut (192
 // heads, 512 tokens: 147 us, in two 156).
 LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype) {
