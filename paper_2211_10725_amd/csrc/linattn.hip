@@ -24,8 +24,9 @@
 // far under the result's own rounding; one part would raise a bf16 result's
 // error by up to 1.4), v g^j in the state's update into as many as keep fp32's
 // precision (three bf16, two fp16).  fp16 parts are taken after a scaling by a
-// power of two that puts the wave's largest value near 2^14, so neither large
-// sums nor small ones leave the type's range.  fp32 operands go through the fp32
+// power of two that puts the largest value near 2^14, so neither large sums nor
+// small ones leave the type's range: the largest of a token's scores, and of the
+// wave's part of the state and of v g^j.  fp32 operands go through the fp32
 // matrix instructions as they are.
 //
 // A masked score is replaced by zero, but a zero times a later token's infinite
@@ -95,6 +96,15 @@ __device__ inline float wave_max(float x) {
     SNN_DPP_MAX(0x143);
 #undef SNN_DPP_MAX
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+// largest over lanes l, l + 16, l + 32 and l + 48 of values >= 0: those that hold one
+// token of the scores, or one column of the state
+__device__ inline float column_max(float x) {
+    const uint32_t a = __float_as_uint(x);
+    const auto b = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1])));
+    const auto c = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return fmaxf(__uint_as_float(c[0]), __uint_as_float(c[1]));
 }
 // m = max(m, |a|, |b|), NaN ignored: one instruction, where fmaxf would first quiet
 // each operand
@@ -591,7 +601,7 @@ void linattn_kernel(LaCall c) {
                     near[x] = score[16 + l - 4 * g - x];
                     far[x] = score[32 + l - 4 * g - x];
                 }
-                float most[2] = {};
+                float most[kTT][2] = {};
 #pragma unroll
                 for (int t = 0; t < kTT; ++t)
 #pragma unroll
@@ -604,36 +614,45 @@ void linattn_kernel(LaCall c) {
                             P[t][s][x] = e;
                         }
                         if constexpr (kNorm) {
-                            grow(most[0], P[t][s][0], P[t][s][1]);
-                            grow(most[1], P[t][s][2], P[t][s][3]);
+                            grow(most[t][0], P[t][s][0], P[t][s][1]);
+                            grow(most[t][1], P[t][s][2], P[t][s][3]);
                         }
                     }
-                int exp_p = 0;
-                // at most 60: what smaller scores lose is far below an fp16 output's least
-                // step
+                // a token's scores have a scale of their own: another token, a later one
+                // least of all, must not take its digits.  At most 2^60: what smaller scores
+                // lose is far below an fp16 output's least step
+                int exp_p[kTT] = {};
                 if constexpr (kNorm) {
-                    float m = wave_max(fmaxf(most[0], most[1]));
-                    if (!(m < __builtin_inff())) {  // of an infinite q or k: the finite ones'
-                        m = 0.f;
+                    float m[kTT];
 #pragma unroll
-                        for (int t = 0; t < kTT; ++t)
+                    for (int t = 0; t < kTT; ++t)
+                        m[t] = column_max(fmaxf(most[t][0], most[t][1]));
+                    if (__any(!(fmaxf(m[0], m[1]) < __builtin_inff()))) {
+                        // of an infinite q or k: the finite ones'
+#pragma unroll
+                        for (int t = 0; t < kTT; ++t) {
+                            m[t] = 0.f;
 #pragma unroll
                             for (int s = 0; s <= t; ++s)
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) grow_finite(m, P[t][s][x]);
-                        m = wave_max(m);
+                                for (int x = 0; x < 4; ++x) grow_finite(m[t], P[t][s][x]);
+                            m[t] = column_max(m[t]);
+                        }
                     }
-                    exp_p = min(60, scale_to_half(m));
+#pragma unroll
+                    for (int t = 0; t < kTT; ++t) exp_p[t] = min(60, scale_to_half(m[t]));
                 }
-                const float fp = pow2(exp_p), back = pow2(-exp_p);
 #pragma unroll
                 for (int t = 0; t < kTT; ++t) {
                     float f = row * tile[t];
-                    if constexpr (kNorm) f = __builtin_ldexpf(f, exp_p - exp_x - exp_s);
+                    if constexpr (kNorm) f = __builtin_ldexpf(f, exp_p[t] - exp_x - exp_s);
 #pragma unroll
                     for (int p = 0; p < G::kPairs; ++p) O[t][p] *= f;
                     f32x4 x = P[t][0], y = t ? P[t][t] : f32x4{0.f, 0.f, 0.f, 0.f};
-                    if constexpr (kNorm) x *= fp, y *= fp;
+                    if constexpr (kNorm) {
+                        const float fp = pow2(exp_p[t]);
+                        x *= fp, y *= fp;
+                    }
                     const u32x4 hi = take_part<T>(x, y, minus), lo = pack<T>(x, y);
 #pragma unroll
                     for (int p = 0; p < G::kPairs; ++p) {
@@ -645,7 +664,7 @@ void linattn_kernel(LaCall c) {
                         char *to = out + 16 * t * obytes;
                         if constexpr (kNorm)
 #pragma unroll
-                            for (int p = 0; p < G::kPairs; ++p) O[t][p] *= back;
+                            for (int p = 0; p < G::kPairs; ++p) O[t][p] *= pow2(-exp_p[t]);
                         if (o_f32) {
 #pragma unroll
                             for (int p = 0; p < G::kPairs; ++p)

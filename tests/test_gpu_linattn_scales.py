@@ -1,0 +1,62 @@
+"""Linear attention of tokens and columns whose sizes differ by many powers of
+two, within the bounds of ``test_gpu_linattn``: what a score, the state or a
+value loses as a 16-bit operand is relative to its own token or column, not to
+others'."""
+import numpy as np
+import pytest
+
+from tests import block_reference as ref
+from tests.test_gpu_linattn import TYPES, Case, _np
+
+torch = pytest.importorskip("torch")
+import paper_2211_10725_amd as snn  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def _rescaled(c, scale):
+    c.scale = scale
+    c.d = snn.linattn_desc(c.q, c.k, c.v, c.o, scale)
+    return c
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("at", [5, 31, 75, 100])
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_later_token_leaves_earlier_outputs(d, at, dt):
+    """q = k = 6e4 of one token: the outputs before it stay as they are, bit for
+    bit, and within their bounds."""
+    c = Case(150, 1, 1, 1, d, d, dt, decay=[1.0])
+    before = c.fwd()[0].clone()
+    wo, _ = ref.linattn(*c.arrays())
+    ao, _ = ref.linattn(*c.arrays(np.abs))
+    c.q[at], c.k[at] = 6e4, 6e4
+    o, _ = c.fwd()
+    assert torch.equal(o[:at], before[:at])
+    c.tol(_np(o[:at]), wo[:at], ao[:at])
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_large_token_within_a_small_scale(dt):
+    """The same with a scale that keeps every output in fp16's range: all tokens."""
+    c = _rescaled(Case(150, 1, 1, 1, 64, 64, dt, decay=[0.9]), 2.0 ** -24)
+    c.q[40], c.k[40] = 6e4, 6e4
+    c.q[100, ..., 7] = -6e4
+    c.check_fwd()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("at", [33, 40, 60])
+def test_large_token_after_an_infinite_value(at, dt):
+    """A chunk whose tokens go one by one for an infinity in v: a later token's
+    size does not reach them either."""
+    c = _rescaled(Case(150, 1, 1, 1, 64, 64, dt, decay=[1.0], state=False), 2.0 ** 10)
+    c.q *= 2.0 ** -20
+    wo, _ = ref.linattn(*c.arrays())
+    ao, _ = ref.linattn(*c.arrays(np.abs))
+    c.v[at - 1, 0, 0, 9] = float("inf")
+    c.q[at], c.k[at] = 6e4, 6e4
+    keep = [i for i in range(64) if i != 9]
+    o, _ = c.fwd()
+    c.tol(_np(o[:at - 1]), wo[:at - 1], ao[:at - 1])
+    c.tol(_np(o[:at])[..., keep], wo[:at][..., keep], ao[:at][..., keep])
