@@ -25,8 +25,8 @@
 // error by up to 1.4), v g^j in the state's update into as many as keep fp32's
 // precision (three bf16, two fp16).  fp16 parts are taken after a scaling by a
 // power of two that puts the largest value near 2^14, so neither large sums nor
-// small ones leave the type's range: the largest of a token's scores, and of the
-// wave's part of the state and of v g^j.  fp32 operands go through the fp32
+// small ones leave the type's range: the largest of a token's scores, of a column of
+// the state, and of the wave's part of v g^j.  Two parts then end at 2^-39 of it.  fp32 operands go through the fp32
 // matrix instructions as they are.
 //
 // A masked score is replaced by zero, but a zero times a later token's infinite
@@ -416,26 +416,30 @@ struct State {
 #pragma unroll
             for (int p = 0; p < kPairs; ++p) s[a][p] *= f;
     }
-    // largest finite magnitude of the wave's part
-    __device__ inline float largest() const {
-        float m[4] = {};
+    // each column's largest finite magnitude
+    __device__ inline void largest(float (&m)[kPairs]) const {
+        bool bad = false;
 #pragma unroll
-        for (int a = 0; a < kTiles; ++a)
+        for (int p = 0; p < kPairs; ++p) {
+            float x[2] = {};
 #pragma unroll
-            for (int p = 0; p < kPairs; ++p) {
-                grow(m[2 * p], s[a][p][0], s[a][p][1]);
-                grow(m[2 * p + 1], s[a][p][2], s[a][p][3]);
+            for (int a = 0; a < kTiles; ++a) {
+                grow(x[0], s[a][p][0], s[a][p][1]);
+                grow(x[1], s[a][p][2], s[a][p][3]);
             }
-        const float t = wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-        if (t < __builtin_inff()) return t;
-        m[0] = 0.f;
+            m[p] = column_max(fmaxf(x[0], x[1]));
+            bad |= !(m[p] < __builtin_inff());
+        }
+        if (!__any(bad)) return;
 #pragma unroll
-        for (int a = 0; a < kTiles; ++a)
+        for (int p = 0; p < kPairs; ++p) {
+            m[p] = 0.f;
 #pragma unroll
-            for (int p = 0; p < kPairs; ++p)
+            for (int a = 0; a < kTiles; ++a)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) grow_finite(m[0], s[a][p][r]);
-        return wave_max(m[0]);
+                for (int r = 0; r < 4; ++r) grow_finite(m[p], s[a][p][r]);
+            m[p] = column_max(m[p]);
+        }
     }
 };
 
@@ -549,8 +553,8 @@ void linattn_kernel(LaCall c) {
         if (OUT) sq.load(left, q4);  // the next chunk, on its way meanwhile
         sk.load(left, k4);
         sv.load(left, v4);
-        float largest = 0.f;
-        if constexpr (kNorm) largest = S.largest();
+        float largest[G::kPairs] = {};
+        if constexpr (kNorm) S.largest(largest);
 
         if constexpr (kHalf) {
             u32x4 vf[G::kPairs];
@@ -563,9 +567,11 @@ void linattn_kernel(LaCall c) {
 #pragma unroll
                     for (int s = 0; s <= t; ++s) P[t][s] = f32x4{0.f, 0.f, 0.f, 0.f};
                 }
-                int exp_x = 0;
-                if constexpr (kNorm) exp_x = scale_to_half(largest);
-                const float fx = pow2(exp_x);
+                int exp_x[G::kPairs] = {};  // of the state as an operand, a column each
+                if constexpr (kNorm)
+#pragma unroll
+                    for (int p = 0; p < G::kPairs; ++p)
+                        exp_x[p] = min(scale_to_half(largest[p]), 126 - exp_s);
 #pragma unroll
                 for (int q = 0; q < D / 32; ++q) {
                     u32x4 qf[kTT], kf[kTT];
@@ -582,7 +588,7 @@ void linattn_kernel(LaCall c) {
 #pragma unroll
                     for (int p = 0; p < G::kPairs; ++p) {
                         f32x4 x = S.s[2 * q][p], y = S.s[2 * q + 1][p];
-                        if constexpr (kNorm) x *= fx, y *= fx;
+                        if constexpr (kNorm) x *= pow2(exp_x[p]), y *= pow2(exp_x[p]);
                         const u32x4 hi = take_part<T>(x, y, minus), lo = pack<T>(x, y);
 #pragma unroll
                         for (int t = 0; t < kTT; ++t) {
@@ -593,6 +599,19 @@ void linattn_kernel(LaCall c) {
                 }
 #pragma unroll
                 for (int p = 0; p < G::kPairs; ++p) vf[p] = read_columns<T, D>(tv, tile0 + p);
+                // a column of the state is a row of the output: lane 4 g + x has its scale
+                if constexpr (kNorm)
+#pragma unroll
+                    for (int p = 0; p < G::kPairs; ++p) {
+                        const int own = __float_as_int(pow2(-(exp_x[p] + exp_s)));
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const float back = __int_as_float(
+                                __builtin_amdgcn_ds_bpermute(4 * (4 * g + x), own));
+#pragma unroll
+                            for (int t = 0; t < kTT; ++t) O[t][p][x] *= back;
+                        }
+                    }
                 // scores: decayed, those of later tokens zero.  A tile's row is s = 4 g + x,
                 // its column t = l, of the same 16 tokens or the 16 before
                 float near[4], far[4];
@@ -645,7 +664,7 @@ void linattn_kernel(LaCall c) {
 #pragma unroll
                 for (int t = 0; t < kTT; ++t) {
                     float f = row * tile[t];
-                    if constexpr (kNorm) f = __builtin_ldexpf(f, exp_p[t] - exp_x - exp_s);
+                    if constexpr (kNorm) f = __builtin_ldexpf(f, exp_p[t]);
 #pragma unroll
                     for (int p = 0; p < G::kPairs; ++p) O[t][p] *= f;
                     f32x4 x = P[t][0], y = t ? P[t][t] : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -714,7 +733,9 @@ void linattn_kernel(LaCall c) {
                 }
                 // the scale of this chunk's v g^j, unless the state would leave 2^61
                 int e = most > 0.f ? scale_to_half(most) : exp_s;
-                const float left_s = largest * __builtin_fabsf(gc);
+                float top = largest[0];
+                if constexpr (G::kPairs == 2) top = fmaxf(top, largest[1]);
+                const float left_s = wave_max(top) * __builtin_fabsf(gc);
                 if (left_s > 0.f)
                     e = min(e, exp_s + min(120, scale_to_half(left_s) + 46));
                 S.scale(left_s > 0.f ? __builtin_ldexpf(gc, e - exp_s) : 0.f);

@@ -60,3 +60,46 @@ def test_large_token_after_an_infinite_value(at, dt):
     o, _ = c.fwd()
     c.tol(_np(o[:at - 1]), wo[:at - 1], ao[:at - 1])
     c.tol(_np(o[:at])[..., keep], wo[:at][..., keep], ao[:at][..., keep])
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,d", [(70, 64), (150, 128), (700, 64)])
+def test_large_column_of_the_state_beside_ordinary_ones(T, d, dt):
+    """The first state of 2^30 and -2^28 in one value of columns 3 and 8, which no
+    query reads: the other columns' outputs keep their digits.  Within the two
+    columns, two fp16 parts end at 2^-39 of the large value."""
+    c = Case(T, 1, 2, 1, d, d, dt, decay=[1.0, 0.999])
+    c.s0[:, :, 0, 3] = 2.0 ** 30
+    c.s0[:, :, 0, 8] = -2.0 ** 28
+    c.q[..., 0] = 0
+    o, s = c.fwd()
+    wo, ws = ref.linattn(*c.arrays())
+    ao, as_ = ref.linattn(*c.arrays(np.abs))
+    keep = [i for i in range(d) if i not in (3, 8)]
+    c.tol(_np(o)[..., keep], wo[..., keep], ao[..., keep])
+    c.tol(_np(s), ws, as_, fp32=True)
+    if dt == "f16":  # in the bound as 2^-16 of its terms
+        q = c.scale * np.abs(_np(c.q)).sum(3)
+        ao[..., 3] += 2.0 ** (16 - 39 + 30) * q
+        ao[..., 8] += 2.0 ** (16 - 39 + 28) * q
+    c.tol(_np(o), wo, ao)
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("T,d", [(70, 64), (150, 128), (700, 64)])
+def test_large_value_within_a_column(T, d, dt):
+    """Two fp16 parts end at 2^-39 of the largest value of their own column, all
+    that a small one may lose beside it: dq reads the state transposed, so its
+    columns hold the 2^30 of the first state beside ordinary values."""
+    c = Case(T, 1, 2, 1, d, d, dt, decay=[1.0, 0.999])
+    c.s0[:, :, 0, 3] = 2.0 ** 30
+    c.go[..., 3] = 0
+    dq = _np(c.bwd()[0])
+    z = np.zeros_like(_np(c.gs))
+    want = ref.linattn_grads(*c.arrays(), _np(c.go), z)[0]
+    absolute = ref.linattn_grads(*c.arrays(np.abs), np.abs(_np(c.go)), z)[0]
+    rel, least = ref.HALF_ULP[dt]
+    bound = ((2 * T + d + 24) * ref.EPS32 + 2.0 ** -16) * absolute + rel * np.abs(want) + least
+    if dt == "f16":
+        bound[..., 0] += 2.0 ** -39 * 2.0 ** 30 * c.scale * np.abs(_np(c.go)).sum(3)
+    assert (np.abs(dq - want) <= bound).all()
