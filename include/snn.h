@@ -481,10 +481,13 @@ int32_t snn_layer_dcur_t_layout(const snn_layer_desc *d);
  * sequence's length, taken as within [0, T]; tokens at and past it are not
  * read, their outputs and gradients are 0, and the state ends at the last token
  * before it.  A token never reaches an earlier token's output, whatever its
- * values (infinities and NaN included).  Sums and the state are fp32; 16-bit
- * operands are multiplied exactly, and where a score or the state becomes an
- * operand of a 16-bit product it is held as two parts (the state's update: as
- * many as keep fp32's precision). */
+ * values (infinities and NaN included; where a term is infinite the sum may come
+ * out as NaN).  Sums and the state are fp32; 16-bit operands are multiplied
+ * exactly, and where a score, the state or a decayed value becomes an operand of a
+ * 16-bit product it is held in parts: a score and the state to 2^-16 of itself, the
+ * value that is added to the state to 2^-24 (fp16: 2^-22), and in fp16 none of them
+ * closer than 2^-39 of the largest beside it (the token's scores, the column of the
+ * state, the column's decayed values of 32 tokens). */
 typedef struct snn_linattn_desc {
     int32_t T, B;            /* tokens, sequences (snn_linattn_step: T = 1) */
     int32_t heads, kv_heads; /* kv_heads divides heads */

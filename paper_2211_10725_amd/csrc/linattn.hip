@@ -26,7 +26,10 @@
 // precision (three bf16, two fp16).  fp16 parts are taken after a scaling by a
 // power of two that puts the largest value near 2^14, so neither large sums nor
 // small ones leave the type's range: the largest of a token's scores, of a column of
-// the state, and of the wave's part of v g^j.  Two parts then end at 2^-39 of it.  fp32 operands go through the fp32
+// the state, of a chunk's column of v g^j.  Two parts then end at 2^-39 of it.  (Shared
+// by more than one token or column, a scale would let one take another's digits.  Two
+// bf16 parts of every fp16 operand need no scales, but 180 matrix instructions a chunk
+// in place of 84: 128 heads of 128 there and back 444 us against 370.)  fp32 operands go through the fp32
 // matrix instructions as they are.
 //
 // A masked score is replaced by zero, but a zero times a later token's infinite
@@ -83,20 +86,6 @@ __device__ inline int divided(int n, double by) {
 }
 __device__ inline float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// largest of 64 lanes' values >= 0, the same in every lane
-__device__ inline float wave_max(float x) {
-#define SNN_DPP_MAX(ctrl)                                                                         \
-    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xf, 0xf, \
-                                                            false)))
-    SNN_DPP_MAX(0x111);  // row_shr:1, 2, 4, 8: lane 15 of each row has the row's
-    SNN_DPP_MAX(0x112);
-    SNN_DPP_MAX(0x114);
-    SNN_DPP_MAX(0x118);
-    SNN_DPP_MAX(0x142);  // row_bcast:15, 31: lane 63 has them all
-    SNN_DPP_MAX(0x143);
-#undef SNN_DPP_MAX
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
-}
 // largest over lanes l, l + 16, l + 32 and l + 48 of values >= 0: those that hold one
 // token of the scores, or one column of the state
 __device__ inline float column_max(float x) {
@@ -410,11 +399,13 @@ struct State {
                 }
         }
     }
+    __device__ inline void scale(int p, float f) {
+#pragma unroll
+        for (int a = 0; a < kTiles; ++a) s[a][p] *= f;
+    }
     __device__ inline void scale(float f) {
 #pragma unroll
-        for (int a = 0; a < kTiles; ++a)
-#pragma unroll
-            for (int p = 0; p < kPairs; ++p) s[a][p] *= f;
+        for (int p = 0; p < kPairs; ++p) scale(p, f);
     }
     // each column's largest finite magnitude
     __device__ inline void largest(float (&m)[kPairs]) const {
@@ -500,7 +491,7 @@ void linattn_kernel(LaCall c) {
                 S.add_slot(decay_power(decay, min(max(len - s * c.seg_len, 0), c.seg_len)),
                            slot + (s + 1) * slot_seg, r.slot_trans);
     }
-    int exp_s = 0;  // fp16: the state is s 2^-exp_s
+    int exp_s[G::kPairs] = {};  // fp16: column p of the state is s 2^-exp_s[p]
 
     // this lane's token and columns of the output, and their step over tokens
     const int64_t ostep = r.reverse ? -r.ot : r.ot;
@@ -571,7 +562,7 @@ void linattn_kernel(LaCall c) {
                 if constexpr (kNorm)
 #pragma unroll
                     for (int p = 0; p < G::kPairs; ++p)
-                        exp_x[p] = min(scale_to_half(largest[p]), 126 - exp_s);
+                        exp_x[p] = min(scale_to_half(largest[p]), 126 - exp_s[p]);
 #pragma unroll
                 for (int q = 0; q < D / 32; ++q) {
                     u32x4 qf[kTT], kf[kTT];
@@ -603,7 +594,7 @@ void linattn_kernel(LaCall c) {
                 if constexpr (kNorm)
 #pragma unroll
                     for (int p = 0; p < G::kPairs; ++p) {
-                        const int own = __float_as_int(pow2(-(exp_x[p] + exp_s)));
+                        const int own = __float_as_int(pow2(-(exp_x[p] + exp_s[p])));
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             const float back = __int_as_float(
@@ -715,43 +706,50 @@ void linattn_kernel(LaCall c) {
             };
             float w[G::kPairs][8];
             if constexpr (kNorm) {
-                float m[2] = {};
+                float most[G::kPairs];
+                bool bad = false;
 #pragma unroll
                 for (int p = 0; p < G::kPairs; ++p) {
+                    float m[2] = {};
                     weighted(p, w[p]);
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) grow(m[p], w[p][j], w[p][j + 1]);
+                    for (int j = 0; j < 8; j += 4) {
+                        grow(m[0], w[p][j], w[p][j + 1]);
+                        grow(m[1], w[p][j + 2], w[p][j + 3]);
+                    }
+                    most[p] = column_max(fmaxf(m[0], m[1]));
+                    bad |= !(most[p] < __builtin_inff());
                 }
-                float most = wave_max(fmaxf(m[0], m[1]));
-                if (!(most < __builtin_inff())) {
-                    most = 0.f;
+                if (__any(bad)) {
 #pragma unroll
-                    for (int p = 0; p < G::kPairs; ++p)
+                    for (int p = 0; p < G::kPairs; ++p) {
+                        most[p] = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) grow_finite(most, w[p][j]);
-                    most = wave_max(most);
+                        for (int j = 0; j < 8; ++j) grow_finite(most[p], w[p][j]);
+                        most[p] = column_max(most[p]);
+                    }
                 }
-                // the scale of this chunk's v g^j, unless the state would leave 2^61
-                int e = most > 0.f ? scale_to_half(most) : exp_s;
-                float top = largest[0];
-                if constexpr (G::kPairs == 2) top = fmaxf(top, largest[1]);
-                const float left_s = wave_max(top) * __builtin_fabsf(gc);
-                if (left_s > 0.f)
-                    e = min(e, exp_s + min(120, scale_to_half(left_s) + 46));
-                S.scale(left_s > 0.f ? __builtin_ldexpf(gc, e - exp_s) : 0.f);
-                exp_s = e;
+#pragma unroll
+                for (int p = 0; p < G::kPairs; ++p) {
+                    // the scale of this chunk's v g^j, unless the state would leave 2^61
+                    int e = most[p] > 0.f ? scale_to_half(most[p]) : exp_s[p];
+                    const float left_s = largest[p] * __builtin_fabsf(gc);
+                    if (left_s > 0.f)
+                        e = min(e, exp_s[p] + min(120, scale_to_half(left_s) + 46));
+                    S.scale(p, left_s > 0.f ? __builtin_ldexpf(gc, e - exp_s[p]) : 0.f);
+                    exp_s[p] = e;
+                }
             } else {
                 S.scale(gc);
             }
             constexpr int kParts = kNorm ? 2 : 3;
-            const float fv = pow2(exp_s);
             u32x4 part[G::kPairs][kParts];
 #pragma unroll
             for (int p = 0; p < G::kPairs; ++p) {
                 float x[8];
                 if constexpr (kNorm) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = w[p][j] * fv;
+                    for (int j = 0; j < 8; ++j) x[j] = w[p][j] * pow2(exp_s[p]);
                 } else {
                     weighted(p, x);
                 }
@@ -875,7 +873,9 @@ void linattn_kernel(LaCall c) {
         n = next;
         out += count * obytes;
     }
-    if (kNorm) S.scale(pow2(-exp_s));  // |exp_s| <= 120
+    if (kNorm)
+#pragma unroll
+        for (int p = 0; p < G::kPairs; ++p) S.scale(p, pow2(-exp_s[p]));  // |exp_s| <= 120
     if constexpr (OUT) {
         // tokens past the sequence's end
         const int from = max(begin, len), to = (int)min((int64_t)begin + c.seg_len, (int64_t)c.T);

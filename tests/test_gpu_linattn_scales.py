@@ -103,3 +103,41 @@ def test_large_value_within_a_column(T, d, dt):
     if dt == "f16":
         bound[..., 0] += 2.0 ** -39 * 2.0 ** 30 * c.scale * np.abs(_np(c.go)).sum(3)
     assert (np.abs(dq - want) <= bound).all()
+
+
+def _columns(x, sizes):
+    """The last dimension's values times powers of two in turn, as the type holds them."""
+    f = torch.as_tensor(np.resize(sizes, x.shape[-1]), dtype=torch.float32, device=x.device)
+    x.copy_((x.float() * f).to(x.dtype))
+
+
+# fp16 holds 2^-24 to 65504; each size is beside every other within 16 columns
+SIZES = [1.0, 2.0 ** 13, 2.0 ** -10, 2.0 ** -22, 1.0, 2.0 ** -16, 2.0 ** 10]
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("decay", [[1.0], [0.97]])
+@pytest.mark.parametrize("T,d", [(70, 64), (150, 128), (700, 64)])
+@pytest.mark.parametrize("what", ["v", "k", "q", "go"])
+def test_columns_of_unequal_size(what, T, d, decay, dt):
+    """Values, keys, queries or output gradients whose columns lie up to 2^35
+    apart, over several chunks and segments: states and gradients of the small
+    columns keep their digits."""
+    c = _rescaled(Case(T, 1, 2, 1, d, d, dt, decay=decay), 2.0 ** -12)
+    c.gs *= 2.0 ** -6  # gradients of at most 2^13 times it stay in fp16's range
+    _columns(getattr(c, what), SIZES)
+    c.check_fwd()
+    c.check_bwd()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_column_of_the_smallest_values_beside_the_largest(dt):
+    """+-6e4 beside 2^-24 in neighbouring columns at decay 1: what every chunk adds
+    to the small one stays in the state."""
+    c = _rescaled(Case(200, 1, 1, 1, 64, 64, dt, decay=[1.0], state=False), 2.0 ** -6)
+    sign = torch.as_tensor((-1.0) ** np.arange(200), device="cuda").view(200, 1, 1)
+    c.v[..., 4] = (6e4 * sign).to(c.v.dtype)
+    c.v[..., 5] = 2.0 ** -24
+    c.k[:] = 1
+    c.check_fwd()
+    assert torch.equal(c.s[0, 0, :, 5], torch.full((64,), 200 * 2.0 ** -24, device="cuda"))
