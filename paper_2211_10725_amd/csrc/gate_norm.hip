@@ -15,6 +15,8 @@
 // Bound by HBM.  16384 rows of 2048 (bf16 block, fp32 residual stream, 16 heads):
 // forward 93 us, 5.0 TB/s, as a large copy; backward 155 to 164, 4.5 to 4.8 TB/s.
 // 8192 rows of 4096 (fp16) with 8-bit checkpoints: 119 and 166.
+#include <float.h>
+
 #include "snn_internal.hpp"
 
 namespace snn {
@@ -37,7 +39,8 @@ __device__ inline float exp_of(float x) {
     return e > 0.f && e < __builtin_inff() ? __builtin_fmaf(e, r * kLn2, e) : e;
 }
 
-// the gate's factor and its derivative
+// The gate's factor and its derivative.  The sigmoid's is p (1 - p), taken as p e^-g p:
+// 1 - p of an open gate would have few digits of e^-g left, from g = 17 on none.
 template <bool SLOPE>
 __device__ inline void gate_of(int gate, float g, float &act, float &slope) {
     if (gate == SNN_GATE_MUL) {
@@ -45,10 +48,10 @@ __device__ inline void gate_of(int gate, float g, float &act, float &slope) {
         slope = 1.f;
         return;
     }
-    const float p = __builtin_amdgcn_rcpf(1.f + exp_of(-g));
+    const float e = exp_of(-g), p = __builtin_amdgcn_rcpf(1.f + e);
     act = gate == SNN_GATE_SILU ? g * p : p;
     if (SLOPE) {
-        const float q = p * (1.f - p);
+        const float q = p * (fminf(e, FLT_MAX) * p);  // (p is 0 where e is infinite)
         slope = gate == SNN_GATE_SILU ? __builtin_fmaf(g, q, p) : q;
     }
 }
