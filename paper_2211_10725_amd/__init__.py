@@ -565,7 +565,8 @@ _GATE = {"none": GATE_NONE, "mul": GATE_MUL, "sigmoid": GATE_SIGMOID, "silu": GA
 
 
 def _row_stride(t):
-    """Row stride of a tensor [..., n] whose leading dimensions are one row index."""
+    """Row stride of a tensor [..., n] whose leading dimensions are one row index
+    and whose rows are contiguous (ValueError for others)."""
     n, st = t.shape, t.stride()
     if t.numel() == 0:
         return max(n[-1], 1)
@@ -613,7 +614,8 @@ def _need_rows(fn, what, t, d, dtype, ld):
     if t.dtype is dtype and shape[-1] == n and t.numel() == rows * n:
         if len(shape) == 2 and t.stride() == (ld, 1):
             return
-        if rows <= 1 or _row_stride(t) == ld:
+        # a single row may have any stride, its values must lie together all the same
+        if _row_stride(t) == ld or rows <= 1:
             return
     raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is not "
                      "what the descriptor says")
