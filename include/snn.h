@@ -475,7 +475,10 @@ int32_t snn_layer_dcur_t_layout(const snn_layer_desc *d);
  * o [T,B,heads,d_v] are strided: element (t,b,h,i) lies at
  * t stride[0] + b stride[1] + h stride[2] + i, so they may be slices of one
  * packed projection.  Query head h reads key and value head
- * h / (heads / kv_heads).  Gradients have their tensors' strides.
+ * h / (heads / kv_heads).  Gradients have their tensors' strides.  What is only read
+ * may be a broadcast (stride 0); of what is written, o and in the backward the
+ * gradients of q, k and v, no two rows may share addresses, and a stride that makes
+ * them (below the row's values, or another dimension's multiple) is SNN_ERR_SHAPE.
  *
  * lens (device int32 [B], or NULL: every sequence has T tokens) gives each
  * sequence's length, taken as within [0, T]; tokens at and past it are not

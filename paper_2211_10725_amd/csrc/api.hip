@@ -913,6 +913,26 @@ bool any_misaligned(std::initializer_list<const void *> ps) {
     return false;
 }
 
+// Whether rows of `width` values surely share addresses, those of neighbours in one
+// dimension or of the nearest elements of two: a broadcast or a window over a tensor.
+// It may be read, but written by many workgroups it would hold the last one's values.
+bool rows_overlap(const snn_linattn_desc *d, int heads, const int64_t *st, int width) {
+    const int64_t n[3] = {d->T, d->B, heads};
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] < 2 || d->T == 0) continue;
+        if (st[i] < width) return true;
+        for (int j = 0; j < 3; ++j) {
+            if (j == i || n[j] < 2 || st[j] < st[i]) continue;
+            // one step of j against a steps of i, from below and from above
+            const int64_t a = st[j] / st[i];
+            if ((a < n[i] && st[j] - a * st[i] < width) ||
+                (a + 1 < n[i] && (a + 1) * st[i] - st[j] < width))
+                return true;
+        }
+    }
+    return false;
+}
+
 LaOperand operand(const void *p, const int64_t *st, int share) {
     return LaOperand{p, st[0], st[1], st[2], 1.0 / share};
 }
@@ -1016,6 +1036,7 @@ snn_status snn_linattn_fwd(const snn_linattn_desc *d, const void *q, const void 
     const snn_status st = check_linattn(d);
     if (st != SNN_OK) return st;
     if (d->B == 0 || d->heads == 0) return SNN_OK;
+    if (rows_overlap(d, d->heads, d->o_stride, d->d_v)) return SNN_ERR_SHAPE;
     if (!decay || (d->T > 0 && (!q || !k || !v || !o))) return SNN_ERR_NULL;
     if (any_misaligned({q, k, v, decay, lens, state_in, o, state_out, ws})) return SNN_ERR_ALIGN;
     const size_t need = snn_linattn_workspace_bytes(d);
@@ -1048,6 +1069,10 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
     const snn_status st = check_linattn(d);
     if (st != SNN_OK) return st;
     if (d->B == 0 || d->heads == 0) return SNN_OK;
+    if (rows_overlap(d, d->heads, d->q_stride, d->d_k) ||
+        rows_overlap(d, d->kv_heads, d->k_stride, d->d_k) ||
+        rows_overlap(d, d->kv_heads, d->v_stride, d->d_v))
+        return SNN_ERR_SHAPE;
     if (!decay || (d->T > 0 && (!q || !k || !v || !grad_o || !grad_q || !grad_k || !grad_v)))
         return SNN_ERR_NULL;
     // grad_k's heads read the state's gradient while grad_v's may have written theirs
@@ -1114,6 +1139,7 @@ snn_status snn_linattn_step(const snn_linattn_desc *d, const void *q, const void
     if (st != SNN_OK) return st;
     if (d->T != 1 || n_slots < 0 || (!slots && n_slots < d->B)) return SNN_ERR_SHAPE;
     if (d->B == 0 || d->heads == 0) return SNN_OK;
+    if (rows_overlap(d, d->heads, d->o_stride, d->d_v)) return SNN_ERR_SHAPE;
     if (!q || !k || !v || !decay || !state_in || !state_out || !o) return SNN_ERR_NULL;
     if (any_misaligned({q, k, v, decay, slots, state_in, state_out, o})) return SNN_ERR_ALIGN;
     const int share = d->heads / d->kv_heads;
