@@ -519,7 +519,7 @@ template <typename T, bool SAVE>
 __global__ __launch_bounds__(256) void checkpoint_kernel(int64_t units, uint32_t per_row, int n,
                                                          int block, int64_t ld, T *x,
                                                          int8_t *codes, float *scales) {
-    const int64_t u = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int64_t u = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + threadIdx.x / 16;
     const bool live = u < units;
     const int64_t row = live ? (uint32_t)u / per_row : 0;
     const int e = live ? (int)((uint32_t)u % per_row) * 128 + 8 * (threadIdx.x & 15) : 0;
@@ -597,7 +597,9 @@ template <typename T>
 void run_checkpoint(int64_t rows, int n, int block, int64_t ld, void *x, int8_t *codes,
                     float *scales, bool save, hipStream_t s) {
     const int64_t per_row = ckpt_blocks(n, 128), units = rows * per_row;
-    const int grid = (int)((units + 15) / 16);
+    // a dimension of a launch has fewer than 2^32 threads
+    const int64_t groups = (units + 15) / 16, x_groups = std::min<int64_t>(groups, 1 << 23);
+    const dim3 grid((unsigned)x_groups, (unsigned)((groups + x_groups - 1) / x_groups));
     if (save)
         checkpoint_kernel<T, true><<<grid, 256, 0, s>>>(units, (uint32_t)per_row, n, block, ld,
                                                         (T *)x, codes, scales);
