@@ -493,7 +493,7 @@ int32_t snn_layer_dcur_t_layout(const snn_layer_desc *d);
  * state, the column's decayed values of 32 tokens). */
 typedef struct snn_linattn_desc {
     int32_t T, B;            /* tokens, sequences (snn_linattn_step: T = 1) */
-    int32_t heads, kv_heads; /* kv_heads divides heads */
+    int32_t heads, kv_heads; /* kv_heads divides heads; B heads < 2^24 */
     int32_t d_k, d_v;        /* multiples of 8, 8 .. 128 */
     int32_t dtype;           /* q, k, v, o and their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
     float scale;             /* finite */

@@ -896,8 +896,8 @@ snn_status check_linattn(const snn_linattn_desc *d) {
         return SNN_ERR_SHAPE;
     if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
     if (!finite(d->scale)) return SNN_ERR_SHAPE;
-    // grids of at most 2^31 workgroups, element offsets far inside 63 bits
-    if (d->T > ((int32_t)1 << 30) || (int64_t)d->B * d->heads > ((int64_t)1 << 24) ||
+    // launches of fewer than 2^32 threads, element offsets far inside 63 bits
+    if (d->T > ((int32_t)1 << 30) || (int64_t)d->B * d->heads >= kLaMaxGroups ||
         (int64_t)d->T * d->B * d->heads > ((int64_t)1 << 34))
         return SNN_ERR_SHAPE;
     const int64_t *strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->o_stride};
@@ -1075,6 +1075,10 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
         return SNN_ERR_SHAPE;
     if (!decay || (d->T > 0 && (!q || !k || !v || !grad_o || !grad_q || !grad_k || !grad_v)))
         return SNN_ERR_NULL;
+    // the sum over shared heads: 8 values a thread
+    if (d->kv_heads < d->heads && (int64_t)d->T * d->B * d->kv_heads *
+                                          (std::max(d->d_k, d->d_v) / 8) > UINT32_MAX - 255)
+        return SNN_ERR_SHAPE;
     // grad_k's heads read the state's gradient while grad_v's may have written theirs
     if (grad_state_in && grad_state_in == grad_state_out) return SNN_ERR_UNSUPPORTED;
     if (any_misaligned({q, k, v, decay, lens, state_in, grad_o, grad_state_out, grad_q, grad_k,

@@ -1127,6 +1127,17 @@ static hipError_t launch_width(const LaCall &c, hipStream_t s) {
 }
 
 hipError_t launch_linattn(const LaCall &c, int dtype, hipStream_t s) {
+    // more heads than one launch takes, uncut by far: a role each
+    if (c.roles > 1 && (int64_t)c.roles * c.B * c.H >= kLaMaxGroups) {
+        for (int i = 0; i < c.roles; ++i) {
+            LaCall one = c;
+            one.role[0] = c.role[i];
+            one.roles = 1;
+            const hipError_t e = launch_linattn(one, dtype, s);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     switch (dtype) {
         case SNN_F32: return launch_width<float>(c, s);
         case SNN_F16: return launch_width<half_t>(c, s);

@@ -329,6 +329,9 @@ struct LaRole {
 };
 constexpr int kLaRoles = 3;
 constexpr int kLaMaxD = 128;  // largest head size
+// Workgroups of a launch, fewer: at 2^32 threads of a dimension (256 of each) a launch
+// wraps without an error.
+constexpr int64_t kLaMaxGroups = (int64_t)1 << 24;
 struct LaCall {
     LaRole role[kLaRoles];
     const float *decay;

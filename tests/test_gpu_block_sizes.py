@@ -20,3 +20,24 @@ def test_checkpoint_of_more_rows_than_a_dimension_of_a_launch():
     back = torch.full_like(x, float("nan"))
     snn.snn_checkpoint_load(kept, back)
     assert torch.equal(back, x)
+
+
+def test_linear_attention_backward_of_more_heads_than_one_launch():
+    """5.6 million heads: three gradients of a workgroup of 256 threads each pass
+    2^32.  One token of integer values, so that every sum is exact."""
+    B, H, d = 349600, 16, 8
+    assert 3 * B * H >= 2 ** 24
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    q, k, v, go = (torch.randint(-3, 4, (1, B, H, d), generator=gen, device="cuda").half()
+                   for _ in range(4))
+    desc = snn.linattn_desc(q, k, v, go, 1.0)
+    decay = torch.full((H,), 0.5, device="cuda")
+    dq, dk, dv = (torch.full_like(x, float("nan")) for x in (q, k, v))
+    ws = torch.empty(max(16, snn.snn_linattn_workspace_bytes(desc)), dtype=torch.uint8,
+                     device="cuda")
+    snn.snn_linattn_bwd(desc, q, k, v, decay, None, None, go, None, dq, dk, dv, None, ws)
+    f = [x.float() for x in (q, k, v, go)]
+    vg = (f[2] * f[3]).sum(3, keepdim=True)
+    kq = (f[0] * f[1]).sum(3, keepdim=True)
+    for got, want in ((dq, f[1] * vg), (dk, f[0] * vg), (dv, kq * f[3])):
+        assert torch.equal(got.float(), want)
