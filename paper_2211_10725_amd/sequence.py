@@ -75,17 +75,51 @@ class SequenceNet:
 
     # ---- buffers and descriptors of one shape -------------------------------
     def _plan(self, T, B, train=False):
-        """Descriptors and buffers for T steps of B sequences, made once per
-        shape (`train`: with what the backward needs)."""
+        """Descriptors and buffers for T steps of B sequences (`train`: with what
+        the backward needs), kept for later calls of the shape.  Those of prompts
+        and steps hold at most four times the largest's memory together: the
+        longest unused go first, but never one that a graph was captured from."""
         key = (T, B, train)
-        if key in self.plans:
-            return self.plans[key]
+        p = self.plans.pop(key, None)
+        made = p is None
+        if made:
+            p = self._new_plan(T, B, train)
+        self.plans[key] = p  # the last one used is the last
+        if p.stream is not None:
+            stream = snn._stream(None)
+            if stream != p.stream and stream not in p.others:
+                p.others[stream] = self.torch.cuda.current_stream()
+            p.stays = p.stays or self.torch.cuda.is_current_stream_capturing()
+        if made:
+            self._drop_plans(p)
+        return p
+
+    def _drop_plans(self, newest):
+        old = {k: p for k, p in self.plans.items() if not k[2] and not p.stays}
+        held = [p.bytes for p in old.values()]
+        most, held, count = 4 * max(held, default=0), sum(held), len(held)
+        for k, p in old.items():
+            if (held <= most and count <= 256) or p is newest:
+                break
+            del self.plans[k]
+            held, count = held - p.bytes, count - 1
+            for t in p.bufs:  # their memory is free once those streams are done, too
+                for other in p.others.values():
+                    t.record_stream(other)
+
+    def _new_plan(self, T, B, train):
         torch = self.torch
         p = type("Plan", (), {})()
+        p.bufs, p.others, p.stays = [], {}, False
+        p.stream = snn._stream(None) if torch.device(self.device).type == "cuda" else None
         L = len(self.W)
 
+        def new(*shape, dtype):
+            p.bufs.append(torch.empty(shape, dtype=dtype, device=self.device))
+            return p.bufs[-1]
+
         def buf(*shape):
-            return torch.empty(shape, dtype=torch.float32, device=self.device)
+            return new(*shape, dtype=torch.float32)
 
         def dense(n_in, n_out, in_dtype=snn.F32):
             return snn.layer_desc(dict(kind="dense", n_in=n_in, n_out=n_out, neuron="leaky",
@@ -110,21 +144,20 @@ class SequenceNet:
         if train:
             sizes += [snn.snn_gate_norm_workspace_bytes(d) for d in (p.norm, p.first)]
             sizes += [snn.snn_loss_workspace_bytes(snn.LOSS_CE_COUNT, B, self.n_out)]
-            p.spk = torch.empty((T, B, self.n_out), dtype=torch.uint8, device=self.device)
-            p.saved = torch.empty(snn.snn_layer_saved_bytes(p.readout), dtype=torch.uint8,
-                                  device=self.device)
+            p.spk = new(T, B, self.n_out, dtype=torch.uint8)
+            p.saved = new(snn.snn_layer_saved_bytes(p.readout), dtype=torch.uint8)
             p.counts, p.gcounts = buf(B, self.n_out), buf(B, self.n_out)
             p.loss = buf(4)
             p.dx, p.dh, p.dcur = buf(T, B, self.n), buf(T, B, self.n), buf(T, B, self.n_proj)
             p.do = buf(T, B, self.n)
             if self.checkpoints:
                 def ckpt(n, block):
-                    return [torch.empty(snn.snn_checkpoint_bytes(T * B, n, block),
-                                        dtype=torch.uint8, device=self.device) for _ in range(L)]
+                    return [new(snn.snn_checkpoint_bytes(T * B, n, block), dtype=torch.uint8)
+                            for _ in range(L)]
                 p.o8, p.gate8 = ckpt(self.n, self.block), ckpt(self.n, self.block)
                 p.h8, p.qkv8 = ckpt(self.n, 128), ckpt(self.n_qkv, self.qkv_block)
-        p.ws = torch.empty(max(sizes + [256]), dtype=torch.uint8, device=self.device)
-        self.plans[key] = p
+        p.ws = new(max(sizes + [256]), dtype=torch.uint8)
+        p.bytes = sum(t.numel() * t.element_size() for t in p.bufs)
         return p
 
     def _parts(self, cur):
