@@ -132,7 +132,6 @@ class SequenceNet:
         p.h = [buf(T, B, self.n) for _ in range(L + 1 if kept == L else 2)]
         p.cur = [buf(T, B, self.n_proj) for _ in range(kept)]
         p.o = [buf(T, B, self.n) for _ in range(kept)]
-        p.logits = buf(T, B, self.n_out)
         q, k, v, gate = self._parts(p.cur[0])
         o = p.o[0].unflatten(2, (self.heads, self.d_v))
         p.attn = snn.linattn_desc(q, k, v, o)
@@ -147,7 +146,6 @@ class SequenceNet:
             p.spk = new(T, B, self.n_out, dtype=torch.uint8)
             p.saved = new(snn.snn_layer_saved_bytes(p.readout), dtype=torch.uint8)
             p.counts, p.gcounts = buf(B, self.n_out), buf(B, self.n_out)
-            p.loss = buf(4)
             p.dx, p.dh, p.dcur = buf(T, B, self.n), buf(T, B, self.n), buf(T, B, self.n_proj)
             p.do = buf(T, B, self.n)
             if self.checkpoints:
@@ -192,31 +190,34 @@ class SequenceNet:
                                   p.o8[i] if ckpt else None, p.gate8[i] if ckpt else None)
         return at(p.h, L)
 
+    def _currents(self, p, h):
+        out = h.new_empty((*h.shape[:2], self.n_out))
+        snn.snn_synapse_fwd(p.readout, h, self.R, None, out, None, p.ws)
+        return out
+
     def prompt(self, spikes, states, lens=None):
         """Whole sequences spikes [T,B,n_in] u8 from `states` (updated in place);
-        returns the readout's currents [T,B,n_out].  lens: int32 [B] lengths."""
+        returns the readout's currents [T,B,n_out], a tensor of their own.  lens:
+        int32 [B] lengths."""
         T, B = spikes.shape[:2]
         p = self._plan(T, B)
 
         def attend(i, q, k, v, o):
             snn.snn_linattn_fwd(p.attn, q, k, v, self.decay, lens, states[i], o, states[i], p.ws)
 
-        h = self._run(p, spikes, attend, False)
-        snn.snn_synapse_fwd(p.readout, h, self.R, None, p.logits, None, p.ws)
-        return p.logits
+        return self._currents(p, self._run(p, spikes, attend, False))
 
     def step(self, spikes, states, slots=None):
         """One time step spikes [B,n_in] of running requests; request b's states
-        lie in slot slots[b] (int32, or b) of `states`, updated in place."""
+        lie in slot slots[b] (int32, or b) of `states`, updated in place.  Returns
+        the currents [B,n_out]."""
         B = spikes.shape[0]
         p = self._plan(1, B)
 
         def attend(i, q, k, v, o):
             snn.snn_linattn_step(p.attn, q, k, v, self.decay, slots, states[i], states[i], o)
 
-        h = self._run(p, spikes.unsqueeze(0), attend, False)
-        snn.snn_synapse_fwd(p.readout, h, self.R, None, p.logits, None, p.ws)
-        return p.logits[0]
+        return self._currents(p, self._run(p, spikes.unsqueeze(0), attend, False))[0]
 
     # ---- training ------------------------------------------------------------
     def train_step(self, spikes, labels):
@@ -230,7 +231,8 @@ class SequenceNet:
 
         h = self._run(p, spikes, attend, True)
         snn.snn_layer_fwd(p.readout, h, self.R, None, None, p.spk, p.saved, p.counts, p.ws)
-        snn.snn_loss(snn.LOSS_CE_COUNT, B, self.n_out, 1, p.counts, labels, None, p.loss,
+        loss = h.new_empty(4)
+        snn.snn_loss(snn.LOSS_CE_COUNT, B, self.n_out, 1, p.counts, labels, None, loss,
                      p.gcounts, p.ws)
         snn.snn_layer_bwd(p.readout, snn.GRAD_BCAST, p.gcounts, h, self.R, None, p.saved, self.gR,
                           None, None, p.dh, p.ws)
@@ -258,7 +260,7 @@ class SequenceNet:
         snn.snn_gate_norm_bwd(p.first, p.dx, p.dh, p.x[0], None, None, None, None, None, None,
                               self.w_pre[0], p.dx, None, None, None, None, self.gw_pre[0], p.ws)
         snn.snn_synapse_bwd(p.embed, p.dx, None, spikes, self.E, self.gE, None, p.ws)
-        return p.loss[0]
+        return loss[0]
 
     def init_adamw(self, **hparams):
         zeros = self.torch.zeros_like
