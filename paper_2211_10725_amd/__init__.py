@@ -205,7 +205,10 @@ def _stream(stream):
         if torch.cuda.is_initialized():
             # the current stream's handle itself: a Stream object around it costs
             # several microseconds, more than a small call's kernel
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+            try:
+                return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+            except AttributeError:  # torch's private names
+                pass
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream

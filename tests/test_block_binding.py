@@ -44,3 +44,18 @@ def test_single_rows_and_single_values_of_any_stride_go_through():
         snn._need_rows("fn", "x", t, d, torch.float32, d.ld_x)
     one = snn.gate_norm_desc(torch.empty(1, 1))
     snn._need_rows("fn", "x", torch.empty(1, 7)[:, ::3][:, :1], one, torch.float32, one.ld_x)
+
+
+def test_current_stream_without_the_private_names(monkeypatch):
+    """The quick way to the current stream's handle is torch's own business: where
+    it is absent, the public one is taken."""
+    class Stream:
+        cuda_stream = 1234
+
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream)
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        with monkeypatch.context() as m:
+            m.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+            m.delattr(torch._C, name, raising=False)
+            assert snn._stream(None) == 1234
