@@ -63,7 +63,7 @@
 extern "C" {
 #endif
 
-#define SNN_ABI_VERSION 12
+#define SNN_ABI_VERSION 13
 
 typedef enum snn_status {
     SNN_OK = 0,
@@ -499,10 +499,14 @@ typedef struct snn_linattn_desc {
     float scale;             /* finite */
     int64_t q_stride[3];     /* elements, multiples of 8, >= 0: time, sequence, head */
     int64_t k_stride[3], v_stride[3], o_stride[3];
+    int32_t forward_only; /* 1: no backward will follow (a prompt), which then is
+                             SNN_ERR_UNSUPPORTED; 0 otherwise */
 } snn_linattn_desc;
 
-/* Scratch bytes of snn_linattn_fwd and snn_linattn_bwd (the larger).  0 for an
- * invalid descriptor, and a valid answer. */
+/* Scratch bytes of snn_linattn_fwd and snn_linattn_bwd (the larger), or of the
+ * forward alone where the descriptor says so: the backward also holds fp32
+ * gradients of every query head where key heads are shared.  0 for an invalid
+ * descriptor, and a valid answer. */
 size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d);
 
 /* Whole sequences (a prompt, or the forward of a training step).

@@ -32,7 +32,7 @@ RESET_DETACHED, RESET_SURROGATE = 0, 1
 GRAD_FULL, GRAD_BCAST, GRAD_FOLD = 0, 1, 2
 LOSS_CE_COUNT, LOSS_MSE_COUNT = 0, 1
 FLAG_FP32_MFMA = 1
-ABI_VERSION = 12
+ABI_VERSION = 13
 DCUR_T_TRANSPOSED, DCUR_T_PLANES = 1, 2
 GATE_NONE, GATE_MUL, GATE_SIGMOID, GATE_SILU = 0, 1, 2, 3
 
@@ -107,7 +107,8 @@ class LinattnDesc(ctypes.Structure):
                 ("kv_heads", ctypes.c_int32), ("d_k", ctypes.c_int32), ("d_v", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
-                ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3)]
+                ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3),
+                ("forward_only", ctypes.c_int32)]
 
 
 class GateNormDesc(ctypes.Structure):
@@ -457,10 +458,11 @@ def snn_adamw(tensors, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay
 # --------------------------------------------------------------------------
 # leaky sequence block
 # --------------------------------------------------------------------------
-def linattn_desc(q, k, v, o, scale=None) -> LinattnDesc:
+def linattn_desc(q, k, v, o, scale=None, forward_only=False) -> LinattnDesc:
     """Descriptor of linear attention over q [T,B,heads,d_k], k [T,B,kv_heads,d_k],
     v [T,B,kv_heads,d_v] and o [T,B,heads,d_v]: tensors of one dtype, each row
-    contiguous, strided over time, sequence and head (scale: 1/sqrt(d_k) if None).
+    contiguous, strided over time, sequence and head (scale: 1/sqrt(d_k) if None;
+    forward_only: for prompts and steps, whose workspace leaves out the backward's).
     Later calls may pass other tensors of the same shapes and strides."""
     T, B, H, DK = q.shape
     KV, DV = k.shape[2], v.shape[3]
@@ -473,7 +475,8 @@ def linattn_desc(q, k, v, o, scale=None) -> LinattnDesc:
         raise ValueError("linattn_desc: each head's values must be contiguous")
     S = ctypes.c_int64 * 3
     return LinattnDesc(T, B, H, KV, DK, DV, _dtype_code(q), DK ** -0.5 if scale is None else scale,
-                       *(S(*t.stride()[:3]) if t.numel() else S() for t in (q, k, v, o)))
+                       *(S(*t.stride()[:3]) if t.numel() else S() for t in (q, k, v, o)),
+                       int(forward_only))
 
 
 def _need_heads(fn, what, t, dtype, shape, stride):

@@ -896,6 +896,7 @@ snn_status check_linattn(const snn_linattn_desc *d) {
         return SNN_ERR_SHAPE;
     if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
     if (!finite(d->scale)) return SNN_ERR_SHAPE;
+    if (d->forward_only != 0 && d->forward_only != 1) return SNN_ERR_UNSUPPORTED;
     // launches of fewer than 2^32 threads, element offsets far inside 63 bits
     if (d->T > ((int32_t)1 << 30) || (int64_t)d->B * d->heads >= kLaMaxGroups ||
         (int64_t)d->T * d->B * d->heads > ((int64_t)1 << 34))
@@ -1024,6 +1025,7 @@ extern "C" {
 
 size_t snn_linattn_workspace_bytes(const snn_linattn_desc *d) {
     if (check_linattn(d) != SNN_OK) return 0;
+    if (d->forward_only) return plan_of(d, 1).slot_bytes;
     return std::max(plan_of(d, 1).slot_bytes,
                     2 * plan_of(d, kLaRoles).slot_bytes + shared_grad_bytes(d, d->d_k) +
                         shared_grad_bytes(d, d->d_v));
@@ -1068,6 +1070,7 @@ snn_status snn_linattn_bwd(const snn_linattn_desc *d, const void *q, const void 
                            hipStream_t stream) {
     const snn_status st = check_linattn(d);
     if (st != SNN_OK) return st;
+    if (d->forward_only) return SNN_ERR_UNSUPPORTED;
     if (d->B == 0 || d->heads == 0) return SNN_OK;
     if (rows_overlap(d, d->heads, d->q_stride, d->d_k) ||
         rows_overlap(d, d->kv_heads, d->k_stride, d->d_k) ||

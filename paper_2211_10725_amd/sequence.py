@@ -134,7 +134,7 @@ class SequenceNet:
         p.o = [buf(T, B, self.n) for _ in range(kept)]
         q, k, v, gate = self._parts(p.cur[0])
         o = p.o[0].unflatten(2, (self.heads, self.d_v))
-        p.attn = snn.linattn_desc(q, k, v, o)
+        p.attn = snn.linattn_desc(q, k, v, o, forward_only=not train)
         p.norm = snn.gate_norm_desc(p.x[0], p.o[0], gate, self.heads, "silu", self.eps,
                                     ckpt_block=self.block)
         p.first = snn.gate_norm_desc(p.x[0], None, None, 1, "none", self.eps)
