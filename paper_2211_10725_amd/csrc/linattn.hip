@@ -1093,15 +1093,17 @@ hipError_t launch_chunks(const LaCall &c, hipStream_t s) {
 // While each has a compute unit to itself, shorter ones too: a chunk of 32 tokens in
 // fp32 (30 heads of 128 there and back, 101 tokens: 53 us, uncut 74; 8 heads, 1000
 // tokens: 98, in seven 135), 64 tokens in 16 bits from three on (the same in bf16,
-// 1000 tokens: 58 against 59; 30 heads, 128 tokens in two 31, uncut 26).  And where a second
-// segment would put two fp32 workgroups of 128 on a compute unit, none is cut (192
-// heads, 512 tokens: 147 us, in two 156).
+// 1000 tokens: 58 against 59; 30 heads, 128 tokens in two 31, uncut 26).  Two fp32
+// workgroups of 128 on a compute unit slow each other down, which three segments are
+// worth (129 heads, 384 tokens: 89 us, uncut 110; 4096: 784 and 1165) and two only over
+// long sequences (255 heads, 256 tokens: 89, uncut 80; 512: 156 and 157; 800: 229 and
+// 242; 4096: 1075 and 1186).
 LaPlan linattn_plan(int T, int64_t heads, int roles, int width, int dtype) {
     const int64_t slots = (width > 64 ? 2 : 4) * kPlanCus;
     const int64_t units = std::max<int64_t>(heads * roles, 1);
     const int least = dtype == SNN_F32 ? 32 : 64, most = (T - 1) / least + 1;
     int64_t segs = std::min<int64_t>(slots / units, T / 128);
-    if (dtype == SNN_F32 && width > 64 && 2 * units > kPlanCus && units <= kPlanCus) segs = 1;
+    if (dtype == SNN_F32 && width > 64 && segs == 2 && 2 * units > kPlanCus && T < 768) segs = 1;
     if (dtype == SNN_F32 || most > 2)
         segs = std::max(segs, std::min<int64_t>(kPlanCus / units, most));
     LaPlan p;

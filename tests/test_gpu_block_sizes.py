@@ -2,6 +2,7 @@
 import pytest
 
 import paper_2211_10725_amd as snn
+from tests.test_gpu_linattn import Case
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -41,3 +42,15 @@ def test_linear_attention_backward_of_more_heads_than_one_launch():
     kq = (f[0] * f[1]).sum(3, keepdim=True)
     for got, want in ((dq, f[1] * vg), (dk, f[0] * vg), (dv, kq * f[3])):
         assert torch.equal(got.float(), want)
+
+
+@pytest.mark.parametrize("H,T", [(131, 400), (200, 790)])
+def test_segments_of_more_heads_than_half_the_units(H, T):
+    c = Case(T, 1, H, H, 72, 104, "f32")
+    c.check_fwd()
+
+
+def test_segments_of_roles_and_heads_between_half_and_all_units():
+    c = Case(400, 1, 45, 45, 72, 80, "f32", lens=[393])
+    c.check_fwd()
+    c.check_bwd()
