@@ -3,7 +3,7 @@
 // sequence block").
 //
 // Every call is one pass over HBM: a row stays in registers between its sums
-// and the values that need them.  A row belongs to TPR threads (a wave for
+// and the values that need them, as far as the registers go (below).  A row belongs to TPR threads (a wave for
 // short rows, else a workgroup), thread t holding the NV runs of 8 channels
 // 8 (i TPR + t): one 16-byte access per 16-bit run.  Rows may start on any
 // element (odd widths, slices), which the memory pipeline takes as it is; only
@@ -13,8 +13,15 @@
 // workgroup order by a second kernel.
 //
 // Bound by HBM.  16384 rows of 2048 (bf16 block, fp32 residual stream, 16 heads):
-// forward 93 us, 5.0 TB/s, as a large copy; backward 155 to 164, 4.5 to 4.8 TB/s.
-// 8192 rows of 4096 (fp16) with 8-bit checkpoints: 119 and 166.
+// forward 93 us, 5.0 TB/s, as a large copy; backward 155 to 164, 4.5 to 4.8 TB/s
+// (all in bf16 131, 4.1).  8192 rows of 4096 (fp16) with 8-bit checkpoints: 119 and 166.
+//
+// The backward holds more than four waves of a SIMD have registers for.  With a 16-bit
+// block 9 to 33 registers a lane lie in scratch (17 in the backward above), in fp32 none
+// with up to 512 threads, which then take three waves, and 35 or 70 with 1024.  Rows of
+// more than 8192 channels, two runs a thread, leave most of theirs there: 4096 rows of
+// 12288 there and back take 1233 us in fp32 and 990 with a bf16 block, 1.6 and 1.4 TB/s
+// (forward alone 254 and 222, 4.0 and 3.2).
 #include <float.h>
 
 #include "snn_internal.hpp"
@@ -229,7 +236,10 @@ __device__ inline void row_sum(float (&s)[N], float *red) {
 // Sum of s over the groups of the row: on entry s[i] is the sum over run i of
 // this thread, on return that of the run's whole group.  `gl` runs make a group
 // (0: the row is one group).  A power of two up to a wave adds by exchanges,
-// anything else through `vec` (one slot per run of the row).
+// anything else through `vec` (one slot per run of the row), where each thread adds
+// its whole group: right for any count, and slow for large groups (8192 rows there and
+// back, bf16 block: four groups of 1000 475 us, one group of 4000 297; four of 2048
+// 1427 against 603; two of 8192 9638 against 2084).
 template <int TPR, int NV>
 __device__ inline void group_sum(float (&s)[NV], int gl, int runs, float *red, float *vec) {
     if (gl == 0) {
@@ -482,7 +492,8 @@ gate_norm_bwd_kernel(GateNormBwd c) {
 
 // Column sums over the workgroups' partial rows, in order within each of the 16
 // waves' shares, then over the waves; w_post's and scale's gradients are the
-// first sum times each other.
+// first sum times each other.  6.6 us for 1024 workgroups' rows of 1001 (32 workgroups
+// of 64 columns), 7.5 of 2048: latency.
 __global__ __launch_bounds__(1024) void column_sum_kernel(GateNormBwd c, int blocks) {
     const bool pre = blockIdx.y == 1;
     if (pre ? !c.dw_pre : !c.dw_post && !c.dscale) return;  // the whole workgroup
@@ -545,9 +556,10 @@ int threads_per_row(int n) {
 }
 int rows_per_block(int n) { return std::max(1, 256 / threads_per_row(n)); }
 
-// Workgroups, as many as are resident at once (four of 256 threads per compute
-// unit; 16384 rows of 2048 there and back 255 us, with half as many 290, with 1.5
-// times 288).  The backward's partial sums are [2][blocks][n].
+// Workgroups: four of 256 threads per compute unit, as many as are resident at once
+// (16384 rows of 2048 there and back 255 us, with half as many 290, with 1.5 times
+// 288) but for the backward of fp32 blocks, of which three are, and one of 512 threads
+// where two are launched.  The backward's partial sums are [2][blocks][n].
 int row_blocks(int64_t rows, int64_t n) {
     const int64_t rpb = rows_per_block((int)n);
     const int64_t most = 4 * kPlanCus * 256 / std::max(256, threads_per_row((int)n));

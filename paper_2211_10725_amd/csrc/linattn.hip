@@ -48,7 +48,7 @@
 // or LDS in 29 % of theirs.  fp32 is bound by the fp32 matrix instructions: 512
 // tokens of 256 heads of 64, forward and backward, 193 us; they take 63 % of the
 // forward's outputs and 74 % of the backward.  fp16 of 64 (8 x 1000 tokens of 16
-// heads, 34 us) is bound by the vector unit: 59 %, matrix cores 14 %.
+// heads, 33 us) is bound by the vector unit: 61 %, matrix cores 14 %.
 #include <type_traits>
 
 #include "snn_internal.hpp"
@@ -178,12 +178,12 @@ __device__ inline void unpack(const u32x4 &p, float (&x)[8]) {
 //
 // Of 64, a wave takes 16: the registers then hold four waves of a SIMD, with chunks of
 // 32 tokens, instead of two with 32 columns and chunks of 64 (2000 tokens of 128 heads
-// there and back: bf16 145 us against 169, fp16 172 against 175; 512 tokens of 256
-// fp32 heads 195 against 213).  Of 128 they do not: 16 while each workgroup has a
+// there and back: bf16 145 us against 169, fp16 172 against 175, now 168; 512 tokens of
+// 256 fp32 heads 195 against 213).  Of 128 they do not: 16 while each workgroup has a
 // compute unit to itself (101 tokens of 8 heads there and back: bf16 27 us against 30;
 // of 30 fp32 heads 55 against 61), else 32, which compute the scores half as often
 // (2000 tokens of 128 bf16 heads 316 against 344, 512 of 256 fp32 heads 512 against
-// 596).
+// 596, with 13 registers a lane of the fp32 outputs' kernel in scratch).
 template <typename T, int D, int N>
 struct Geo {
     static constexpr bool kHalf = sizeof(T) == 2;
