@@ -63,7 +63,7 @@
 extern "C" {
 #endif
 
-#define SNN_ABI_VERSION 13
+#define SNN_ABI_VERSION 14
 
 typedef enum snn_status {
     SNN_OK = 0,
@@ -627,6 +627,157 @@ snn_status snn_checkpoint_save(int32_t rows, int32_t n, int32_t block, int64_t l
 /* x of dtype (SNN_F32 | SNN_F16 | SNN_BF16), each value rounded once. */
 snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t ld,
                                int32_t dtype, const void *ckpt, void *x, hipStream_t stream);
+
+/* ---- selective leaky block ---------------------------------------------------
+ * Leaky integrators whose step the input chooses, with the short convolution
+ * before them and layer norm.  Row tensors are time-major and strided: element
+ * (t,b,c) lies at t stride[0] + b stride[1] + c, so they may be slices of wider
+ * projections; they need only their element's alignment, and strides are >= 0 and
+ * at most 2^32.  What is only read may be a broadcast (stride 0); of what is
+ * written no two rows may share addresses (SNN_ERR_SHAPE).  Gradients have their
+ * tensors' strides.  Arithmetic and states are fp32, each output rounded once.
+ *
+ * lens (device int32 [B], or NULL: every sequence has T tokens) gives each
+ * sequence's length, taken as within [0, T]; tokens at and past it are not read,
+ * their outputs and gradients are 0, and the state is that after the last token
+ * before it (state_in itself over no tokens).
+ *
+ * Selective scan.  Channel c of n holds `states` integrators h; with
+ * d = softplus(dt + dt_bias) (delta_softplus; else dt + dt_bias):
+ *     h_t[i,c] = exp(d_t[c] a[i,c]) h_{t-1}[i,c] + d_t[c] u_t[c] b_t[g,i]
+ *     y_t[c]   = (sum_i c_t[g,i] h_t[i,c] + skip[c] u_t[c]) silu(z_t[c])
+ * with channel c in group g = c / (n / groups).  b and c are [T,B,groups,states]
+ * with stride [time, sequence, group].  a is fp32 [states,n], meant to be negative;
+ * states of a sequence or slot are fp32 [states,n]. */
+typedef struct snn_selscan_desc {
+    int32_t T, B;           /* tokens, sequences (snn_selscan_step: T = 1) */
+    int32_t n, states;      /* channels; integrators of each, 1 .. 64 */
+    int32_t groups;         /* divides n; B groups < 2^24 */
+    int32_t dtype;          /* u, dt, z, b, c, y, their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
+    int32_t delta_softplus; /* 0 or 1 */
+    int32_t forward_only;   /* 1: no backward will follow (a prompt), which then is
+                               SNN_ERR_UNSUPPORTED, and nothing is saved for it */
+    int64_t u_stride[2], dt_stride[2], z_stride[2], y_stride[2];
+    int64_t b_stride[3], c_stride[3];
+} snn_selscan_desc;
+
+/* Bytes of the forward-to-backward state: the integrators before every 16th token.
+ * 0 for an invalid descriptor, and where it says forward_only. */
+size_t snn_selscan_saved_bytes(const snn_selscan_desc *d);
+
+/* Scratch bytes of snn_selscan_fwd and snn_selscan_bwd (the larger; of the forward
+ * alone where the descriptor says so).  0 for an invalid descriptor, and a valid
+ * answer. */
+size_t snn_selscan_workspace_bytes(const snn_selscan_desc *d);
+
+/* Whole sequences.
+ *   skip, dt_bias  fp32 [n], or NULL for zeros
+ *   z              gate, or NULL for a factor of 1
+ *   state_in       fp32 [B,states,n], or NULL for zeros
+ *   state_out      fp32 [B,states,n], or NULL; may be state_in
+ *   saved          snn_selscan_saved_bytes(d) bytes, kept for the backward; NULL
+ *                  where the descriptor says forward_only
+ * y overlaps no input.  B or n may be 0 (no work); T == 0 copies the state. */
+snn_status snn_selscan_fwd(const snn_selscan_desc *d, const void *u, const void *dt,
+                           const float *a, const void *b, const void *c, const float *skip,
+                           const float *dt_bias, const void *z, const int32_t *lens,
+                           const float *state_in, void *y, float *state_out, void *saved,
+                           void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Backward, from the forward's inputs and what it saved.
+ *   grad_y          strides of y
+ *   grad_state_out  fp32 [B,states,n], or NULL for zeros
+ *   grad_u, grad_dt, grad_b, grad_c  required, strides of u, dt, b, c; b's and c's
+ *                   are sums over the group's channels
+ *   grad_a          fp32 [states,n], grad_skip, grad_dt_bias fp32 [n]: sums over
+ *                   tokens and sequences in a fixed order, or NULL; grad_skip and
+ *                   grad_dt_bias must be where skip and dt_bias are
+ *   grad_z          required where z is, NULL otherwise
+ *   grad_state_in   fp32 [B,states,n], or NULL; may be grad_state_out
+ * No other output may overlap an input or another output. */
+snn_status snn_selscan_bwd(const snn_selscan_desc *d, const void *u, const void *dt,
+                           const float *a, const void *b, const void *c, const float *skip,
+                           const float *dt_bias, const void *z, const int32_t *lens,
+                           const void *saved, const void *grad_y,
+                           const float *grad_state_out, void *grad_u, void *grad_dt,
+                           float *grad_a, void *grad_b, void *grad_c, float *grad_skip,
+                           float *grad_dt_bias, void *grad_z, float *grad_state_in, void *ws,
+                           size_t ws_bytes, hipStream_t stream);
+
+/* One token of every running request (d->T = 1, d->B requests); slots, n_slots and
+ * the pools state_in, state_out (fp32 [n_slots,states,n], may be the same) as in
+ * snn_linattn_step. */
+snn_status snn_selscan_step(const snn_selscan_desc *d, const void *u, const void *dt,
+                            const float *a, const void *b, const void *c, const float *skip,
+                            const float *dt_bias, const void *z, const int32_t *slots,
+                            int32_t n_slots, const float *state_in, float *state_out, void *y,
+                            hipStream_t stream);
+
+/* Short causal convolution, each channel by itself:
+ *     y_t[c] = act(bias[c] + sum_{j < width} w[j,c] x_{t-width+1+j}[c])
+ * with act the identity (SNN_GATE_NONE) or SNN_GATE_SILU, w fp32 [width,n] and the
+ * state, fp32 [B,width-1,n], the last width - 1 inputs, the oldest first. */
+typedef struct snn_shortconv_desc {
+    int32_t T, B, n;        /* tokens, sequences (snn_shortconv_step: T = 1), channels */
+    int32_t width;          /* taps, 2 .. 8 */
+    int32_t act;            /* SNN_GATE_NONE | SNN_GATE_SILU */
+    int32_t dtype;          /* x, y, their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
+    int64_t x_stride[2], y_stride[2];
+} snn_shortconv_desc;
+
+/* Scratch bytes of snn_shortconv_bwd. */
+size_t snn_shortconv_workspace_bytes(const snn_shortconv_desc *d);
+
+/* Whole sequences.  bias fp32 [n] or NULL; state_in (NULL: zeros) and state_out
+ * (NULL: not wanted) fp32 [B,width-1,n], which may be the same.  y overlaps no
+ * input. */
+snn_status snn_shortconv_fwd(const snn_shortconv_desc *d, const void *x, const float *w,
+                             const float *bias, const int32_t *lens, const float *state_in,
+                             void *y, float *state_out, hipStream_t stream);
+
+/* Backward.  grad_y has y's strides; grad_state_out fp32 [B,width-1,n] or NULL for
+ * zeros; grad_x (x's strides) is required; grad_w fp32 [width,n] and grad_bias fp32
+ * [n] (sums over tokens and sequences in a fixed order) and grad_state_in (not
+ * grad_state_out: SNN_ERR_UNSUPPORTED) may be NULL.  No output may overlap an input
+ * or another output. */
+snn_status snn_shortconv_bwd(const snn_shortconv_desc *d, const void *x, const float *w,
+                             const float *bias, const int32_t *lens, const float *state_in,
+                             const void *grad_y, const float *grad_state_out, void *grad_x,
+                             float *grad_w, float *grad_bias, float *grad_state_in, void *ws,
+                             size_t ws_bytes, hipStream_t stream);
+
+/* One token of every running request; slots, n_slots and the pools (fp32
+ * [n_slots,width-1,n], may be the same) as in snn_linattn_step. */
+snn_status snn_shortconv_step(const snn_shortconv_desc *d, const void *x, const float *w,
+                              const float *bias, const int32_t *slots, int32_t n_slots,
+                              const float *state_in, float *state_out, void *y,
+                              hipStream_t stream);
+
+/* Layer norm, per row of n values:
+ *     y = (x - mean) / sqrt(mean((x - mean)^2) + eps) w + b */
+typedef struct snn_layer_norm_desc {
+    int32_t rows, n;        /* n 1 .. 16384 */
+    int32_t x_dtype;        /* x, grad_x, grad_res: SNN_F32, or y_dtype */
+    int32_t y_dtype;        /* y, grad_y: SNN_F32 | SNN_F16 | SNN_BF16 */
+    float eps;              /* > 0 */
+    int64_t ld_x, ld_y;     /* row strides, >= n, of x, grad_x and grad_res; of y and grad_y */
+} snn_layer_norm_desc;
+
+/* Scratch bytes of snn_layer_norm_bwd. */
+size_t snn_layer_norm_workspace_bytes(const snn_layer_norm_desc *d);
+
+/* w, b: fp32 [n], or NULL for ones and zeros.  y may be x where both have one type
+ * and row stride. */
+snn_status snn_layer_norm_fwd(const snn_layer_norm_desc *d, const void *x, const float *w,
+                              const float *b, void *y, hipStream_t stream);
+
+/* Backward: grad_x = grad_res + the norm's gradient, its statistics taken from x
+ * again.  grad_res (the gradient that reaches x past the norm) may be NULL, or
+ * grad_x.  grad_w, grad_b (fp32 [n], sums over the rows in a fixed order) may be
+ * NULL.  ws: as queried. */
+snn_status snn_layer_norm_bwd(const snn_layer_norm_desc *d, const void *x, const void *grad_y,
+                              const void *grad_res, const float *w, void *grad_x, float *grad_w,
+                              float *grad_b, void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

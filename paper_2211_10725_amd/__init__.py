@@ -32,7 +32,7 @@ RESET_DETACHED, RESET_SURROGATE = 0, 1
 GRAD_FULL, GRAD_BCAST, GRAD_FOLD = 0, 1, 2
 LOSS_CE_COUNT, LOSS_MSE_COUNT = 0, 1
 FLAG_FP32_MFMA = 1
-ABI_VERSION = 13
+ABI_VERSION = 14
 DCUR_T_TRANSPOSED, DCUR_T_PLANES = 1, 2
 GATE_NONE, GATE_MUL, GATE_SIGMOID, GATE_SILU = 0, 1, 2, 3
 
@@ -49,7 +49,11 @@ EXPORTS = ["snn_abi_version", "snn_status_str", "snn_layer_saved_bytes",
            "snn_linattn_workspace_bytes", "snn_linattn_fwd", "snn_linattn_bwd",
            "snn_linattn_step", "snn_gate_norm_workspace_bytes", "snn_gate_norm_fwd",
            "snn_gate_norm_bwd", "snn_checkpoint_bytes", "snn_checkpoint_save",
-           "snn_checkpoint_load"]
+           "snn_checkpoint_load", "snn_selscan_saved_bytes", "snn_selscan_workspace_bytes",
+           "snn_selscan_fwd", "snn_selscan_bwd", "snn_selscan_step",
+           "snn_shortconv_workspace_bytes", "snn_shortconv_fwd", "snn_shortconv_bwd",
+           "snn_shortconv_step", "snn_layer_norm_workspace_bytes", "snn_layer_norm_fwd",
+           "snn_layer_norm_bwd"]
 
 
 class LayerDesc(ctypes.Structure):
@@ -119,6 +123,28 @@ class GateNormDesc(ctypes.Structure):
                 ("ld_y", ctypes.c_int64), ("ld_g", ctypes.c_int64), ("ld_h", ctypes.c_int64)]
 
 
+class SelscanDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("states", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("delta_softplus", ctypes.c_int32),
+                ("forward_only", ctypes.c_int32), ("u_stride", ctypes.c_int64 * 2),
+                ("dt_stride", ctypes.c_int64 * 2), ("z_stride", ctypes.c_int64 * 2),
+                ("y_stride", ctypes.c_int64 * 2), ("b_stride", ctypes.c_int64 * 3),
+                ("c_stride", ctypes.c_int64 * 3)]
+
+
+class ShortconvDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("n", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64 * 2), ("y_stride", ctypes.c_int64 * 2)]
+
+
+class LayerNormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("n", ctypes.c_int32), ("x_dtype", ctypes.c_int32),
+                ("y_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("ld_x", ctypes.c_int64),
+                ("ld_y", ctypes.c_int64)]
+
+
 class SNNError(RuntimeError):
     def __init__(self, fn, status):
         self.status = status
@@ -142,6 +168,7 @@ def lib():
     G = ctypes.POINTER(GradIn)
     i32, i64 = ctypes.c_int32, ctypes.c_int64
     LA, GN = ctypes.POINTER(LinattnDesc), ctypes.POINTER(GateNormDesc)
+    SS, SC, LN = (ctypes.POINTER(d) for d in (SelscanDesc, ShortconvDesc, LayerNormDesc))
     sig = {
         "snn_abi_version": ([], ctypes.c_int),
         "snn_status_str": ([ctypes.c_int], ctypes.c_char_p),
@@ -174,6 +201,18 @@ def lib():
         "snn_checkpoint_bytes": ([i32, i32, i32], S),
         "snn_checkpoint_save": ([i32, i32, i32, i64, i32, P, P, P], ctypes.c_int),
         "snn_checkpoint_load": ([i32, i32, i32, i64, i32, P, P, P], ctypes.c_int),
+        "snn_selscan_saved_bytes": ([SS], S),
+        "snn_selscan_workspace_bytes": ([SS], S),
+        "snn_selscan_fwd": ([SS] + [P] * 14 + [S, P], ctypes.c_int),
+        "snn_selscan_bwd": ([SS] + [P] * 22 + [S, P], ctypes.c_int),
+        "snn_selscan_step": ([SS] + [P] * 9 + [i32] + [P] * 4, ctypes.c_int),
+        "snn_shortconv_workspace_bytes": ([SC], S),
+        "snn_shortconv_fwd": ([SC] + [P] * 8, ctypes.c_int),
+        "snn_shortconv_bwd": ([SC] + [P] * 12 + [S, P], ctypes.c_int),
+        "snn_shortconv_step": ([SC] + [P] * 4 + [i32] + [P] * 4, ctypes.c_int),
+        "snn_layer_norm_workspace_bytes": ([LN], S),
+        "snn_layer_norm_fwd": ([LN] + [P] * 5, ctypes.c_int),
+        "snn_layer_norm_bwd": ([LN] + [P] * 8 + [S, P], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -706,6 +745,232 @@ def snn_checkpoint_save(x, ckpt, block=128, stream=None):
 def snn_checkpoint_load(ckpt, x, block=128, stream=None):
     """Reads the checkpoint of x's shape back into x (any of its dtypes)."""
     _checkpoint("snn_checkpoint_load", x, ckpt, block, (_p(ckpt), _p(x)), stream)
+
+
+# --------------------------------------------------------------------------
+# selective leaky block
+# --------------------------------------------------------------------------
+def _strides(fn, t, dims):
+    """Strides of the leading `dims` dimensions of a tensor whose last is contiguous
+    (0 for a dimension of one element: it has none to speak of)."""
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{fn}: a row's values must be contiguous")
+    st = [s if n > 1 and t.numel() else 0 for n, s in zip(t.shape[:dims], t.stride())]
+    return (ctypes.c_int64 * dims)(*st)
+
+
+def _need_strided(fn, what, t, code, shape, stride):
+    """A strided argument of the shape, type and strides the descriptor has."""
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype is _torch_dtype(code) and t.shape == shape:
+        st = t.stride()
+        if not t.numel() or (st[-1] == 1 or shape[-1] == 1) and all(
+                n == 1 or a == b for n, a, b in zip(shape, st, stride)):
+            return
+    raise ValueError(f"{fn}: {what} {tuple(t.shape)} {t.dtype} with strides {t.stride()} is not "
+                     "what the descriptor says")
+
+
+def selscan_desc(u, dt, b, c, y, z=None, delta_softplus=True, forward_only=False) -> SelscanDesc:
+    """Descriptor of a selective scan over u, dt, y and the gate z (or None) [T,B,n],
+    b and c [T,B,groups,states]: tensors of one dtype, each row contiguous, strided over
+    time, sequence and group (forward_only: for prompts and steps, for which nothing is
+    saved).  Later calls may pass other tensors of the same shapes and strides."""
+    fn = "selscan_desc"
+    T, B, n = u.shape
+    if any(t is not None and t.shape != u.shape for t in (dt, y, z)) or b.dim() != 4 or \
+            b.shape[:2] != (T, B) or c.shape != b.shape:
+        raise ValueError(f"{fn}: shapes {[tuple(t.shape) for t in (u, dt, b, c, y)]} do not go "
+                         "together")
+    if any(t is not None and t.dtype != u.dtype for t in (dt, b, c, y, z)):
+        raise ValueError(f"{fn}: u, dt, b, c, y and z must have one dtype")
+    return SelscanDesc(T, B, n, b.shape[3], b.shape[2], _dtype_code(u), int(delta_softplus),
+                       int(forward_only), *(_strides(fn, t, 2) for t in (u, dt)),
+                       _strides(fn, z if z is not None else u, 2), _strides(fn, y, 2),
+                       _strides(fn, b, 3), _strides(fn, c, 3))
+
+
+def snn_selscan_saved_bytes(desc: SelscanDesc) -> int:
+    return int(lib().snn_selscan_saved_bytes(ctypes.byref(desc)))
+
+
+def snn_selscan_workspace_bytes(desc: SelscanDesc) -> int:
+    return int(lib().snn_selscan_workspace_bytes(ctypes.byref(desc)))
+
+
+def _need_selscan(fn, d, u, dt, a, b, c, skip, dt_bias, z, y, prefix=""):
+    rows, vecs = (d.T, d.B, d.n), (d.T, d.B, d.groups, d.states)
+    for what, t, st in (("u", u, d.u_stride), ("dt", dt, d.dt_stride), ("z", z, d.z_stride)):
+        _need_strided(fn, prefix + what, t, d.dtype, rows, st)
+    _need_strided(fn, "y or its gradient", y, d.dtype, rows, d.y_stride)
+    _need_strided(fn, prefix + "b", b, d.dtype, vecs, d.b_stride)
+    _need_strided(fn, prefix + "c", c, d.dtype, vecs, d.c_stride)
+    _need_array(fn, a, F32, d.states * d.n, prefix + "a")
+    _need_array(fn, skip, F32, d.n, prefix + "skip")
+    _need_array(fn, dt_bias, F32, d.n, prefix + "dt_bias")
+
+
+def _need_bytes(fn, t, need, what):
+    if t is None or isinstance(t, int):
+        return
+    if not t.is_contiguous() or _nbytes(t) < need:
+        raise ValueError(f"{fn}: {what} needs {need} contiguous bytes")
+
+
+def snn_selscan_fwd(desc, u, dt, a, b, c, skip, dt_bias, z, lens, state_in, y, state_out, saved,
+                    ws, stream=None):
+    """Whole sequences: y and, where given, the states after each (from state_in, or
+    zeros); saved (snn_selscan_saved_bytes) is for the backward.  lens: int32 [B] lengths,
+    or None."""
+    fn, d = "snn_selscan_fwd", desc
+    _need_selscan(fn, d, u, dt, a, b, c, skip, dt_bias, z, y)
+    _need_array(fn, lens, I32, d.B, "lens")
+    for what, t in (("state_in", state_in), ("state_out", state_out)):
+        _need_array(fn, t, F32, d.B * d.states * d.n, what)
+    if saved is not None:
+        _need_bytes(fn, saved, snn_selscan_saved_bytes(d), "saved")
+    _check(fn, lib().snn_selscan_fwd(
+        ctypes.byref(d), _p(u), _p(dt), _p(a), _p(b), _p(c), _p(skip), _p(dt_bias), _p(z),
+        _p(lens), _p(state_in), _p(y), _p(state_out), _p(saved), _p(ws), _nbytes(ws),
+        _stream(stream)))
+
+
+def snn_selscan_bwd(desc, u, dt, a, b, c, skip, dt_bias, z, lens, saved, grad_y, grad_state_out,
+                    grad_u, grad_dt, grad_a, grad_b, grad_c, grad_skip, grad_dt_bias, grad_z,
+                    grad_state_in, ws, stream=None):
+    fn, d = "snn_selscan_bwd", desc
+    _need_selscan(fn, d, u, dt, a, b, c, skip, dt_bias, z, grad_y)
+    _need_selscan(fn, d, grad_u, grad_dt, grad_a, grad_b, grad_c, grad_skip, grad_dt_bias, grad_z,
+                  None, "grad_")
+    _need_array(fn, lens, I32, d.B, "lens")
+    for what, t in (("grad_state_out", grad_state_out), ("grad_state_in", grad_state_in)):
+        _need_array(fn, t, F32, d.B * d.states * d.n, what)
+    _need_bytes(fn, saved, snn_selscan_saved_bytes(d), "saved")
+    _check(fn, lib().snn_selscan_bwd(
+        ctypes.byref(d), _p(u), _p(dt), _p(a), _p(b), _p(c), _p(skip), _p(dt_bias), _p(z),
+        _p(lens), _p(saved), _p(grad_y), _p(grad_state_out), _p(grad_u), _p(grad_dt), _p(grad_a),
+        _p(grad_b), _p(grad_c), _p(grad_skip), _p(grad_dt_bias), _p(grad_z), _p(grad_state_in),
+        _p(ws), _nbytes(ws), _stream(stream)))
+
+
+def snn_selscan_step(desc, u, dt, a, b, c, skip, dt_bias, z, slots, state_in, state_out, y,
+                     stream=None):
+    """One token of every request; states [n_slots, states, n] in pools (one and the same
+    for an update in place), slots int32 [B] or None."""
+    fn, d, n_slots = "snn_selscan_step", desc, state_in.shape[0]
+    _need_selscan(fn, d, u, dt, a, b, c, skip, dt_bias, z, y)
+    _need_array(fn, slots, I32, d.B, "slots")
+    for what, t in (("state_in", state_in), ("state_out", state_out)):
+        _need_array(fn, t, F32, n_slots * d.states * d.n, what)
+    _check(fn, lib().snn_selscan_step(
+        ctypes.byref(d), _p(u), _p(dt), _p(a), _p(b), _p(c), _p(skip), _p(dt_bias), _p(z),
+        _p(slots), n_slots, _p(state_in), _p(state_out), _p(y), _stream(stream)))
+
+
+def shortconv_desc(x, y, width, act="none") -> ShortconvDesc:
+    """Descriptor of the short causal convolution of x into y [T,B,n], each row contiguous,
+    strided over time and sequence, with `width` taps and act "none" or "silu".  Later
+    calls may pass other tensors of the same shapes and strides."""
+    fn = "shortconv_desc"
+    if x.dim() != 3 or x.shape != y.shape or x.dtype != y.dtype:
+        raise ValueError(f"{fn}: {tuple(x.shape)} {x.dtype} and {tuple(y.shape)} {y.dtype} do "
+                         "not go together")
+    return ShortconvDesc(*x.shape, width, _GATE[act], _dtype_code(x), _strides(fn, x, 2),
+                         _strides(fn, y, 2))
+
+
+def snn_shortconv_workspace_bytes(desc: ShortconvDesc) -> int:
+    return int(lib().snn_shortconv_workspace_bytes(ctypes.byref(desc)))
+
+
+def _need_shortconv(fn, d, x, w, bias, y, prefix=""):
+    rows = (d.T, d.B, d.n)
+    _need_strided(fn, prefix + "x", x, d.dtype, rows, d.x_stride)
+    _need_strided(fn, "y or its gradient", y, d.dtype, rows, d.y_stride)
+    _need_array(fn, w, F32, d.width * d.n, prefix + "w")
+    _need_array(fn, bias, F32, d.n, prefix + "bias")
+
+
+def snn_shortconv_fwd(desc, x, w, bias, lens, state_in, y, state_out, stream=None):
+    """Whole sequences: y and, where given, the last width - 1 inputs (after those of
+    state_in, or zeros), fp32 [B, width - 1, n].  lens: int32 [B] lengths, or None."""
+    fn, d = "snn_shortconv_fwd", desc
+    _need_shortconv(fn, d, x, w, bias, y)
+    _need_array(fn, lens, I32, d.B, "lens")
+    for what, t in (("state_in", state_in), ("state_out", state_out)):
+        _need_array(fn, t, F32, d.B * (d.width - 1) * d.n, what)
+    _check(fn, lib().snn_shortconv_fwd(
+        ctypes.byref(d), _p(x), _p(w), _p(bias), _p(lens), _p(state_in), _p(y), _p(state_out),
+        _stream(stream)))
+
+
+def snn_shortconv_bwd(desc, x, w, bias, lens, state_in, grad_y, grad_state_out, grad_x, grad_w,
+                      grad_bias, grad_state_in, ws, stream=None):
+    fn, d = "snn_shortconv_bwd", desc
+    _need_shortconv(fn, d, x, w, bias, grad_y)
+    _need_shortconv(fn, d, grad_x, grad_w, grad_bias, None, "grad_")
+    _need_array(fn, lens, I32, d.B, "lens")
+    for what, t in (("state_in", state_in), ("grad_state_out", grad_state_out),
+                    ("grad_state_in", grad_state_in)):
+        _need_array(fn, t, F32, d.B * (d.width - 1) * d.n, what)
+    _check(fn, lib().snn_shortconv_bwd(
+        ctypes.byref(d), _p(x), _p(w), _p(bias), _p(lens), _p(state_in), _p(grad_y),
+        _p(grad_state_out), _p(grad_x), _p(grad_w), _p(grad_bias), _p(grad_state_in), _p(ws),
+        _nbytes(ws), _stream(stream)))
+
+
+def snn_shortconv_step(desc, x, w, bias, slots, state_in, state_out, y, stream=None):
+    """One token of every request; the last inputs [n_slots, width - 1, n] in pools (one
+    and the same for an update in place), slots int32 [B] or None."""
+    fn, d, n_slots = "snn_shortconv_step", desc, state_in.shape[0]
+    _need_shortconv(fn, d, x, w, bias, y)
+    _need_array(fn, slots, I32, d.B, "slots")
+    for what, t in (("state_in", state_in), ("state_out", state_out)):
+        _need_array(fn, t, F32, n_slots * (d.width - 1) * d.n, what)
+    _check(fn, lib().snn_shortconv_step(
+        ctypes.byref(d), _p(x), _p(w), _p(bias), _p(slots), n_slots, _p(state_in),
+        _p(state_out), _p(y), _stream(stream)))
+
+
+def layer_norm_desc(x, y=None, eps=1e-5) -> LayerNormDesc:
+    """Descriptor of a layer norm of the rows of x [..., n] into y (contiguous rows of x's
+    dtype if None).  Later calls may pass other tensors of the same strides."""
+    n = x.shape[-1]
+    if y is not None and y.shape != x.shape:
+        raise ValueError(f"layer_norm_desc: shapes {tuple(x.shape)} and {tuple(y.shape)}")
+    return LayerNormDesc(x.numel() // n if n else 0, n, _dtype_code(x),
+                         _dtype_code(x if y is None else y), eps, _row_stride(x),
+                         n if y is None else _row_stride(y))
+
+
+def snn_layer_norm_workspace_bytes(desc: LayerNormDesc) -> int:
+    return int(lib().snn_layer_norm_workspace_bytes(ctypes.byref(desc)))
+
+
+def snn_layer_norm_fwd(desc, x, w, b, y, stream=None):
+    """y = (x - mean) / sqrt(var + eps) w + b over each row (w, b: None for ones, zeros)."""
+    fn, d = "snn_layer_norm_fwd", desc
+    _need_rows(fn, "x", x, d, _torch_dtype(d.x_dtype), d.ld_x)
+    _need_rows(fn, "y", y, d, _torch_dtype(d.y_dtype), d.ld_y)
+    _need_array(fn, w, F32, d.n, "w")
+    _need_array(fn, b, F32, d.n, "b")
+    _check(fn, lib().snn_layer_norm_fwd(ctypes.byref(d), _p(x), _p(w), _p(b), _p(y),
+                                        _stream(stream)))
+
+
+def snn_layer_norm_bwd(desc, x, grad_y, grad_res, w, grad_x, grad_w, grad_b, ws, stream=None):
+    """grad_x = grad_res (or None) + the norm's gradient; grad_w, grad_b sums over rows."""
+    fn, d = "snn_layer_norm_bwd", desc
+    xt = _torch_dtype(d.x_dtype)
+    for what, t in (("x", x), ("grad_res", grad_res), ("grad_x", grad_x)):
+        _need_rows(fn, what, t, d, xt, d.ld_x)
+    _need_rows(fn, "grad_y", grad_y, d, _torch_dtype(d.y_dtype), d.ld_y)
+    for what, t in (("w", w), ("grad_w", grad_w), ("grad_b", grad_b)):
+        _need_array(fn, t, F32, d.n, what)
+    _check(fn, lib().snn_layer_norm_bwd(
+        ctypes.byref(d), _p(x), _p(grad_y), _p(grad_res), _p(w), _p(grad_x), _p(grad_w),
+        _p(grad_b), _p(ws), _nbytes(ws), _stream(stream)))
 
 
 # --------------------------------------------------------------------------

@@ -1275,3 +1275,372 @@ snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t l
 }
 
 }  // extern "C"
+
+// ---- selective leaky block -----------------------------------------------------
+
+namespace {
+
+// lengths whose launches have fewer than 2^32 threads and whose offsets stay far
+// inside 63 bits
+constexpr int64_t kMostStride = (int64_t)1 << 32, kMostBlocks = (int64_t)1 << 24;
+
+bool strides_valid(const int64_t *st, int count) {
+    for (int i = 0; i < count; ++i)
+        if (st[i] < 0 || st[i] > kMostStride) return false;
+    return true;
+}
+
+// Whether rows of `width` values at the strides surely share addresses (rows_overlap).
+bool strided_overlap(std::initializer_list<int64_t> sizes, const int64_t *st, int64_t width) {
+    const int64_t *n = sizes.begin();
+    const int dims = (int)sizes.size();
+    for (int i = 0; i < dims; ++i) {
+        if (n[i] == 0) return false;
+    }
+    for (int i = 0; i < dims; ++i) {
+        if (n[i] < 2) continue;
+        if (st[i] < width) return true;
+        for (int j = 0; j < dims; ++j) {
+            if (j == i || n[j] < 2 || st[j] < st[i]) continue;
+            const int64_t a = st[j] / st[i];
+            if ((a < n[i] && st[j] - a * st[i] < width) ||
+                (a + 1 < n[i] && (a + 1) * st[i] - st[j] < width))
+                return true;
+        }
+    }
+    return false;
+}
+
+snn_status check_selscan(const snn_selscan_desc *d) {
+    if (!d) return SNN_ERR_NULL;
+    if (d->T < 0 || d->B < 0 || d->n < 0 || d->states < 1 || d->states > kSelscanMaxStates ||
+        d->groups < 1 || d->n % d->groups != 0)
+        return SNN_ERR_SHAPE;
+    if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
+    if ((d->delta_softplus != 0 && d->delta_softplus != 1) ||
+        (d->forward_only != 0 && d->forward_only != 1))
+        return SNN_ERR_UNSUPPORTED;
+    for (const int64_t *st : {d->u_stride, d->dt_stride, d->z_stride, d->y_stride})
+        if (!strides_valid(st, 2)) return SNN_ERR_SHAPE;
+    if (!strides_valid(d->b_stride, 3) || !strides_valid(d->c_stride, 3)) return SNN_ERR_SHAPE;
+    if (d->n == 0) return SNN_OK;
+    const int64_t vec = (int64_t)d->groups * d->states, row = (int64_t)d->n * (d->states + 2);
+    if (d->T > ((int32_t)1 << 30) || (int64_t)d->B * selscan_tiles(d->n, d->groups) >= kMostBlocks ||
+        row >= ((int64_t)1 << 31) || (int64_t)d->B * row >= ((int64_t)1 << 32) ||
+        (d->T > 0 && (int64_t)d->T * d->B > ((int64_t)1 << 31) / vec))
+        return SNN_ERR_SHAPE;
+    return SNN_OK;
+}
+
+int64_t selscan_units(const snn_selscan_desc *d) {
+    return (int64_t)d->B * selscan_tiles(d->n, d->groups);
+}
+
+// workspace: segments' states and sums of steps, then (backward) the partial sums
+struct SelscanRoom {
+    size_t slot, sums, vec, part;
+    size_t forward() const { return slot + sums; }
+    size_t all() const { return slot + sums + vec + part; }
+};
+SelscanRoom selscan_room(const snn_selscan_desc *d) {
+    SelscanRoom r{};
+    if (d->n == 0 || d->B == 0) return r;
+    const SelscanPlan p = selscan_plan(d->T, selscan_units(d));
+    const size_t row = (size_t)d->B * d->n * sizeof(float);
+    if (p.segs > 1) {
+        r.slot = align_up((size_t)p.segs * d->states * row);
+        r.sums = align_up((size_t)p.segs * row);
+    }
+    if (!d->forward_only) {
+        r.vec = align_up((size_t)2 * (selscan_tiles(d->n, d->groups) / d->groups) * d->T * d->B *
+                         d->groups * d->states * sizeof(float));
+        r.part = align_up((size_t)p.segs * (d->states + 2) * row);
+    }
+    return r;
+}
+
+SelscanRows rows_of(const void *p, const int64_t *st) { return SelscanRows{p, st[0], st[1]}; }
+SelscanVec vec_of(const void *p, const int64_t *st) {
+    return SelscanVec{p, st[0], st[1], st[2]};
+}
+
+Selscan selscan_args(const snn_selscan_desc *d, const void *u, const void *dt, const float *a,
+                     const void *b, const void *c, const float *skip, const float *dt_bias,
+                     const void *z, const int32_t *lens) {
+    Selscan s{};
+    s.T = d->T, s.B = d->B, s.n = d->n, s.N = d->states, s.groups = d->groups;
+    s.softplus = d->delta_softplus;
+    s.tiles = selscan_tiles(d->n, d->groups);
+    const SelscanPlan p = selscan_plan(d->T, selscan_units(d));
+    s.segs = p.segs, s.seg_len = p.seg_len;
+    s.lens = lens;
+    s.u = rows_of(u, d->u_stride), s.dt = rows_of(dt, d->dt_stride), s.z = rows_of(z, d->z_stride);
+    s.b = vec_of(b, d->b_stride), s.c = vec_of(c, d->c_stride);
+    s.a = a, s.skip = skip, s.dt_bias = dt_bias;
+    s.y_st = d->y_stride[0], s.y_sb = d->y_stride[1];
+    return s;
+}
+
+snn_status check_shortconv(const snn_shortconv_desc *d) {
+    if (!d) return SNN_ERR_NULL;
+    if (d->T < 0 || d->B < 0 || d->n < 0 || d->width < 2 || d->width > 8) return SNN_ERR_SHAPE;
+    if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
+    if (d->act != SNN_GATE_NONE && d->act != SNN_GATE_SILU) return SNN_ERR_UNSUPPORTED;
+    if (!strides_valid(d->x_stride, 2) || !strides_valid(d->y_stride, 2)) return SNN_ERR_SHAPE;
+    // workgroups of 256 threads for 256 channels and 32 tokens or more
+    if (d->T > ((int32_t)1 << 30) ||
+        ((int64_t)d->n + 255) / 256 * d->B > (kMostBlocks - 1) / (d->T / 32 + 1))
+        return SNN_ERR_SHAPE;
+    return SNN_OK;
+}
+
+Shortconv shortconv_args(const snn_shortconv_desc *d, const void *x, const float *w,
+                         const float *bias, const int32_t *lens, const float *state_in) {
+    Shortconv a{};
+    a.T = d->T, a.B = d->B, a.n = d->n, a.silu = d->act == SNN_GATE_SILU;
+    a.lens = lens;
+    a.x = rows_of(x, d->x_stride);
+    a.w = w, a.bias = bias, a.state_in = state_in;
+    a.y_st = d->y_stride[0], a.y_sb = d->y_stride[1];
+    return a;
+}
+
+snn_status check_layer_norm(const snn_layer_norm_desc *d) {
+    if (!d) return SNN_ERR_NULL;
+    if (d->rows < 0 || d->n < 1 || d->n > kLayerNormMaxN) return SNN_ERR_SHAPE;
+    if (!float_dtype(d->y_dtype) || (d->x_dtype != SNN_F32 && d->x_dtype != d->y_dtype))
+        return SNN_ERR_DTYPE;
+    if (!finite(d->eps) || !(d->eps > 0.f)) return SNN_ERR_SHAPE;
+    if (d->ld_x < d->n || d->ld_x > kMostStride || d->ld_y < d->n || d->ld_y > kMostStride)
+        return SNN_ERR_SHAPE;
+    return SNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t snn_selscan_saved_bytes(const snn_selscan_desc *d) {
+    if (check_selscan(d) != SNN_OK || d->forward_only) return 0;
+    const size_t tiles = ((size_t)d->T + kSelscanTile - 1) / kSelscanTile;
+    return align_up(tiles * d->B * d->states * d->n * sizeof(float));
+}
+
+size_t snn_selscan_workspace_bytes(const snn_selscan_desc *d) {
+    if (check_selscan(d) != SNN_OK) return 0;
+    return selscan_room(d).all();
+}
+
+snn_status snn_selscan_fwd(const snn_selscan_desc *d, const void *u, const void *dt,
+                           const float *a, const void *b, const void *c, const float *skip,
+                           const float *dt_bias, const void *z, const int32_t *lens,
+                           const float *state_in, void *y, float *state_out, void *saved,
+                           void *ws, size_t ws_bytes, hipStream_t stream) {
+    const snn_status st = check_selscan(d);
+    if (st != SNN_OK) return st;
+    if (d->B == 0 || d->n == 0) return SNN_OK;
+    if (strided_overlap({d->T, d->B}, d->y_stride, d->n)) return SNN_ERR_SHAPE;
+    if (d->forward_only && saved) return SNN_ERR_UNSUPPORTED;
+    if (!a || (d->T > 0 && (!u || !dt || !b || !c || !y || (!d->forward_only && !saved))))
+        return SNN_ERR_NULL;
+    if (any_misaligned({a, skip, dt_bias, lens, state_in, state_out, saved, ws}) ||
+        any_misaligned_rows(d->dtype, {u, dt, b, c, z, y}))
+        return SNN_ERR_ALIGN;
+    const SelscanRoom room = selscan_room(d);
+    if (ws_bytes < room.all() || (room.all() > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    Selscan s = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, lens);
+    s.state_in = state_in;
+    s.y = y;
+    s.state_out = state_out;
+    s.saved = (float *)saved;
+    s.slot = (float *)ws;
+    s.sums = (float *)((char *)ws + room.slot);
+    (void)hipGetLastError();
+    return hip_status(launch_selscan(s, d->dtype, stream));
+}
+
+snn_status snn_selscan_bwd(const snn_selscan_desc *d, const void *u, const void *dt,
+                           const float *a, const void *b, const void *c, const float *skip,
+                           const float *dt_bias, const void *z, const int32_t *lens,
+                           const void *saved, const void *grad_y, const float *grad_state_out,
+                           void *grad_u, void *grad_dt, float *grad_a, void *grad_b, void *grad_c,
+                           float *grad_skip, float *grad_dt_bias, void *grad_z,
+                           float *grad_state_in, void *ws, size_t ws_bytes, hipStream_t stream) {
+    const snn_status st = check_selscan(d);
+    if (st != SNN_OK) return st;
+    if (d->forward_only) return SNN_ERR_UNSUPPORTED;
+    if ((grad_skip && !skip) || (grad_dt_bias && !dt_bias) || (grad_z && !z))
+        return SNN_ERR_UNSUPPORTED;
+    if (d->n == 0) return SNN_OK;
+    if (strided_overlap({d->T, d->B}, d->u_stride, d->n) ||
+        strided_overlap({d->T, d->B}, d->dt_stride, d->n) ||
+        (z && strided_overlap({d->T, d->B}, d->z_stride, d->n)) ||
+        strided_overlap({d->T, d->B, d->groups}, d->b_stride, d->states) ||
+        strided_overlap({d->T, d->B, d->groups}, d->c_stride, d->states))
+        return SNN_ERR_SHAPE;
+    // over no sequences the sums are 0
+    if (d->B > 0 && (!a || (d->T > 0 && (!u || !dt || !b || !c || !saved || !grad_y || !grad_u ||
+                                         !grad_dt || !grad_b || !grad_c || (z && !grad_z)))))
+        return SNN_ERR_NULL;
+    if (any_misaligned({a, skip, dt_bias, lens, saved, grad_state_out, grad_a, grad_skip,
+                        grad_dt_bias, grad_state_in, ws}) ||
+        any_misaligned_rows(d->dtype, {u, dt, b, c, z, grad_y, grad_u, grad_dt, grad_b, grad_c,
+                                       grad_z}))
+        return SNN_ERR_ALIGN;
+    const SelscanRoom room = selscan_room(d);
+    if (ws_bytes < room.all() || (room.all() > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    SelscanBwd q{};
+    q.a = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, lens);
+    q.gy = grad_y;
+    q.saved = (const float *)saved;
+    q.grad_state_out = grad_state_out;
+    q.du = rows_of(grad_u, d->u_stride), q.ddt = rows_of(grad_dt, d->dt_stride);
+    q.dz = rows_of(grad_z, d->z_stride);
+    q.db = vec_of(grad_b, d->b_stride), q.dc = vec_of(grad_c, d->c_stride);
+    q.grad_a = grad_a, q.grad_skip = grad_skip, q.grad_dt_bias = grad_dt_bias;
+    q.grad_state_in = grad_state_in;
+    char *at = (char *)ws;
+    q.a.slot = (float *)at;
+    q.a.sums = (float *)(at + room.slot);
+    q.vec = (float *)(at + room.slot + room.sums);
+    q.part = (float *)(at + room.slot + room.sums + room.vec);
+    (void)hipGetLastError();
+    return hip_status(launch_selscan_bwd(q, d->dtype, stream));
+}
+
+snn_status snn_selscan_step(const snn_selscan_desc *d, const void *u, const void *dt,
+                            const float *a, const void *b, const void *c, const float *skip,
+                            const float *dt_bias, const void *z, const int32_t *slots,
+                            int32_t n_slots, const float *state_in, float *state_out, void *y,
+                            hipStream_t stream) {
+    const snn_status st = check_selscan(d);
+    if (st != SNN_OK) return st;
+    if (d->T != 1 || n_slots < 0 || (!slots && n_slots < d->B)) return SNN_ERR_SHAPE;
+    if (d->B == 0 || d->n == 0) return SNN_OK;
+    if (strided_overlap({d->T, d->B}, d->y_stride, d->n)) return SNN_ERR_SHAPE;
+    if (!u || !dt || !a || !b || !c || !state_in || !state_out || !y) return SNN_ERR_NULL;
+    if (any_misaligned({a, skip, dt_bias, slots, state_in, state_out}) ||
+        any_misaligned_rows(d->dtype, {u, dt, b, c, z, y}))
+        return SNN_ERR_ALIGN;
+    Selscan s = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, nullptr);
+    s.state_in = state_in;
+    s.state_out = state_out;
+    s.y = y;
+    (void)hipGetLastError();
+    return hip_status(launch_selscan_step(s, slots, n_slots, d->dtype, stream));
+}
+
+size_t snn_shortconv_workspace_bytes(const snn_shortconv_desc *d) {
+    if (check_shortconv(d) != SNN_OK || d->B == 0 || d->n == 0) return 0;
+    return shortconv_workspace_bytes(d->T, d->B, d->n, d->width);
+}
+
+snn_status snn_shortconv_fwd(const snn_shortconv_desc *d, const void *x, const float *w,
+                             const float *bias, const int32_t *lens, const float *state_in,
+                             void *y, float *state_out, hipStream_t stream) {
+    const snn_status st = check_shortconv(d);
+    if (st != SNN_OK) return st;
+    if (d->B == 0 || d->n == 0) return SNN_OK;
+    if (strided_overlap({d->T, d->B}, d->y_stride, d->n)) return SNN_ERR_SHAPE;
+    if (!w || (d->T > 0 && (!x || !y))) return SNN_ERR_NULL;
+    if (any_misaligned({w, bias, lens, state_in, state_out}) ||
+        any_misaligned_rows(d->dtype, {x, y}))
+        return SNN_ERR_ALIGN;
+    Shortconv a = shortconv_args(d, x, w, bias, lens, state_in);
+    a.y = y;
+    a.state_out = state_out;
+    (void)hipGetLastError();
+    return hip_status(launch_shortconv(a, d->width, d->dtype, stream));
+}
+
+snn_status snn_shortconv_bwd(const snn_shortconv_desc *d, const void *x, const float *w,
+                             const float *bias, const int32_t *lens, const float *state_in,
+                             const void *grad_y, const float *grad_state_out, void *grad_x,
+                             float *grad_w, float *grad_bias, float *grad_state_in, void *ws,
+                             size_t ws_bytes, hipStream_t stream) {
+    const snn_status st = check_shortconv(d);
+    if (st != SNN_OK) return st;
+    if (d->n == 0) return SNN_OK;
+    if (grad_bias && !bias) return SNN_ERR_UNSUPPORTED;
+    // the first tokens' threads write rows that others read as the last tokens'
+    if (grad_state_in && grad_state_in == grad_state_out) return SNN_ERR_UNSUPPORTED;
+    if (strided_overlap({d->T, d->B}, d->x_stride, d->n)) return SNN_ERR_SHAPE;
+    if (d->B > 0 && (!w || (d->T > 0 && (!x || !grad_y || !grad_x)))) return SNN_ERR_NULL;
+    if (any_misaligned({w, bias, lens, state_in, grad_state_out, grad_w, grad_bias, grad_state_in,
+                        ws}) ||
+        any_misaligned_rows(d->dtype, {x, grad_y, grad_x}))
+        return SNN_ERR_ALIGN;
+    const size_t need = snn_shortconv_workspace_bytes(d);
+    if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    ShortconvBwd q{};
+    q.a = shortconv_args(d, x, w, bias, lens, state_in);
+    q.gy = grad_y;
+    q.grad_state_out = grad_state_out;
+    q.gx = grad_x;
+    q.grad_w = grad_w, q.grad_bias = grad_bias, q.grad_state_in = grad_state_in;
+    q.part = (float *)ws;
+    (void)hipGetLastError();
+    return hip_status(launch_shortconv_bwd(q, d->width, d->dtype, stream));
+}
+
+snn_status snn_shortconv_step(const snn_shortconv_desc *d, const void *x, const float *w,
+                              const float *bias, const int32_t *slots, int32_t n_slots,
+                              const float *state_in, float *state_out, void *y,
+                              hipStream_t stream) {
+    const snn_status st = check_shortconv(d);
+    if (st != SNN_OK) return st;
+    if (d->T != 1 || n_slots < 0 || (!slots && n_slots < d->B)) return SNN_ERR_SHAPE;
+    if (d->B == 0 || d->n == 0) return SNN_OK;
+    if (strided_overlap({d->T, d->B}, d->y_stride, d->n)) return SNN_ERR_SHAPE;
+    if (!x || !w || !state_in || !state_out || !y) return SNN_ERR_NULL;
+    if (any_misaligned({w, bias, slots, state_in, state_out}) ||
+        any_misaligned_rows(d->dtype, {x, y}))
+        return SNN_ERR_ALIGN;
+    Shortconv a = shortconv_args(d, x, w, bias, nullptr, state_in);
+    a.y = y;
+    a.state_out = state_out;
+    (void)hipGetLastError();
+    return hip_status(launch_shortconv_step(a, slots, n_slots, d->width, d->dtype, stream));
+}
+
+size_t snn_layer_norm_workspace_bytes(const snn_layer_norm_desc *d) {
+    return check_layer_norm(d) == SNN_OK ? layer_norm_workspace_bytes(d->rows, d->n) : 0;
+}
+
+snn_status snn_layer_norm_fwd(const snn_layer_norm_desc *d, const void *x, const float *w,
+                              const float *b, void *y, hipStream_t stream) {
+    const snn_status st = check_layer_norm(d);
+    if (st != SNN_OK) return st;
+    if (d->rows == 0) return SNN_OK;
+    if (!x || !y) return SNN_ERR_NULL;
+    if (x == y && (d->x_dtype != d->y_dtype || d->ld_x != d->ld_y)) return SNN_ERR_UNSUPPORTED;
+    if (any_misaligned({w, b}) || any_misaligned_rows(d->x_dtype, {x}) ||
+        any_misaligned_rows(d->y_dtype, {y}))
+        return SNN_ERR_ALIGN;
+    const LayerNorm a{d->rows, d->n, d->eps, d->ld_x, d->ld_y, x, w, b, y};
+    (void)hipGetLastError();
+    return hip_status(launch_layer_norm(a, d->x_dtype, d->y_dtype, stream));
+}
+
+snn_status snn_layer_norm_bwd(const snn_layer_norm_desc *d, const void *x, const void *grad_y,
+                              const void *grad_res, const float *w, void *grad_x, float *grad_w,
+                              float *grad_b, void *ws, size_t ws_bytes, hipStream_t stream) {
+    const snn_status st = check_layer_norm(d);
+    if (st != SNN_OK) return st;
+    if (d->rows > 0 && (!x || !grad_y || !grad_x)) return SNN_ERR_NULL;
+    if (any_misaligned({w, grad_w, grad_b, ws}) ||
+        any_misaligned_rows(d->x_dtype, {x, grad_res, grad_x}) ||
+        any_misaligned_rows(d->y_dtype, {grad_y}))
+        return SNN_ERR_ALIGN;
+    const size_t need = snn_layer_norm_workspace_bytes(d);
+    if (ws_bytes < need || (need > 0 && !ws)) return SNN_ERR_WORKSPACE;
+    LayerNormBwd q{};
+    q.a = LayerNorm{d->rows, d->n, d->eps, d->ld_x, d->ld_y, x, w, nullptr, nullptr};
+    q.gy = grad_y, q.gres = grad_res, q.gx = grad_x;
+    q.grad_w = grad_w, q.grad_b = grad_b;
+    q.part = (float *)ws;
+    (void)hipGetLastError();
+    return hip_status(launch_layer_norm_bwd(q, d->x_dtype, d->y_dtype, stream));
+}
+
+}  // extern "C"

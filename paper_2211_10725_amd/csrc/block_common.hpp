@@ -1,0 +1,108 @@
+// Helpers of the selective leaky block's kernels (selscan.hip, shortconv.hip,
+// layer_norm.hip).
+#pragma once
+
+#include "snn_internal.hpp"
+
+namespace snn {
+namespace {
+
+typedef _Float16 half_t;
+typedef __bf16 bf16_t;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// V consecutive values of a row as they lie in memory, of any element alignment; only
+// the first m are in the row and read, the others are 0.
+template <typename T, int V>
+struct Raw {
+    static constexpr int kWords = V * (int)sizeof(T) / 4, kEach = 4 / (int)sizeof(T);
+    static_assert(kWords * 4 == V * (int)sizeof(T), "whole words");
+    uint32_t w[kWords];
+    __device__ inline void load(const T *p, int m) {
+        if (m >= V) {
+            __builtin_memcpy(w, p, sizeof(w));
+        } else {
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) {
+                T t[kEach];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j)
+                    t[j] = k * kEach + j < m ? p[k * kEach + j] : (T)0.f;
+                __builtin_memcpy(&w[k], t, 4);
+            }
+        }
+    }
+    __device__ inline void get(float (&x)[V]) const {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) {
+            T t[kEach];
+            __builtin_memcpy(t, &w[k], 4);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) x[k * kEach + j] = (float)t[j];
+        }
+    }
+};
+
+template <typename T, int V>
+__device__ inline void load_run(const T *p, int m, float (&v)[V]) {
+    Raw<T, V> r;
+    r.load(p, m);
+    r.get(v);
+}
+
+template <typename T, int V>
+__device__ inline void store_run(T *p, int m, const float (&v)[V]) {
+    if (m >= V) {
+        T t[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) t[j] = (T)v[j];
+        __builtin_memcpy(p, t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j < m) p[j] = (T)v[j];
+    }
+}
+
+// e^x to about 1e-7 of itself: x log2 e with its rounding error put back.
+__device__ inline float exp_of(float x) {
+    const float p = x * kLog2e;
+    const float r = __builtin_fmaf(x, kLog2e, -p) + x * 1.9259629911266175e-8f;
+    const float e = __builtin_amdgcn_exp2f(p);
+    return e > 0.f && e < __builtin_inff() ? __builtin_fmaf(e, r * kLn2, e) : e;
+}
+
+// silu and its slope p (1 + z (1 - p)), where 1 - p is taken as e^-z p, which keeps its
+// digits while the gate is open.
+__device__ inline float silu(float z) {
+    return z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
+}
+__device__ inline void silu_slope(float z, float &act, float &slope) {
+    const float e = exp_of(-z), p = __builtin_amdgcn_rcpf(1.f + e);
+    act = z * p;
+    slope = __builtin_fmaf(z, p * (fminf(e, 3.4028235e38f) * p), p);
+}
+
+// softplus log(1 + e^x) = max(x, 0) + log1p(e^-|x|) and its slope, the sigmoid.
+// log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by the series in s^2 to s^15 (the
+// next term is below 2^-31 of the sum): good to the last digits where e is small, as
+// the logarithm of a rounded 1 + e is not.
+__device__ inline void softplus(float x, float &value, float &slope) {
+    const float e = exp_of(-__builtin_fabsf(x));
+    const float s = e / (2.f + e), q = s * s;
+    float t = 1.f / 15.f;
+    t = __builtin_fmaf(t, q, 1.f / 13.f);
+    t = __builtin_fmaf(t, q, 1.f / 11.f);
+    t = __builtin_fmaf(t, q, 1.f / 9.f);
+    t = __builtin_fmaf(t, q, 1.f / 7.f);
+    t = __builtin_fmaf(t, q, 1.f / 5.f);
+    t = __builtin_fmaf(t, q, 1.f / 3.f);
+    value = fmaxf(x, 0.f) + 2.f * __builtin_fmaf(s * q, t, s);
+    const float p = __builtin_amdgcn_rcpf(1.f + e);
+    slope = x >= 0.f ? p : e * p;
+}
+
+}  // namespace
+}  // namespace snn

@@ -1,0 +1,835 @@
+// Selective scan: leaky integrators whose step the input chooses (include/snn.h,
+// "selective leaky block").
+//
+//     h_t[i] = exp(d_t a[i]) h_{t-1}[i] + d_t u_t b_t[i],   y_t = c_t . h_t + skip u_t
+//
+// Every decay is a channel's and an integrator's own, so nothing here is a matrix
+// product: a token costs each integrator an exponential and four multiply-adds, and
+// the vector unit bounds it.  The kernels are laid out for that: a lane is a channel,
+// so that the four integrators a wave holds of it need no exchange between lanes, and
+// the waves of a workgroup hold further integrators of the same 64 channels.  16 tokens
+// at a time: the workgroup stages their steps d and d u (one softplus for all of a
+// channel's integrators) and b and c in LDS, the waves run through them, and what they
+// add to each (token, channel) is summed over the waves through LDS, in order.
+//
+// Few channels and long sequences: the sequence is cut into segments.  A first pass
+// leaves each segment's end state from a zero start and its sum of steps (over a
+// segment the decay is exp(a sum d)), a second joins them, the third runs every segment
+// from its true start.
+//
+// Backward, tile by tile from the end: the forward left the states before each tile of
+// 16 tokens, the tile's states and decays are computed again into registers, then
+//     g_t = c_t gy_t + exp(d_{t+1} a) g_{t+1},   q = exp(d_t a) g_t h_{t-1},
+//     dc_t += gy_t h_t, db_t += d u g_t (sums over channels), d(d u) = b_t . g_t,
+//     d(d) += a q, da += d q.
+// The sums over channels are sums over lanes: 8 values of a token (4 integrators of b
+// and c) are halved three times by exchanges that leave each lane half of the values,
+// and joined with those of 7 more tokens, two instructions for a value of 64 lanes; the
+// workgroups' sums are added by another kernel in order.
+#include "block_common.hpp"
+
+namespace snn {
+namespace {
+
+constexpr int kTile = kSelscanTile;  // tokens
+constexpr int kLanes = 64;           // channels of a workgroup
+constexpr int kHold = 4;             // integrators of a wave
+
+// Where this workgroup works.
+struct Place {
+    int tile, seg, b, g, c0, live;  // channel tile, .., first channel, channels
+};
+__device__ inline Place place_of(const Selscan &a, int segs) {
+    Place p;
+    int x = blockIdx.x;
+    p.tile = x % a.tiles;
+    x /= a.tiles;
+    p.seg = x % segs;
+    p.b = x / segs;
+    const int per = a.tiles / a.groups, k = p.tile % per;
+    p.g = p.tile / per;
+    const int size = a.n / a.groups;
+    p.c0 = p.g * size + k * kLanes;
+    p.live = min(kLanes, size - k * kLanes);
+    return p;
+}
+
+__device__ inline int length_of(const Selscan &a, int b) {
+    return a.lens ? min(max(a.lens[b], 0), a.T) : a.T;
+}
+
+// b or c of a tile: thread (token, integrator) holds one value of each 4 W of them
+template <typename T, int W>
+__device__ inline float vec_value(const SelscanVec &v, int t, int b, int g, int i, bool in) {
+    return in ? (float)static_cast<const T *>(v.p)[t * v.st + b * v.sb + g * v.sg + i] : 0.f;
+}
+
+template <int W>
+struct Geo {
+    static constexpr int kThreads = kLanes * W;
+    static constexpr int kRow = 4 * W;           // threads of a token, and integrators at once
+    static constexpr int kEl = kLanes / kRow;    // channels of a staging thread
+};
+
+// OUT: outputs (and saved states), from a.slot's or the caller's start; else the end
+// state from zero and the sum of the steps, into a.slot and a.sums.
+template <typename T, int W, bool MANY, bool OUT>
+__global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
+    using G = Geo<W>;
+    constexpr int EL = G::kEl, ROW = G::kRow, MOST = MANY ? kSelscanMaxStates : ROW;
+    __shared__ float2 sd[kTile][kLanes];
+    __shared__ __attribute__((aligned(16))) float sb[kTile][MOST], sc[OUT ? kTile : 1][MOST];
+    __shared__ float yp[OUT ? W : 1][kTile][kLanes];
+    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int st = tid / ROW, se = tid % ROW * EL, si = tid % ROW;  // staging
+    const Place p = place_of(a, OUT ? a.segs : a.segs - 1);
+    const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
+    const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+    const int m = min(EL, max(0, p.live - se));
+    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;  // state [b][0][c]
+    const bool on = lane < p.live;
+    const float *first = OUT && a.segs > 1
+                             ? a.slot + (int64_t)p.seg * a.B * a.N * a.n
+                             : OUT ? a.state_in : nullptr;
+    float h[kHold], a2[kHold];
+    auto state = [&](int r, int k) { return r * ROW + w * kHold + k; };
+    auto load_round = [&](int r) {
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) {
+            const int i = state(r, k);
+            const bool in = on && i < a.N;
+            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+            h[k] = in && first ? first[sbase + (int64_t)i * a.n] : 0.f;
+        }
+    };
+    if (MANY) {
+        for (int r = 0; r < rounds; ++r) {
+            load_round(r);
+#pragma unroll
+            for (int k = 0; k < kHold; ++k) carry[state(r, k)][lane] = h[k];
+        }
+    } else {
+        load_round(0);
+    }
+    float bias[EL], skip[EL], sum[EL];
+#pragma unroll
+    for (int j = 0; j < EL; ++j) {
+        bias[j] = a.dt_bias && j < m ? a.dt_bias[p.c0 + se + j] : 0.f;
+        skip[j] = a.skip && j < m ? a.skip[p.c0 + se + j] : 0.f;
+        sum[j] = 0.f;
+    }
+    Raw<T, EL> ru, rd, rz;
+    float rb[MANY ? kSelscanMaxStates / ROW : 1], rc[MANY ? kSelscanMaxStates / ROW : 1];
+    auto fetch = [&](int t0) {
+        const int t = t0 + st, k = t < len && t < end ? m : 0;
+        const bool in = t < len && t < end;
+        ru.load(static_cast<const T *>(a.u.p) + t * a.u.st + p.b * a.u.sb + p.c0 + se, k);
+        rd.load(static_cast<const T *>(a.dt.p) + t * a.dt.st + p.b * a.dt.sb + p.c0 + se, k);
+        if (OUT && a.z.p)
+            rz.load(static_cast<const T *>(a.z.p) + t * a.z.st + p.b * a.z.sb + p.c0 + se, k);
+#pragma unroll
+        for (int r = 0; r < (MANY ? kSelscanMaxStates / ROW : 1); ++r) {
+            const int i = r * ROW + si;
+            rb[r] = vec_value<T, W>(a.b, t, p.b, p.g, i, in && i < a.N);
+            if (OUT) rc[r] = vec_value<T, W>(a.c, t, p.b, p.g, i, in && i < a.N);
+        }
+    };
+    const int stop = min(end, len);
+    if (begin < stop) fetch(begin);
+    for (int t0 = begin; t0 < stop; t0 += kTile) {
+        float u[EL], z[EL], d[EL];
+        const bool in = t0 + st < stop;
+        ru.get(u);
+        rd.get(d);
+        if (OUT && a.z.p) rz.get(z);
+#pragma unroll
+        for (int j = 0; j < EL; ++j) {
+            float v = d[j] + bias[j], s;
+            if (a.softplus) softplus(v, v, s);
+            d[j] = in && j < m ? v : 0.f;
+            sd[st][se + j] = make_float2(d[j], d[j] * u[j]);
+            sum[j] += d[j];
+        }
+#pragma unroll
+        for (int r = 0; r < (MANY ? kSelscanMaxStates / ROW : 1); ++r) {
+            sb[st][r * ROW + si] = rb[r];
+            if (OUT) sc[st][r * ROW + si] = rc[r];
+        }
+        if (t0 + kTile < stop) fetch(t0 + kTile);
+        __syncthreads();
+        for (int r = 0; r < (MANY ? rounds : 1); ++r) {
+            if (MANY) {
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) {
+                    const int i = state(r, k);
+                    a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+                    h[k] = carry[i][lane];
+                }
+            }
+            if (OUT && a.saved) {
+                float *s = a.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase;
+#pragma unroll
+                for (int k = 0; k < kHold; ++k)
+                    if (on && state(r, k) < a.N) s[(int64_t)state(r, k) * a.n] = h[k];
+            }
+            const int i0 = state(r, 0);
+#pragma unroll
+            for (int t = 0; t < kTile; ++t) {
+                const float2 v = sd[t][lane];
+                float y = 0.f;
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) {
+                    const float e = __builtin_amdgcn_exp2f(v.x * a2[k]);
+                    h[k] = __builtin_fmaf(e, h[k], v.y * sb[t][i0 + k]);
+                    if (OUT) y = __builtin_fmaf(sc[t][i0 + k], h[k], y);
+                }
+                if (OUT) yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
+            }
+            if (MANY) {
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) carry[state(r, k)][lane] = h[k];
+            }
+        }
+        __syncthreads();
+        if (OUT) {
+            float y[EL];
+#pragma unroll
+            for (int j = 0; j < EL; ++j) {
+                y[j] = yp[0][st][se + j];
+#pragma unroll
+                for (int k = 1; k < W; ++k) y[j] += yp[k][st][se + j];
+                y[j] = __builtin_fmaf(skip[j], u[j], y[j]);
+                if (a.z.p) y[j] *= silu(z[j]);
+                if (!in) y[j] = 0.f;
+            }
+            if (t0 + st < end)
+                store_run(static_cast<T *>(a.y) + (t0 + st) * a.y_st + p.b * a.y_sb + p.c0 + se, m,
+                          y);
+        }
+    }
+    // rows past the sequence, from the first tile that the loop left out
+    if (OUT) {
+        const float none[EL] = {};
+        const int from = begin < stop ? begin + (stop - begin + kTile - 1) / kTile * kTile : begin;
+        for (int t = from + st; t < end; t += kTile)
+            store_run(static_cast<T *>(a.y) + t * a.y_st + p.b * a.y_sb + p.c0 + se, m, none);
+    }
+    float *last = OUT ? (p.seg == a.segs - 1 ? a.state_out : nullptr)
+                      : a.slot + (int64_t)p.seg * a.B * a.N * a.n;
+    if (last)
+        for (int r = 0; r < (MANY ? rounds : 1); ++r)
+#pragma unroll
+            for (int k = 0; k < kHold; ++k) {
+                const int i = state(r, k);
+                if (on && i < a.N)
+                    last[sbase + (int64_t)i * a.n] = MANY ? carry[i][lane] : h[k];
+            }
+    if (!OUT) {  // the steps' sum: over the staging threads of a channel
+        __syncthreads();
+        float *s = &sd[0][0].x;
+#pragma unroll
+        for (int j = 0; j < EL; ++j) s[st * kLanes + se + j] = sum[j];
+        __syncthreads();
+        if (w == 0 && on) {
+            float t = 0.f;
+            for (int k = 0; k < kTile; ++k) t += s[k * kLanes + lane];
+            a.sums[((int64_t)p.seg * a.B + p.b) * a.n + p.c0 + lane] = t;
+        }
+    }
+}
+
+// Joins the segments: slot s, a segment's end state from zero, becomes the state that
+// enters it (reverse: the gradient of the state that leaves it).
+__global__ __launch_bounds__(256) void selscan_join_kernel(Selscan a, const float *from,
+                                                           bool reverse) {
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, size = (int64_t)a.B * a.N * a.n;
+    if (e >= size) return;
+    const int64_t c = e % a.n, i = e / a.n % a.N, b = e / a.n / a.N;
+    const float a2 = a.a[i * a.n + c] * kLog2e;
+    float h = from ? from[e] : 0.f;
+    for (int k = 0; k < a.segs; ++k) {
+        const int s = reverse ? a.segs - 1 - k : k;
+        float *slot = a.slot + s * size + e;
+        const bool last = k == a.segs - 1;
+        const float own = last ? 0.f : *slot;
+        *slot = h;
+        if (!last)
+            h = __builtin_fmaf(__builtin_amdgcn_exp2f(
+                                   a.sums[((int64_t)s * a.B + b) * a.n + c] * a2),
+                               h, own);
+    }
+}
+
+// ---- backward ------------------------------------------------------------------------
+
+// Lanes add up pairs of registers so that half of the lanes go on with x's sum and half,
+// those with the bit BIT of their number set, with y's.  The other lane of a pair is the
+// one across BIT, for 4 across 7 and for 2 across 3 (a reversal is one instruction):
+// taken in the order 32, 16, 8, 4, 2, 1 it has every earlier bit in common.
+template <int BIT>
+__device__ inline float halve(float x, float y) {
+    if constexpr (BIT == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y),
+                                                        false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else if constexpr (BIT == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y),
+                                                        false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else {
+        // row_ror:8, row_half_mirror, quad_perm [3,2,1,0], quad_perm [1,0,3,2]
+        constexpr int kCtrl = BIT == 8 ? 0x128 : BIT == 4 ? 0x141 : BIT == 2 ? 0x1b : 0xb1;
+        const bool up = (threadIdx.x & BIT) != 0;
+        const float keep = up ? y : x, give = up ? x : y;
+        return keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), kCtrl,
+                                                                 0xf, 0xf, false));
+    }
+}
+
+template <typename T, int W, bool MANY>
+__global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_kernel(SelscanBwd q) {
+    using G = Geo<W>;
+    const Selscan &a = q.a;
+    constexpr int EL = G::kEl, ROW = G::kRow, MOST = MANY ? kSelscanMaxStates : ROW;
+    constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
+    __shared__ float sd[kTile][kLanes], su[kTile][kLanes], sg[kTile][kLanes];
+    __shared__ __attribute__((aligned(16))) float sb[kTile][MOST], sc[kTile][MOST];
+    __shared__ float yp[W][kTile][kLanes], up[W][kTile][kLanes], dp[W][kTile][kLanes];
+    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
+    __shared__ float asum[MANY ? kSelscanMaxStates : 1][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int st = tid / ROW, se = tid % ROW * EL, si = tid % ROW;
+    const Place p = place_of(a, a.segs);
+    const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
+    const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+    const int m = min(EL, max(0, p.live - se));
+    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;
+    const bool on = lane < p.live;
+    const float *first = a.segs > 1 ? a.slot + (int64_t)p.seg * a.B * a.N * a.n
+                                    : q.grad_state_out;
+    float g[kHold], a2[kHold], acc[kHold];
+    auto state = [&](int r, int k) { return r * ROW + w * kHold + k; };
+    for (int r = 0; r < (MANY ? rounds : 1); ++r)
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) {
+            const int i = state(r, k);
+            const bool in = on && i < a.N;
+            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+            g[k] = in && first ? first[sbase + (int64_t)i * a.n] : 0.f;
+            acc[k] = 0.f;
+            if (MANY) carry[i][lane] = g[k], asum[i][lane] = 0.f;
+        }
+    float gskip[EL] = {}, gbias[EL] = {};
+    Raw<T, EL> ru, rd, rz, rg;
+    float rb[RND], rc[RND];
+    const int stop = min(end, len);
+    auto fetch = [&](int t0) {
+        const int t = t0 + st;
+        const bool in = t < stop;
+        const int k = in ? m : 0;
+        ru.load(static_cast<const T *>(a.u.p) + t * a.u.st + p.b * a.u.sb + p.c0 + se, k);
+        rd.load(static_cast<const T *>(a.dt.p) + t * a.dt.st + p.b * a.dt.sb + p.c0 + se, k);
+        rg.load(static_cast<const T *>(q.gy) + t * a.y_st + p.b * a.y_sb + p.c0 + se, k);
+        if (a.z.p)
+            rz.load(static_cast<const T *>(a.z.p) + t * a.z.st + p.b * a.z.sb + p.c0 + se, k);
+#pragma unroll
+        for (int r = 0; r < RND; ++r) {
+            const int i = r * ROW + si;
+            rb[r] = vec_value<T, W>(a.b, t, p.b, p.g, i, in && i < a.N);
+            rc[r] = vec_value<T, W>(a.c, t, p.b, p.g, i, in && i < a.N);
+        }
+    };
+    const float none[EL] = {};
+    auto put = [&](const SelscanRows &x, int t, const float (&v)[EL]) {
+        store_run(static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.c0 + se, m,
+                  v);
+    };
+    // rows past the sequence
+    for (int t = max(begin, stop) + st; t < end; t += kTile) {
+        put(q.du, t, none);
+        put(q.ddt, t, none);
+        if (a.z.p) put(q.dz, t, none);
+    }
+    const int tiles = begin < stop ? (stop - begin + kTile - 1) / kTile : 0;
+    if (tiles > 0) fetch(begin + (tiles - 1) * kTile);
+    for (int x = tiles - 1; x >= 0; --x) {
+        const int t0 = begin + x * kTile;
+        const bool in = t0 + st < stop;
+        float u[EL], slope[EL], zs[EL] = {};  // zs: gradient of the gate's input over y
+        {
+            float d[EL], gy[EL];
+            ru.get(u);
+            rd.get(d);
+            rg.get(gy);
+            if (a.z.p) rz.get(zs);
+#pragma unroll
+            for (int j = 0; j < EL; ++j) {
+                float v = d[j] + (j < m && a.dt_bias ? a.dt_bias[p.c0 + se + j] : 0.f);
+                slope[j] = 1.f;
+                if (a.softplus) softplus(v, v, slope[j]);
+                v = in && j < m ? v : 0.f;
+                float act = 1.f;
+                if (a.z.p) silu_slope(zs[j], act, zs[j]);
+                sd[st][se + j] = v;
+                su[st][se + j] = v * u[j];
+                sg[st][se + j] = gy[j] * act;
+                zs[j] *= gy[j];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RND; ++r) {
+            sb[st][r * ROW + si] = rb[r];
+            sc[st][r * ROW + si] = rc[r];
+        }
+        if (x > 0) fetch(t0 - kTile);
+        __syncthreads();
+        for (int r = 0; r < (MANY ? rounds : 1); ++r) {
+            const int i0 = state(r, 0);
+            float h0[kHold], h[kTile][kHold], e[kTile][kHold];
+            const float *s = q.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase;
+#pragma unroll
+            for (int k = 0; k < kHold; ++k) {
+                h0[k] = on && i0 + k < a.N ? s[(int64_t)(i0 + k) * a.n] : 0.f;
+                if (MANY) {
+                    a2[k] = on && i0 + k < a.N
+                                ? a.a[(int64_t)(i0 + k) * a.n + p.c0 + lane] * kLog2e
+                                : 0.f;
+                    g[k] = carry[i0 + k][lane];
+                    acc[k] = asum[i0 + k][lane];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kTile; ++t) {
+                const float dv = sd[t][lane], uv = su[t][lane];
+                float y = 0.f;
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) {
+                    e[t][k] = __builtin_amdgcn_exp2f(dv * a2[k]);
+                    h[t][k] = __builtin_fmaf(e[t][k], t ? h[t - 1][k] : h0[k],
+                                             uv * sb[t][i0 + k]);
+                    y = __builtin_fmaf(sc[t][i0 + k], h[t][k], y);
+                }
+                if (a.z.p) yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float part[3];
+#pragma unroll
+            for (int t = kTile - 1; t >= 0; --t) {
+                __builtin_amdgcn_sched_barrier(0);
+                const float dv = sd[t][lane], uv = su[t][lane], gv = sg[t][lane];
+                float gin = 0.f, gd = 0.f, vb[kHold], vc[kHold];
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) {
+                    const float full = __builtin_fmaf(sc[t][i0 + k], gv, g[k]);
+                    vc[k] = gv * h[t][k];
+                    vb[k] = full * uv;
+                    gin = __builtin_fmaf(full, sb[t][i0 + k], gin);
+                    g[k] = e[t][k] * full;
+                    const float x_ = g[k] * (t ? h[t - 1][k] : h0[k]);
+                    acc[k] = __builtin_fmaf(x_, dv, acc[k]);
+                    gd = __builtin_fmaf(x_, a2[k], gd);
+                }
+                up[w][t][lane] = MANY && r ? up[w][t][lane] + gin : gin;
+                dp[w][t][lane] = MANY && r ? dp[w][t][lane] + gd : gd;
+                // bits of the lane: 32 b or c, 16 and 8 the integrator's, 4, 2, 1 the
+                // token's (1, 2, 4 of 8)
+                float v = halve<8>(halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[2], vc[2])),
+                                   halve<16>(halve<32>(vb[1], vc[1]), halve<32>(vb[3], vc[3])));
+                if (t & 1) {
+                    part[0] = v;
+                    continue;
+                }
+                v = halve<4>(v, part[0]);
+                if (t & 2) {
+                    part[1] = v;
+                    continue;
+                }
+                v = halve<2>(v, part[1]);
+                if (t & 4) {
+                    part[2] = v;
+                    continue;
+                }
+                v = halve<1>(v, part[2]);
+                const int tt = t0 + t + (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4;
+                const int i = i0 + (lane >> 3 & 3), per = a.tiles / a.groups;
+                if (tt < stop && i < a.N)
+                    q.vec[((((int64_t)(lane >> 5) * per + p.tile % per) * a.T + tt) * a.B + p.b) *
+                              a.groups * a.N +
+                          p.g * a.N + i] = v;
+            }
+            if (MANY) {
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) carry[i0 + k][lane] = g[k], asum[i0 + k][lane] = acc[k];
+            }
+        }
+        __syncthreads();
+        float gu[EL], gdt[EL];
+#pragma unroll
+        for (int j = 0; j < EL; ++j) {
+            float y = a.z.p ? yp[0][st][se + j] : 0.f, gin = up[0][st][se + j],
+                  gd = dp[0][st][se + j];
+#pragma unroll
+            for (int k = 1; k < W; ++k) {
+                if (a.z.p) y += yp[k][st][se + j];
+                gin += up[k][st][se + j];
+                gd += dp[k][st][se + j];
+            }
+            const float d = sd[st][se + j], gi = sg[st][se + j];
+            const float skip = a.skip && j < m ? a.skip[p.c0 + se + j] : 0.f;
+            gu[j] = __builtin_fmaf(gin, d, gi * skip);
+            gdt[j] = in ? __builtin_fmaf(gin, u[j], gd * kLn2) * slope[j] : 0.f;
+            zs[j] *= __builtin_fmaf(skip, u[j], y);
+            gskip[j] = __builtin_fmaf(gi, u[j], gskip[j]);
+            gbias[j] += gdt[j];
+        }
+        if (in) {
+            put(q.du, t0 + st, gu);
+            put(q.ddt, t0 + st, gdt);
+            if (a.z.p) put(q.dz, t0 + st, zs);
+        }
+    }
+    // the gradient of the state before the segment, and the sums over its tokens
+    float *last = p.seg == 0 ? q.grad_state_in : nullptr;
+    float *rows = q.part + ((int64_t)p.b * a.segs + p.seg) * (a.N + 2) * a.n + p.c0 + lane;
+    for (int r = 0; r < (MANY ? rounds : 1); ++r)
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) {
+            const int i = state(r, k);
+            if (on && i < a.N) {
+                if (last) last[sbase + (int64_t)i * a.n] = MANY ? carry[i][lane] : g[k];
+                rows[(int64_t)i * a.n] = MANY ? asum[i][lane] : acc[k];
+            }
+        }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < EL; ++j) sd[st][se + j] = gskip[j], su[st][se + j] = gbias[j];
+    __syncthreads();
+    if (w == 0 && on) {
+        float s0 = 0.f, s1 = 0.f;
+        for (int k = 0; k < kTile; ++k) s0 += sd[k][lane], s1 += su[k][lane];
+        rows[(int64_t)a.N * a.n] = s0;
+        rows[(int64_t)(a.N + 1) * a.n] = s1;
+    }
+}
+
+// The gradient that a segment passes on from its own tokens, and the sum of its steps:
+// segments 1 .. segs - 1.
+template <typename T, int W, bool MANY>
+__global__ __launch_bounds__(Geo<W>::kThreads) void selscan_back_kernel(SelscanBwd q) {
+    using G = Geo<W>;
+    const Selscan &a = q.a;
+    constexpr int EL = G::kEl, ROW = G::kRow, MOST = MANY ? kSelscanMaxStates : ROW;
+    constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
+    __shared__ float2 sd[kTile][kLanes];
+    __shared__ __attribute__((aligned(16))) float sc[kTile][MOST];
+    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int st = tid / ROW, se = tid % ROW * EL, si = tid % ROW;
+    Place p = place_of(a, a.segs - 1);
+    p.seg += 1;
+    const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
+    const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
+    const int m = min(EL, max(0, p.live - se));
+    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;
+    const bool on = lane < p.live;
+    float g[kHold], a2[kHold];
+    auto state = [&](int r, int k) { return r * ROW + w * kHold + k; };
+    auto rates = [&](int r) {
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) {
+            const int i = state(r, k);
+            a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+        }
+    };
+    rates(0);
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) g[k] = 0.f;
+    if (MANY)
+        for (int i = w; i < kSelscanMaxStates; i += W) carry[i][lane] = 0.f;
+    float bias[EL], sum[EL];
+#pragma unroll
+    for (int j = 0; j < EL; ++j) {
+        bias[j] = a.dt_bias && j < m ? a.dt_bias[p.c0 + se + j] : 0.f;
+        sum[j] = 0.f;
+    }
+    Raw<T, EL> rd, rz, rg;
+    float rc[RND];
+    const int stop = min(end, len);
+    auto fetch = [&](int t0) {
+        const int t = t0 + st;
+        const bool in = t < stop;
+        const int k = in ? m : 0;
+        rd.load(static_cast<const T *>(a.dt.p) + t * a.dt.st + p.b * a.dt.sb + p.c0 + se, k);
+        rg.load(static_cast<const T *>(q.gy) + t * a.y_st + p.b * a.y_sb + p.c0 + se, k);
+        if (a.z.p)
+            rz.load(static_cast<const T *>(a.z.p) + t * a.z.st + p.b * a.z.sb + p.c0 + se, k);
+#pragma unroll
+        for (int r = 0; r < RND; ++r) {
+            const int i = r * ROW + si;
+            rc[r] = vec_value<T, W>(a.c, t, p.b, p.g, i, in && i < a.N);
+        }
+    };
+    const int tiles = begin < stop ? (stop - begin + kTile - 1) / kTile : 0;
+    if (tiles > 0) fetch(begin + (tiles - 1) * kTile);
+    for (int x = tiles - 1; x >= 0; --x) {
+        const int t0 = begin + x * kTile;
+        const bool in = t0 + st < stop;
+        float z[EL], d[EL], gy[EL];
+        rd.get(d);
+        rg.get(gy);
+        if (a.z.p) rz.get(z);
+        __syncthreads();  // the tile before has been read
+#pragma unroll
+        for (int j = 0; j < EL; ++j) {
+            float v = d[j] + bias[j], s;
+            if (a.softplus) softplus(v, v, s);
+            v = in && j < m ? v : 0.f;
+            sd[st][se + j] = make_float2(v, a.z.p ? gy[j] * silu(z[j]) : gy[j]);
+            sum[j] += v;
+        }
+#pragma unroll
+        for (int r = 0; r < RND; ++r) sc[st][r * ROW + si] = rc[r];
+        if (x > 0) fetch(t0 - kTile);
+        __syncthreads();
+        for (int r = 0; r < (MANY ? rounds : 1); ++r) {
+            const int i0 = state(r, 0);
+            if (MANY) {
+                rates(r);
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) g[k] = carry[i0 + k][lane];
+            }
+#pragma unroll
+            for (int t = kTile - 1; t >= 0; --t) {
+                const float2 v = sd[t][lane];
+#pragma unroll
+                for (int k = 0; k < kHold; ++k)
+                    g[k] = __builtin_amdgcn_exp2f(v.x * a2[k]) *
+                           __builtin_fmaf(sc[t][i0 + k], v.y, g[k]);
+            }
+            if (MANY) {
+#pragma unroll
+                for (int k = 0; k < kHold; ++k) carry[i0 + k][lane] = g[k];
+            }
+        }
+    }
+    for (int r = 0; r < (MANY ? rounds : 1); ++r)
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) {
+            const int i = state(r, k);
+            if (on && i < a.N)
+                a.slot[(int64_t)p.seg * a.B * a.N * a.n + sbase + (int64_t)i * a.n] =
+                    MANY ? carry[i][lane] : g[k];
+        }
+    __syncthreads();
+    float *s = &sd[0][0].x;
+#pragma unroll
+    for (int j = 0; j < EL; ++j) s[st * kLanes + se + j] = sum[j];
+    __syncthreads();
+    if (w == 0 && on) {
+        float t = 0.f;
+        for (int k = 0; k < kTile; ++k) t += s[k * kLanes + lane];
+        a.sums[((int64_t)p.seg * a.B + p.b) * a.n + p.c0 + lane] = t;
+    }
+}
+
+// Gradients of b and c: the channel tiles' sums, in order; tokens past a sequence 0.
+template <typename T>
+__global__ __launch_bounds__(256) void selscan_vec_kernel(SelscanBwd q) {
+    const Selscan &a = q.a;
+    const int64_t per = (int64_t)a.T * a.B * a.groups * a.N;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= per) return;
+    const int which = blockIdx.y, tiles = a.tiles / a.groups;
+    const int gi = (int)(e % (a.groups * a.N)), i = gi % a.N, g = gi / a.N;
+    const int64_t tb = e / (a.groups * a.N);
+    const int b = (int)(tb % a.B), t = (int)(tb / a.B);
+    float s = 0.f;
+    if (t < length_of(a, b)) {
+        const float *p = q.vec + which * tiles * per + e;
+        for (int k = 0; k < tiles; ++k) s += p[k * per];
+    }
+    const SelscanVec &v = which ? q.dc : q.db;
+    static_cast<T *>(const_cast<void *>(v.p))[t * v.st + b * v.sb + g * v.sg + i] = (T)s;
+}
+
+// Gradients of a, skip and dt_bias: the sequences' and segments' sums, in order.
+__global__ __launch_bounds__(256) void selscan_rows_kernel(SelscanBwd q, int rows) {
+    const Selscan &a = q.a;
+    const int64_t size = (int64_t)(a.N + 2) * a.n;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= size) return;
+    const int i = (int)(e / a.n);
+    float *out = i < a.N ? q.grad_a : i == a.N ? q.grad_skip : q.grad_dt_bias;
+    if (!out) return;
+    float s = 0.f;
+    for (int k = 0; k < rows; ++k) s += q.part[k * size + e];
+    out[i < a.N ? e : e % a.n] = s;
+}
+
+// ---- one token -----------------------------------------------------------------------
+// A thread takes V channels of a request, one after the other integrator.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void selscan_step_kernel(Selscan a, const int32_t *slots,
+                                                           int n_slots) {
+    const int per = (a.n + 256 * V - 1) / (256 * V), b = blockIdx.x / per;
+    const int c = ((blockIdx.x - b * per) * 256 + threadIdx.x) * V;
+    const int m = min(V, a.n - c);
+    if (m <= 0) return;
+    T *y = static_cast<T *>(a.y) + b * a.y_sb + c;
+    const int slot = slots ? slots[b] : b;
+    float out[V] = {};
+    if (slot < 0 || slot >= n_slots) {
+        store_run(y, m, out);
+        return;
+    }
+    float u[V], d[V], z[V], sk[V] = {}, bi[V] = {};
+    if constexpr (V * sizeof(T) >= 4) {
+        load_run(static_cast<const T *>(a.u.p) + b * a.u.sb + c, m, u);
+        load_run(static_cast<const T *>(a.dt.p) + b * a.dt.sb + c, m, d);
+        if (a.z.p) load_run(static_cast<const T *>(a.z.p) + b * a.z.sb + c, m, z);
+    } else {
+        u[0] = (float)static_cast<const T *>(a.u.p)[b * a.u.sb + c];
+        d[0] = (float)static_cast<const T *>(a.dt.p)[b * a.dt.sb + c];
+        if (a.z.p) z[0] = (float)static_cast<const T *>(a.z.p)[b * a.z.sb + c];
+    }
+    if (a.skip) load_run(a.skip + c, m, sk);
+    if (a.dt_bias) load_run(a.dt_bias + c, m, bi);
+    float du[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        float v = d[j] + bi[j], s;
+        if (a.softplus) softplus(v, v, s);
+        d[j] = v * kLog2e;
+        du[j] = v * u[j];
+    }
+    const int size = a.n / a.groups;
+    int g[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) g[j] = min(c + j, a.n - 1) / size;
+    const T *pb = static_cast<const T *>(a.b.p) + b * a.b.sb;
+    const T *pc = static_cast<const T *>(a.c.p) + b * a.c.sb;
+    const float *in = a.state_in + (int64_t)slot * a.N * a.n + c;
+    float *to = a.state_out + (int64_t)slot * a.N * a.n + c;
+#pragma unroll 4
+    for (int i = 0; i < a.N; ++i) {
+        float h[V], r[V];
+        load_run(in + (int64_t)i * a.n, m, h);
+        load_run(a.a + (int64_t)i * a.n + c, m, r);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float bv = (float)pb[g[j] * a.b.sg + i], cv = (float)pc[g[j] * a.c.sg + i];
+            h[j] = __builtin_fmaf(__builtin_amdgcn_exp2f(d[j] * r[j]), h[j], du[j] * bv);
+            out[j] = __builtin_fmaf(cv, h[j], out[j]);
+        }
+        store_run(to + (int64_t)i * a.n, m, h);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        out[j] = __builtin_fmaf(sk[j], u[j], out[j]);
+        if (a.z.p) out[j] *= silu(z[j]);
+    }
+    store_run(y, m, out);
+}
+
+template <typename T, int W, bool MANY>
+hipError_t run_fwd(const Selscan &a, hipStream_t s) {
+    const int units = a.tiles * a.B, threads = Geo<W>::kThreads;
+    if (a.segs > 1) {
+        selscan_kernel<T, W, MANY, false><<<units * (a.segs - 1), threads, 0, s>>>(a);
+        const int64_t size = (int64_t)a.B * a.N * a.n;
+        selscan_join_kernel<<<(unsigned)((size + 255) / 256), 256, 0, s>>>(a, a.state_in, false);
+    }
+    selscan_kernel<T, W, MANY, true><<<units * a.segs, threads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int W, bool MANY>
+hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
+    const Selscan &a = q.a;
+    const int units = a.tiles * a.B, threads = Geo<W>::kThreads;
+    if (units > 0 && a.segs > 1) {
+        selscan_back_kernel<T, W, MANY><<<units * (a.segs - 1), threads, 0, s>>>(q);
+        const int64_t size = (int64_t)a.B * a.N * a.n;
+        selscan_join_kernel<<<(unsigned)((size + 255) / 256), 256, 0, s>>>(a, q.grad_state_out,
+                                                                          true);
+    }
+    if (units > 0) selscan_bwd_kernel<T, W, MANY><<<units * a.segs, threads, 0, s>>>(q);
+    const int64_t per = (int64_t)a.T * a.B * a.groups * a.N;
+    if (per > 0)
+        selscan_vec_kernel<T><<<dim3((unsigned)((per + 255) / 256), 2), 256, 0, s>>>(q);
+    if (q.grad_a || q.grad_skip || q.grad_dt_bias)
+        selscan_rows_kernel<<<(unsigned)(((int64_t)(a.N + 2) * a.n + 255) / 256), 256, 0, s>>>(
+            q, a.B * a.segs);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t by_states(const Selscan &a, hipStream_t s) {
+    if (a.N <= 4) return run_fwd<T, 1, false>(a, s);
+    if (a.N <= 8) return run_fwd<T, 2, false>(a, s);
+    if (a.N <= 16) return run_fwd<T, 4, false>(a, s);
+    return run_fwd<T, 4, true>(a, s);
+}
+template <typename T>
+hipError_t by_states(const SelscanBwd &q, hipStream_t s) {
+    if (q.a.N <= 4) return run_bwd<T, 1, false>(q, s);
+    if (q.a.N <= 8) return run_bwd<T, 2, false>(q, s);
+    if (q.a.N <= 16) return run_bwd<T, 4, false>(q, s);
+    return run_bwd<T, 4, true>(q, s);
+}
+
+template <typename T>
+void run_step(const Selscan &a, const int32_t *slots, int n_slots, hipStream_t s) {
+    // four channels a thread once the threads left fill the device
+    if ((int64_t)a.B * a.n >= 4 * 256 * kPlanCus)
+        selscan_step_kernel<T, 4><<<a.B * ((a.n + 1023) / 1024), 256, 0, s>>>(a, slots, n_slots);
+    else
+        selscan_step_kernel<T, 1><<<a.B * ((a.n + 255) / 256), 256, 0, s>>>(a, slots, n_slots);
+}
+
+}  // namespace
+
+int selscan_tiles(int n, int groups) {
+    return groups * ((n / groups + kLanes - 1) / kLanes);
+}
+
+// Workgroups of 64 channels of a sequence, and of segments of it where they are few.
+SelscanPlan selscan_plan(int T, int64_t units) {
+    SelscanPlan p{1, std::max(T, 1)};
+    if (units < 1 || units > kPlanCus / 2) return p;
+    const int tiles = (T + kTile - 1) / kTile;
+    const int segs = (int)std::min<int64_t>(4 * kPlanCus / units, tiles / 4);
+    if (segs < 2) return p;
+    p.seg_len = (tiles + segs - 1) / segs * kTile;
+    p.segs = (T + p.seg_len - 1) / p.seg_len;
+    return p;
+}
+
+hipError_t launch_selscan(const Selscan &a, int dtype, hipStream_t s) {
+    switch (dtype) {
+        case SNN_F32: return by_states<float>(a, s);
+        case SNN_F16: return by_states<half_t>(a, s);
+        default: return by_states<bf16_t>(a, s);
+    }
+}
+
+hipError_t launch_selscan_bwd(const SelscanBwd &q, int dtype, hipStream_t s) {
+    switch (dtype) {
+        case SNN_F32: return by_states<float>(q, s);
+        case SNN_F16: return by_states<half_t>(q, s);
+        default: return by_states<bf16_t>(q, s);
+    }
+}
+
+hipError_t launch_selscan_step(const Selscan &a, const int32_t *slots, int n_slots, int dtype,
+                               hipStream_t s) {
+    switch (dtype) {
+        case SNN_F32: run_step<float>(a, slots, n_slots, s); break;
+        case SNN_F16: run_step<half_t>(a, slots, n_slots, s); break;
+        default: run_step<bf16_t>(a, slots, n_slots, s); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace snn

@@ -408,4 +408,94 @@ size_t gate_norm_workspace_bytes(int64_t rows, int64_t n);
 hipError_t launch_checkpoint(int64_t rows, int n, int block, int64_t ld, int dtype, void *x,
                              int8_t *codes, float *scales, bool save, hipStream_t s);
 
+// ---- selective scan (selscan.hip) -----------------------------------------------
+constexpr int kSelscanTile = 16;       // tokens between saved states
+constexpr int kSelscanMaxStates = 64;
+struct SelscanRows {  // element (t, b, c) at t st + b sb + c
+    const void *p;
+    int64_t st, sb;
+};
+struct SelscanVec {   // element (t, b, g, i) at t st + b sb + g sg + i
+    const void *p;
+    int64_t st, sb, sg;
+};
+struct Selscan {
+    int T, B, n, N, groups, softplus;
+    int tiles;            // of 64 channels, none over two groups
+    int segs, seg_len;    // of tokens; whole tiles of kSelscanTile
+    const int32_t *lens;
+    SelscanRows u, dt, z;  // z.p NULL: no gate
+    SelscanVec b, c;
+    const float *a, *skip, *dt_bias, *state_in;
+    void *y;              // forward and step; its strides are grad_y's too
+    int64_t y_st, y_sb;
+    float *state_out, *saved;
+    float *slot, *sums;   // segs > 1: [segs, B, N, n] states, [segs, B, n] sums of steps
+};
+struct SelscanBwd {
+    Selscan a;
+    const void *gy;
+    const float *saved, *grad_state_out;
+    SelscanRows du, ddt, dz;
+    SelscanVec db, dc;
+    float *grad_a, *grad_skip, *grad_dt_bias, *grad_state_in;
+    float *vec;           // [2, tiles / groups, T, B, groups, N]
+    float *part;          // [B, segs, N + 2, n]
+};
+struct SelscanPlan {
+    int segs, seg_len;
+};
+int selscan_tiles(int n, int groups);
+SelscanPlan selscan_plan(int T, int64_t units);  // units: channel tiles by sequences
+hipError_t launch_selscan(const Selscan &a, int dtype, hipStream_t s);
+hipError_t launch_selscan_bwd(const SelscanBwd &q, int dtype, hipStream_t s);
+hipError_t launch_selscan_step(const Selscan &a, const int32_t *slots, int n_slots, int dtype,
+                               hipStream_t s);
+
+// ---- short causal convolution (shortconv.hip) ------------------------------------
+struct Shortconv {
+    int T, B, n, silu;
+    const int32_t *lens;
+    SelscanRows x;
+    const float *w, *bias, *state_in;
+    void *y;
+    int64_t y_st, y_sb;
+    float *state_out;
+    int slice;            // tokens of a thread, set by the launcher
+};
+struct ShortconvBwd {
+    Shortconv a;
+    const void *gy;
+    const float *grad_state_out;
+    void *gx;
+    float *grad_w, *grad_bias, *grad_state_in;
+    float *part;          // [workgroups of a channel, width + 1, n]
+};
+size_t shortconv_workspace_bytes(int T, int B, int n, int width);
+hipError_t launch_shortconv(const Shortconv &a, int width, int dtype, hipStream_t s);
+hipError_t launch_shortconv_bwd(const ShortconvBwd &q, int width, int dtype, hipStream_t s);
+hipError_t launch_shortconv_step(const Shortconv &a, const int32_t *slots, int n_slots, int width,
+                                 int dtype, hipStream_t s);
+
+// ---- layer norm (layer_norm.hip) ---------------------------------------------------
+constexpr int kLayerNormMaxN = 16384;
+struct LayerNorm {
+    int rows, n;
+    float eps;
+    int64_t ld_x, ld_y;
+    const void *x;
+    const float *w, *b;
+    void *y;
+};
+struct LayerNormBwd {
+    LayerNorm a;
+    const void *gy, *gres;
+    void *gx;
+    float *grad_w, *grad_b;
+    float *part;          // [2][workgroups][n] column sums
+};
+size_t layer_norm_workspace_bytes(int64_t rows, int64_t n);
+hipError_t launch_layer_norm(const LayerNorm &a, int xt, int yt, hipStream_t s);
+hipError_t launch_layer_norm_bwd(const LayerNormBwd &q, int xt, int yt, hipStream_t s);
+
 }  // namespace snn

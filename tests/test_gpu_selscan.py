@@ -1,0 +1,321 @@
+"""Selective scan with its backward and single tokens against the 64-bit reference, whose
+carried error is the tolerance (``selective_reference``)."""
+import numpy as np
+import pytest
+
+import paper_2211_10725_amd as snn
+from tests import selective_reference as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+GRADS = ["du", "ddt", "da", "db", "dc", "dskip", "dbias", "dz", "dstate"]
+
+
+def _np(x):
+    return x.detach().double().cpu().numpy()
+
+
+def _dev(x, dt="f32"):
+    return torch.as_tensor(x, dtype=torch.float32).to(TYPES[dt]).cuda()
+
+
+def _nan_like(x):
+    out = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    return out.fill_(float("nan"))
+
+
+def _room(size):
+    return torch.full((max(size, 16),), 0xff, dtype=torch.uint8, device="cuda")
+
+
+class Case:
+    """Inputs of a scan; `pad` channels of other tensors beside each row, which start
+    `off` elements into memory."""
+
+    def __init__(self, T, B, n, N, G=1, dt="f32", gate=True, soft=True, ragged=False, pad=0,
+                 off=0, seed=0, state=True, vecs=True, poison=False):
+        rng = np.random.default_rng(seed)
+        self.T, self.B, self.n, self.N, self.G, self.dt, self.soft = T, B, n, N, G, dt, soft
+
+        def rows(width, scale=1.0, shift=0.0):
+            x = _dev(rng.standard_normal((T, B, width + pad + off)) * scale + shift, dt)
+            return x[:, :, off:off + width]
+
+        self.u, self.z, self.gy = rows(n), rows(n) if gate else None, rows(n)
+        self.step = rows(n) if soft else rows(n, 0.05, 0.3)
+        self.b, self.c = (rows(G * N).unflatten(2, (G, N)) for _ in range(2))
+        self.a = _dev(-np.exp(rng.uniform(-3, 1, (N, n))))
+        self.skip = _dev(rng.standard_normal(n)) if vecs else None
+        # steps between 0.02 and 1 before the tokens have their say
+        self.bias = _dev(rng.uniform(-4, 0.5, n) if soft else rng.uniform(0, 0.2, n)) if vecs \
+            else None
+        self.init = _dev(rng.standard_normal((B, N, n))) if state else None
+        self.gs = _dev(rng.standard_normal((B, N, n))) if state else None
+        lens = np.full(B, T)
+        if ragged:
+            lens = np.array([(i * (5 * T // 7 + 1)) % (T + 1) if i else T for i in range(B)])
+        self.lens = torch.as_tensor(lens, dtype=torch.int32).cuda() if ragged else None
+        if poison:  # what lies past a sequence is not read
+            for x in (self.u, self.z, self.step, self.b, self.c, self.gy):
+                for i in range(B):
+                    if x is not None:
+                        x[lens[i]:, i] = [float("nan"), float("inf")][i % 2]
+        zero = np.zeros((B, N, n))
+        self.args = [_np(self.u), _np(self.step), _np(self.a), _np(self.b), _np(self.c),
+                     _np(self.skip) if vecs else np.zeros(n),
+                     _np(self.bias) if vecs else np.zeros(n), _np(self.z) if gate else None, lens,
+                     _np(self.init) if state else zero, soft]
+        self.grads_in = dict(gy=_np(self.gy), gs=_np(self.gs) if state else zero)
+        self.y = _nan_like(self.gy)
+        self.d = snn.selscan_desc(self.u, self.step, self.b, self.c, self.y, self.z, soft)
+        self.ws = _room(snn.snn_selscan_workspace_bytes(self.d))
+
+    def ins(self):
+        return [self.u, self.step, self.a, self.b, self.c, self.skip, self.bias, self.z, self.lens]
+
+    def fwd(self, state_out=None):
+        self.saved = _room(snn.snn_selscan_saved_bytes(self.d))
+        self.out = torch.full((self.B, self.N, self.n), float("nan"), device="cuda") \
+            if state_out is None else state_out
+        snn.snn_selscan_fwd(self.d, *self.ins(), self.init, self.y, self.out, self.saved, self.ws)
+
+    def bwd(self, dstate=None):
+        new = {"du": self.u, "ddt": self.step, "da": self.a, "db": self.b, "dc": self.c,
+               "dskip": self.skip, "dbias": self.bias, "dz": self.z}
+        self.got = {k: None if t is None else _nan_like(t) for k, t in new.items()}
+        self.got["dstate"] = torch.full((self.B, self.N, self.n), float("nan"), device="cuda") \
+            if dstate is None else dstate
+        snn.snn_selscan_bwd(self.d, *self.ins(), self.saved, self.gy, self.gs,
+                            *(self.got[k] for k in GRADS), self.ws)
+
+    def check(self):
+        self.fwd()
+        self.bwd()
+        y, state, want = ref.selscan(*self.args, **self.grads_in)
+        ref.near(_np(self.y), y, self.dt, "y")
+        ref.near(_np(self.out), state, "f32", "state")
+        for k in GRADS:
+            if self.got[k] is not None:
+                ref.near(_np(self.got[k]), want[k],
+                         self.dt if k in ("du", "ddt", "db", "dc", "dz") else "f32", k)
+
+
+# one of each, past a tile of tokens, of channels and of integrators, and group ends
+SIZES = [(1, 1, 1, 1, 1), (5, 2, 3, 2, 1), (16, 1, 64, 4, 1), (17, 3, 65, 5, 1),
+         (33, 2, 130, 8, 2), (47, 2, 96, 12, 3), (64, 1, 70, 16, 1), (40, 2, 66, 17, 1),
+         (35, 1, 40, 33, 2), (20, 1, 30, 64, 1)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_sizes(size, dt):
+    Case(*size, dt=dt, seed=sum(size)).check()
+
+
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("soft", [True, False])
+@pytest.mark.parametrize("state", [True, False])
+def test_options(gate, soft, state):
+    Case(21, 3, 40, 6, gate=gate, soft=soft, state=state, vecs=state, seed=5).check()
+
+
+@pytest.mark.parametrize("N", [3, 16, 24])
+@pytest.mark.parametrize("dt", list(TYPES))
+def test_ragged_lengths_and_what_lies_behind(N, dt):
+    Case(37, 6, 70, N, dt=dt, ragged=True, poison=True, seed=N).check()
+
+
+@pytest.mark.parametrize("pad,off", [(8, 0), (5, 3), (1, 1)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_slices_of_any_alignment(pad, off, dt):
+    Case(19, 2, 67, 16, dt=dt, pad=pad, off=off, seed=pad).check()
+
+
+@pytest.mark.parametrize("T,B,n,N", [(700, 1, 64, 16), (1000, 2, 30, 3), (333, 1, 100, 20)])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_segments(T, B, n, N, ragged):
+    Case(T, B, n, N, ragged=ragged, seed=T).check()
+
+
+def test_no_tokens_and_no_sequences():
+    c = Case(0, 2, 20, 4)
+    c.fwd()
+    c.bwd()
+    assert torch.equal(c.out, c.init) and torch.equal(c.got["dstate"], c.gs)
+    assert all((c.got[k] == 0).all() for k in ("da", "dskip", "dbias"))
+    c = Case(5, 0, 20, 4)
+    c.fwd()
+    c.bwd()
+    assert all((c.got[k] == 0).all() for k in ("da", "dskip", "dbias"))
+
+
+@pytest.mark.parametrize("T", [30, 900])
+def test_states_in_place(T):
+    c = Case(T, 2, 48, 16, seed=1)
+    c.fwd()
+    c.bwd()
+    y, out, du, dstate = c.y.clone(), c.out.clone(), c.got["du"].clone(), c.got["dstate"].clone()
+    c.init_was = c.init.clone()
+    c.fwd(c.init)
+    c.bwd(c.gs)
+    assert torch.equal(c.y, y) and torch.equal(c.init, out)
+    assert torch.equal(c.got["du"], du) and torch.equal(c.gs, dstate)
+
+
+def test_same_call_same_bits_and_optional_outputs():
+    c = Case(200, 2, 96, 16, dt="bf16", seed=2)
+    c.fwd()
+    c.bwd()
+    first = {k: v.clone() for k, v in c.got.items()}
+    c.bwd()
+    assert all(torch.equal(first[k], c.got[k]) for k in GRADS)
+    du = c.got["du"].clone()
+    snn.snn_selscan_bwd(c.d, *c.ins(), c.saved, c.gy, c.gs, c.got["du"], c.got["ddt"], None,
+                        c.got["db"], c.got["dc"], None, None, c.got["dz"], None, c.ws)
+    assert torch.equal(du, c.got["du"])
+    snn.snn_selscan_fwd(c.d, *c.ins(), c.init, c.y, None, c.saved, c.ws)
+
+
+def test_forward_only_is_the_same_forward():
+    c = Case(300, 1, 64, 16, dt="f16", seed=3)
+    c.fwd()
+    y, out = c.y.clone(), c.out.clone()
+    d = snn.selscan_desc(c.u, c.step, c.b, c.c, c.y, c.z, forward_only=True)
+    need = snn.snn_selscan_workspace_bytes(d)
+    assert need < snn.snn_selscan_workspace_bytes(c.d) and snn.snn_selscan_saved_bytes(d) == 0
+    snn.snn_selscan_fwd(d, *c.ins(), c.init, c.y, c.out, None, _room(need))
+    assert torch.equal(y, c.y) and torch.equal(out, c.out)
+
+
+def test_vectors_shared_by_sequences():
+    """b and c broadcast over the sequences (stride 0) are read in the forward."""
+    c = Case(20, 3, 40, 8)
+    one = [x[:, :1] for x in (c.b, c.c)]
+    c.b, c.c = (x.expand(-1, 3, -1, -1) for x in one)
+    c.d = snn.selscan_desc(c.u, c.step, c.b, c.c, c.y, c.z)
+    c.args[3], c.args[4] = _np(c.b), _np(c.c)
+    c.fwd()
+    y, state = ref.selscan(*c.args)
+    ref.near(_np(c.y), y, "f32", "y")
+    ref.near(_np(c.out), state, "f32", "state")
+    with pytest.raises(snn.SNNError):
+        c.bwd()
+
+
+@pytest.mark.parametrize("dt", list(TYPES))
+@pytest.mark.parametrize("B,n,N,G", [(1, 1, 1, 1), (3, 70, 5, 2), (5, 1030, 16, 1), (2, 90, 64, 3),
+                                     (70, 4096, 16, 1)])
+def test_step(B, n, N, G, dt):
+    c = Case(1, B, n, N, G, dt=dt, seed=n, pad=2, off=1)
+    pool = torch.randn((B + 3, N, n), device="cuda")
+    slots = torch.randperm(B + 3, device="cuda")[:B].to(torch.int32)
+    idle = B > 1
+    if idle:
+        slots[1] = -1
+    out, at = pool.clone(), slots.long()
+    ins = c.ins()[:8]
+    snn.snn_selscan_step(c.d, *ins, slots, out, out, c.y)  # in place
+    c.args[9] = _np(pool[at.clamp(min=0)])
+    y, state = ref.selscan(*c.args)
+    keep = [b for b in range(B) if not (idle and b == 1)]
+    ref.near(_np(c.y)[0][keep], y[0][keep], dt, "y")
+    ref.near(_np(out[at])[keep], state[keep], "f32", "state")
+    if idle:
+        assert (c.y[0, 1] == 0).all()
+    rest = torch.ones(B + 3, dtype=torch.bool, device="cuda")
+    rest[at[keep]] = False
+    assert torch.equal(out[rest], pool[rest])
+    other = torch.full_like(pool, 7.0)
+    y0 = c.y.clone()
+    snn.snn_selscan_step(c.d, *ins, slots, pool, other, c.y)
+    assert torch.equal(c.y, y0) and torch.equal(other[at[keep]], out[at[keep]])
+    assert (other[rest] == 7).all()
+
+
+def test_steps_continue_a_prompt():
+    c = Case(24, 2, 80, 16, seed=9)
+    c.fwd()
+    state = c.init.clone()
+    part = [x[:10] if x is not None else None for x in (c.u, c.step, c.b, c.c, c.y, c.z)]
+    d = snn.selscan_desc(*part, forward_only=True)
+    y = torch.empty_like(c.y)
+    vecs = (c.skip, c.bias)
+    snn.snn_selscan_fwd(d, part[0], part[1], c.a, part[2], part[3], *vecs, part[5], None, state,
+                        y[:10], state, None, _room(snn.snn_selscan_workspace_bytes(d)))
+    one = snn.selscan_desc(c.u[:1], c.step[:1], c.b[:1], c.c[:1], y[:1], c.z[:1])
+    for t in range(10, 24):
+        s = slice(t, t + 1)
+        snn.snn_selscan_step(one, c.u[s], c.step[s], c.a, c.b[s], c.c[s], *vecs, c.z[s], None,
+                             state, state, y[s])
+    want, last = ref.selscan(*c.args)
+    ref.near(_np(y), want, "f32", "y")
+    ref.near(_np(state), last, "f32", "state")
+
+
+def test_far_apart_tokens():
+    """Offsets past 2^32 bytes and 2^31 elements."""
+    c = Case(3, 1, 40, 8, dt="bf16", seed=4)
+    far = torch.empty(2 * (1 << 31) + 64, dtype=torch.bfloat16, device="cuda")
+    u = far.as_strided((3, 1, 40), (1 << 31, 40, 1))
+    u.copy_(c.u)
+    c.u = u
+    c.d = snn.selscan_desc(c.u, c.step, c.b, c.c, c.y, c.z)
+    c.fwd()
+    y, state = ref.selscan(*c.args)
+    ref.near(_np(c.y), y, "bf16", "y")
+
+
+def test_replayed_graph_and_other_stream():
+    c = Case(150, 2, 64, 16, dt="bf16", seed=6)
+    c.fwd()
+    c.bwd()
+    want = [c.y.clone(), c.out.clone()] + [c.got[k].clone() for k in GRADS]
+    got = [c.y, c.out] + [c.got[k] for k in GRADS]
+
+    def both():
+        snn.snn_selscan_fwd(c.d, *c.ins(), c.init, c.y, c.out, c.saved, c.ws)
+        snn.snn_selscan_bwd(c.d, *c.ins(), c.saved, c.gy, c.gs, *(c.got[k] for k in GRADS), c.ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        both()
+    for _ in range(3):
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        x = torch.randn(1 << 20, device="cuda").sum().item()
+        assert x == x
+    for t in got:
+        t.fill_(float("nan"))
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_infinite_and_huge_values_stay_in_their_token_and_channel():
+    """An infinite u reaches its own channel only, and no token before it."""
+    c = Case(20, 2, 30, 16, seed=8)
+    c.fwd()
+    y = c.y.clone()
+    c.u[9, 1, 4] = float("inf")
+    c.fwd()
+    same = torch.ones_like(y, dtype=torch.bool)
+    same[9:, 1, 4] = False
+    assert torch.equal(y[same], c.y[same])
+    assert not torch.isfinite(c.y[9, 1, 4])
+
+
+def test_open_and_shut_steps():
+    """Raw steps far from zero: softplus is the step itself, or almost nothing."""
+    c = Case(18, 1, 8, 4, seed=10)
+    c.step[:, :, 0], c.step[:, :, 1], c.step[:, :, 2] = 30.0, -30.0, -100.0
+    c.args[1] = _np(c.step)
+    c.check()
