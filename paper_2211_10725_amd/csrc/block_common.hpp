@@ -66,32 +66,37 @@ __device__ inline void store_run(T *p, int m, const float (&v)[V]) {
     }
 }
 
-// e^x to about 1e-7 of itself: x log2 e with its rounding error put back.
+// e^x, within e^-150 .. e^88.5 (past that 1 + e^x is 1, or its reciprocal as good as
+// nothing).  FINE: to about 1e-7 of itself, 2^p e^(x - p ln 2) with p = fl(x log2 e);
+// else with p's error, |x| 2^-24, which a result of 16 bits does not show.
+template <bool FINE>
 __device__ inline float exp_of(float x) {
-    const float p = x * kLog2e;
-    const float r = __builtin_fmaf(x, kLog2e, -p) + x * 1.9259629911266175e-8f;
-    const float e = __builtin_amdgcn_exp2f(p);
-    return e > 0.f && e < __builtin_inff() ? __builtin_fmaf(e, r * kLn2, e) : e;
+    if (!FINE) return __builtin_amdgcn_exp2f(fminf(x * kLog2e, 127.f));
+    x = __builtin_amdgcn_fmed3f(x, -150.f, 88.5f);
+    const float p = x * kLog2e, e = __builtin_amdgcn_exp2f(p);
+    return __builtin_fmaf(e, __builtin_fmaf(p, -kLn2, x), e);
 }
 
 // silu and its slope p (1 + z (1 - p)), where 1 - p is taken as e^-z p, which keeps its
 // digits while the gate is open.
+template <bool FINE>
 __device__ inline float silu(float z) {
-    return z * __builtin_amdgcn_rcpf(1.f + exp_of(-z));
+    return z * __builtin_amdgcn_rcpf(1.f + exp_of<FINE>(-z));
 }
+template <bool FINE>
 __device__ inline void silu_slope(float z, float &act, float &slope) {
-    const float e = exp_of(-z), p = __builtin_amdgcn_rcpf(1.f + e);
+    const float e = exp_of<FINE>(-z), p = __builtin_amdgcn_rcpf(1.f + e);
     act = z * p;
-    slope = __builtin_fmaf(z, p * (fminf(e, 3.4028235e38f) * p), p);
+    slope = __builtin_fmaf(z, p * (e * p), p);
 }
 
 // softplus log(1 + e^x) = max(x, 0) + log1p(e^-|x|) and its slope, the sigmoid.
 // log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by the series in s^2 to s^15 (the
 // next term is below 2^-31 of the sum): good to the last digits where e is small, as
-// the logarithm of a rounded 1 + e is not.
+// the logarithm of a rounded 1 + e is not.  Fine always: states of 32 bits come of it.
 __device__ inline void softplus(float x, float &value, float &slope) {
-    const float e = exp_of(-__builtin_fabsf(x));
-    const float s = e / (2.f + e), q = s * s;
+    const float e = exp_of<true>(-__builtin_fabsf(x));
+    const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
     float t = 1.f / 15.f;
     t = __builtin_fmaf(t, q, 1.f / 13.f);
     t = __builtin_fmaf(t, q, 1.f / 11.f);
@@ -99,7 +104,7 @@ __device__ inline void softplus(float x, float &value, float &slope) {
     t = __builtin_fmaf(t, q, 1.f / 7.f);
     t = __builtin_fmaf(t, q, 1.f / 5.f);
     t = __builtin_fmaf(t, q, 1.f / 3.f);
-    value = fmaxf(x, 0.f) + 2.f * __builtin_fmaf(s * q, t, s);
+    value = __builtin_fmaf(2.f, __builtin_fmaf(s * q, t, s), x < 0.f ? 0.f : x);
     const float p = __builtin_amdgcn_rcpf(1.f + e);
     slope = x >= 0.f ? p : e * p;
 }

@@ -26,6 +26,8 @@
 // and c) are halved three times by exchanges that leave each lane half of the values,
 // and joined with those of 7 more tokens, two instructions for a value of 64 lanes; the
 // workgroups' sums are added by another kernel in order.
+#include <type_traits>
+
 #include "block_common.hpp"
 
 namespace snn {
@@ -33,7 +35,6 @@ namespace {
 
 constexpr int kTile = kSelscanTile;  // tokens
 constexpr int kLanes = 64;           // channels of a workgroup
-constexpr int kHold = 4;             // integrators of a wave
 
 // Where this workgroup works.
 struct Place {
@@ -58,31 +59,107 @@ __device__ inline int length_of(const Selscan &a, int b) {
     return a.lens ? min(max(a.lens[b], 0), a.T) : a.T;
 }
 
-// b or c of a tile: thread (token, integrator) holds one value of each 4 W of them
-template <typename T, int W>
-__device__ inline float vec_value(const SelscanVec &v, int t, int b, int g, int i, bool in) {
-    return in ? (float)static_cast<const T *>(v.p)[t * v.st + b * v.sb + g * v.sg + i] : 0.f;
+// b or c of a token and integrator, not yet converted (that would wait for the load)
+template <typename T>
+__device__ inline T vec_value(const SelscanVec &v, int t, int b, int g, int i) {
+    return static_cast<const T *>(v.p)[t * v.st + b * v.sb + g * v.sg + i];
+}
+// EL values of a row, all of a workgroup's 64 channels there or only m of these
+template <typename T, int EL>
+__device__ inline void fetch_run(Raw<T, EL> &r, const SelscanRows &x, int t, const Place &p, int se,
+                                 int m) {
+    const T *at = static_cast<const T *>(x.p) + t * x.st + p.b * x.sb + p.c0 + se;
+    if (p.live == kLanes) __builtin_memcpy(r.w, at, sizeof(r.w));
+    else r.load(at, m);
 }
 
-template <int W>
+// raw steps and their bias to steps, the condition outside the loop: one stretch of
+// code in which the elements' chains overlap
+template <int EL>
+__device__ inline void steps(int soft, float (&d)[EL], const float (&bias)[EL]) {
+#pragma unroll
+    for (int j = 0; j < EL; ++j) d[j] += bias[j];
+    if (soft)
+#pragma unroll
+        for (int j = 0; j < EL; ++j) {
+            float slope;
+            softplus(d[j], d[j], slope);
+        }
+}
+
+// W waves of 64 channels, each with H integrators of them at once.
+template <int W, int H>
 struct Geo {
     static constexpr int kThreads = kLanes * W;
-    static constexpr int kRow = 4 * W;           // threads of a token, and integrators at once
-    static constexpr int kEl = kLanes / kRow;    // channels of a staging thread
+    static constexpr int kTok = 4 * W;           // threads that stage a token
+    static constexpr int kEl = kLanes / kTok;    // channels of such a thread
+    static constexpr int kRow = W * H;           // integrators at once
+    static constexpr int kSlots = 2 * H;         // values of b and c for a wave and token
 };
+
+// b and c of a tile for a wave, 16 values to a register: token t's are the 2 H from
+// 2 H t on.  Every lane wants the same ones; a register read with its lanes' own 16
+// values (a quarter of the LDS traffic of a broadcast read) and the operand of an
+// instruction that takes one lane of 16 for all of them.
+template <int H>
+using Vecs = float[kTile * H / 8][16];
+
+template <int N, int I = 0, typename F>
+__device__ inline void each(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, I + 1>(f);
+    }
+}
+template <int L>
+__device__ inline float lane_of16(float v) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + L, 0xf, 0xf, true));
+}
+// acc + (lane L of 16 of v) x.  The wait is for a v that the instruction before wrote.
+template <int L>
+__device__ inline void fma_lane(float &acc, float v, float x) {
+    asm("s_nop 1\n\tv_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf"
+        : "+v"(acc)
+        : "v"(v), "v"(x), "n"(L));
+}
+// sum over k of (lane L + k of 16 of v) x[k]
+template <int L>
+__device__ inline float dot_lanes(float v, const float (&x)[4]) {
+    float r;
+    asm("s_nop 1\n\t"
+        "v_mul_f32_dpp %0, %1, %2 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
+        : "=&v"(r)
+        : "v"(v), "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "n"(L), "n"(L + 1), "n"(L + 2),
+          "n"(L + 3));
+    return r;
+}
+template <int L>
+__device__ inline float dot_lanes(float v, const float (&x)[2]) {
+    float r;
+    asm("s_nop 1\n\t"
+        "v_mul_f32_dpp %0, %1, %2 row_newbcast:%4 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%5 row_mask:0xf bank_mask:0xf"
+        : "=&v"(r)
+        : "v"(v), "v"(x[0]), "v"(x[1]), "n"(L), "n"(L + 1));
+    return r;
+}
 
 // OUT: outputs (and saved states), from a.slot's or the caller's start; else the end
 // state from zero and the sum of the steps, into a.slot and a.sums.
-template <typename T, int W, bool MANY, bool OUT>
-__global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
-    using G = Geo<W>;
-    constexpr int EL = G::kEl, ROW = G::kRow, MOST = MANY ? kSelscanMaxStates : ROW;
+template <typename T, int W, int H, bool MANY, bool OUT>
+__global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
+    using G = Geo<W, H>;
+    constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
+    constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
     __shared__ float2 sd[kTile][kLanes];
-    __shared__ __attribute__((aligned(16))) float sb[kTile][MOST], sc[OUT ? kTile : 1][MOST];
+    __shared__ Vecs<H> vecs[RND][W];
     __shared__ float yp[OUT ? W : 1][kTile][kLanes];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int st = tid / ROW, se = tid % ROW * EL, si = tid % ROW;  // staging
+    const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;  // staging
     const Place p = place_of(a, OUT ? a.segs : a.segs - 1);
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
     const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
@@ -92,11 +169,11 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
     const float *first = OUT && a.segs > 1
                              ? a.slot + (int64_t)p.seg * a.B * a.N * a.n
                              : OUT ? a.state_in : nullptr;
-    float h[kHold], a2[kHold];
-    auto state = [&](int r, int k) { return r * ROW + w * kHold + k; };
+    float h[H], a2[H];
+    auto state = [&](int r, int k) { return r * ROW + w * H + k; };
     auto load_round = [&](int r) {
 #pragma unroll
-        for (int k = 0; k < kHold; ++k) {
+        for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             const bool in = on && i < a.N;
             a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
@@ -107,7 +184,7 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
         for (int r = 0; r < rounds; ++r) {
             load_round(r);
 #pragma unroll
-            for (int k = 0; k < kHold; ++k) carry[state(r, k)][lane] = h[k];
+            for (int k = 0; k < H; ++k) carry[state(r, k)][lane] = h[k];
         }
     } else {
         load_round(0);
@@ -120,22 +197,21 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
         sum[j] = 0.f;
     }
     Raw<T, EL> ru, rd, rz;
-    float rb[MANY ? kSelscanMaxStates / ROW : 1], rc[MANY ? kSelscanMaxStates / ROW : 1];
+    T rb[RND], rc[RND];
+    const int stop = min(end, len);
     auto fetch = [&](int t0) {
-        const int t = t0 + st, k = t < len && t < end ? m : 0;
-        const bool in = t < len && t < end;
-        ru.load(static_cast<const T *>(a.u.p) + t * a.u.st + p.b * a.u.sb + p.c0 + se, k);
-        rd.load(static_cast<const T *>(a.dt.p) + t * a.dt.st + p.b * a.dt.sb + p.c0 + se, k);
-        if (OUT && a.z.p)
-            rz.load(static_cast<const T *>(a.z.p) + t * a.z.st + p.b * a.z.sb + p.c0 + se, k);
+        // past the end the last token again, which the staging leaves out
+        const int t = min(t0 + st, stop - 1);
+        fetch_run(ru, a.u, t, p, se, m);
+        fetch_run(rd, a.dt, t, p, se, m);
+        if (OUT && a.z.p) fetch_run(rz, a.z, t, p, se, m);
 #pragma unroll
-        for (int r = 0; r < (MANY ? kSelscanMaxStates / ROW : 1); ++r) {
-            const int i = r * ROW + si;
-            rb[r] = vec_value<T, W>(a.b, t, p.b, p.g, i, in && i < a.N);
-            if (OUT) rc[r] = vec_value<T, W>(a.c, t, p.b, p.g, i, in && i < a.N);
+        for (int r = 0; r < RND; ++r) {
+            const int i = min(r * ROW + si, a.N - 1);
+            rb[r] = vec_value<T>(a.b, t, p.b, p.g, i);
+            if (OUT) rc[r] = vec_value<T>(a.c, t, p.b, p.g, i);
         }
     };
-    const int stop = min(end, len);
     if (begin < stop) fetch(begin);
     for (int t0 = begin; t0 < stop; t0 += kTile) {
         float u[EL], z[EL], d[EL];
@@ -143,25 +219,28 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
         ru.get(u);
         rd.get(d);
         if (OUT && a.z.p) rz.get(z);
+        steps<EL>(a.softplus, d, bias);
 #pragma unroll
         for (int j = 0; j < EL; ++j) {
-            float v = d[j] + bias[j], s;
-            if (a.softplus) softplus(v, v, s);
-            d[j] = in && j < m ? v : 0.f;
-            sd[st][se + j] = make_float2(d[j], d[j] * u[j]);
+            d[j] = in && j < m ? d[j] : 0.f;
+            sd[st][se + j] = make_float2(d[j], in ? d[j] * u[j] : 0.f);
             sum[j] += d[j];
         }
 #pragma unroll
-        for (int r = 0; r < (MANY ? kSelscanMaxStates / ROW : 1); ++r) {
-            sb[st][r * ROW + si] = rb[r];
-            if (OUT) sc[st][r * ROW + si] = rc[r];
+        for (int r = 0; r < RND; ++r) {
+            if (si < ROW) {
+                float *v = &vecs[r][si / H][0][0] + st * G::kSlots + si % H;
+                const bool there = in && r * ROW + si < a.N;
+                v[0] = there ? (float)rb[r] : 0.f;
+                if (OUT) v[H] = there ? (float)rc[r] : 0.f;
+            }
         }
         if (t0 + kTile < stop) fetch(t0 + kTile);
         __syncthreads();
         for (int r = 0; r < (MANY ? rounds : 1); ++r) {
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < kHold; ++k) {
+                for (int k = 0; k < H; ++k) {
                     const int i = state(r, k);
                     a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
                     h[k] = carry[i][lane];
@@ -170,25 +249,27 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
             if (OUT && a.saved) {
                 float *s = a.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase;
 #pragma unroll
-                for (int k = 0; k < kHold; ++k)
+                for (int k = 0; k < H; ++k)
                     if (on && state(r, k) < a.N) s[(int64_t)state(r, k) * a.n] = h[k];
             }
-            const int i0 = state(r, 0);
-#pragma unroll
-            for (int t = 0; t < kTile; ++t) {
+            float vr = 0.f;
+            each<kTile>([&](auto tt) {
+                constexpr int t = decltype(tt)::value, at = t * G::kSlots % 16;
+                if constexpr (at == 0) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
                 const float2 v = sd[t][lane];
-                float y = 0.f;
-#pragma unroll
-                for (int k = 0; k < kHold; ++k) {
+                each<H>([&](auto kk) {
+                    constexpr int k = decltype(kk)::value;
                     const float e = __builtin_amdgcn_exp2f(v.x * a2[k]);
-                    h[k] = __builtin_fmaf(e, h[k], v.y * sb[t][i0 + k]);
-                    if (OUT) y = __builtin_fmaf(sc[t][i0 + k], h[k], y);
+                    h[k] = __builtin_fmaf(e, h[k], v.y * lane_of16<at + k>(vr));
+                });
+                if constexpr (OUT) {
+                    const float y = dot_lanes<at + H>(vr, h);
+                    yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
                 }
-                if (OUT) yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
-            }
+            });
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < kHold; ++k) carry[state(r, k)][lane] = h[k];
+                for (int k = 0; k < H; ++k) carry[state(r, k)][lane] = h[k];
             }
         }
         __syncthreads();
@@ -200,9 +281,12 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
 #pragma unroll
                 for (int k = 1; k < W; ++k) y[j] += yp[k][st][se + j];
                 y[j] = __builtin_fmaf(skip[j], u[j], y[j]);
-                if (a.z.p) y[j] *= silu(z[j]);
-                if (!in) y[j] = 0.f;
             }
+            if (a.z.p)
+#pragma unroll
+                for (int j = 0; j < EL; ++j) y[j] *= silu<sizeof(T) == 4>(z[j]);
+#pragma unroll
+            for (int j = 0; j < EL; ++j) y[j] = in ? y[j] : 0.f;
             if (t0 + st < end)
                 store_run(static_cast<T *>(a.y) + (t0 + st) * a.y_st + p.b * a.y_sb + p.c0 + se, m,
                           y);
@@ -220,7 +304,7 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_kernel(Selscan a) {
     if (last)
         for (int r = 0; r < (MANY ? rounds : 1); ++r)
 #pragma unroll
-            for (int k = 0; k < kHold; ++k) {
+            for (int k = 0; k < H; ++k) {
                 const int i = state(r, k);
                 if (on && i < a.N)
                     last[sbase + (int64_t)i * a.n] = MANY ? carry[i][lane] : h[k];
@@ -287,19 +371,19 @@ __device__ inline float halve(float x, float y) {
     }
 }
 
-template <typename T, int W, bool MANY>
-__global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_kernel(SelscanBwd q) {
-    using G = Geo<W>;
+template <typename T, int W, int H, bool MANY>
+__global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(SelscanBwd q) {
+    using G = Geo<W, H>;
     const Selscan &a = q.a;
-    constexpr int EL = G::kEl, ROW = G::kRow, MOST = MANY ? kSelscanMaxStates : ROW;
+    constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
     __shared__ float sd[kTile][kLanes], su[kTile][kLanes], sg[kTile][kLanes];
-    __shared__ __attribute__((aligned(16))) float sb[kTile][MOST], sc[kTile][MOST];
+    __shared__ Vecs<H> vecs[RND][W];
     __shared__ float yp[W][kTile][kLanes], up[W][kTile][kLanes], dp[W][kTile][kLanes];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     __shared__ float asum[MANY ? kSelscanMaxStates : 1][kLanes];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int st = tid / ROW, se = tid % ROW * EL, si = tid % ROW;
+    const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;
     const Place p = place_of(a, a.segs);
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
     const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
@@ -308,11 +392,11 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
     const bool on = lane < p.live;
     const float *first = a.segs > 1 ? a.slot + (int64_t)p.seg * a.B * a.N * a.n
                                     : q.grad_state_out;
-    float g[kHold], a2[kHold], acc[kHold];
-    auto state = [&](int r, int k) { return r * ROW + w * kHold + k; };
+    float g[H], a2[H], acc[H];
+    auto state = [&](int r, int k) { return r * ROW + w * H + k; };
     for (int r = 0; r < (MANY ? rounds : 1); ++r)
 #pragma unroll
-        for (int k = 0; k < kHold; ++k) {
+        for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             const bool in = on && i < a.N;
             a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
@@ -322,22 +406,20 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
         }
     float gskip[EL] = {}, gbias[EL] = {};
     Raw<T, EL> ru, rd, rz, rg;
-    float rb[RND], rc[RND];
+    T rb[RND], rc[RND];
     const int stop = min(end, len);
+    const SelscanRows gy_rows{q.gy, a.y_st, a.y_sb};
     auto fetch = [&](int t0) {
-        const int t = t0 + st;
-        const bool in = t < stop;
-        const int k = in ? m : 0;
-        ru.load(static_cast<const T *>(a.u.p) + t * a.u.st + p.b * a.u.sb + p.c0 + se, k);
-        rd.load(static_cast<const T *>(a.dt.p) + t * a.dt.st + p.b * a.dt.sb + p.c0 + se, k);
-        rg.load(static_cast<const T *>(q.gy) + t * a.y_st + p.b * a.y_sb + p.c0 + se, k);
-        if (a.z.p)
-            rz.load(static_cast<const T *>(a.z.p) + t * a.z.st + p.b * a.z.sb + p.c0 + se, k);
+        const int t = min(t0 + st, stop - 1);
+        fetch_run(ru, a.u, t, p, se, m);
+        fetch_run(rd, a.dt, t, p, se, m);
+        fetch_run(rg, gy_rows, t, p, se, m);
+        if (a.z.p) fetch_run(rz, a.z, t, p, se, m);
 #pragma unroll
         for (int r = 0; r < RND; ++r) {
-            const int i = r * ROW + si;
-            rb[r] = vec_value<T, W>(a.b, t, p.b, p.g, i, in && i < a.N);
-            rc[r] = vec_value<T, W>(a.c, t, p.b, p.g, i, in && i < a.N);
+            const int i = min(r * ROW + si, a.N - 1);
+            rb[r] = vec_value<T>(a.b, t, p.b, p.g, i);
+            rc[r] = vec_value<T>(a.c, t, p.b, p.g, i);
         }
     };
     const float none[EL] = {};
@@ -358,38 +440,57 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
         const bool in = t0 + st < stop;
         float u[EL], slope[EL], zs[EL] = {};  // zs: gradient of the gate's input over y
         {
-            float d[EL], gy[EL];
+            float d[EL], gy[EL], bias[EL] = {};
+            if (a.dt_bias) load_run(a.dt_bias + p.c0 + se, m, bias);
             ru.get(u);
             rd.get(d);
             rg.get(gy);
             if (a.z.p) rz.get(zs);
 #pragma unroll
             for (int j = 0; j < EL; ++j) {
-                float v = d[j] + (j < m && a.dt_bias ? a.dt_bias[p.c0 + se + j] : 0.f);
                 slope[j] = 1.f;
-                if (a.softplus) softplus(v, v, slope[j]);
-                v = in && j < m ? v : 0.f;
-                float act = 1.f;
-                if (a.z.p) silu_slope(zs[j], act, zs[j]);
-                sd[st][se + j] = v;
-                su[st][se + j] = v * u[j];
-                sg[st][se + j] = gy[j] * act;
-                zs[j] *= gy[j];
+                d[j] += bias[j];
+            }
+            if (a.softplus)
+#pragma unroll
+                for (int j = 0; j < EL; ++j) softplus(d[j], d[j], slope[j]);
+            float gi[EL];
+#pragma unroll
+            for (int j = 0; j < EL; ++j) gi[j] = gy[j];
+            if (a.z.p)
+#pragma unroll
+                for (int j = 0; j < EL; ++j) {
+                    float act;
+                    silu_slope<sizeof(T) == 4>(zs[j], act, zs[j]);
+                    gi[j] *= act;
+                    zs[j] *= gy[j];
+                }
+#pragma unroll
+            for (int j = 0; j < EL; ++j) {
+                d[j] = in && j < m ? d[j] : 0.f;
+                sd[st][se + j] = d[j];
+                u[j] = in ? u[j] : 0.f;
+                su[st][se + j] = d[j] * u[j];
+                sg[st][se + j] = in ? gi[j] : 0.f;
             }
         }
 #pragma unroll
         for (int r = 0; r < RND; ++r) {
-            sb[st][r * ROW + si] = rb[r];
-            sc[st][r * ROW + si] = rc[r];
+            if (si < ROW) {
+                float *v = &vecs[r][si / H][0][0] + st * G::kSlots + si % H;
+                const bool there = in && r * ROW + si < a.N;
+                v[0] = there ? (float)rb[r] : 0.f;
+                v[H] = there ? (float)rc[r] : 0.f;
+            }
         }
         if (x > 0) fetch(t0 - kTile);
         __syncthreads();
         for (int r = 0; r < (MANY ? rounds : 1); ++r) {
             const int i0 = state(r, 0);
-            float h0[kHold], h[kTile][kHold], e[kTile][kHold];
+            float h0[H], h[kTile][H], e[kTile][H];
             const float *s = q.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase;
 #pragma unroll
-            for (int k = 0; k < kHold; ++k) {
+            for (int k = 0; k < H; ++k) {
                 h0[k] = on && i0 + k < a.N ? s[(int64_t)(i0 + k) * a.n] : 0.f;
                 if (MANY) {
                     a2[k] = on && i0 + k < a.N
@@ -399,72 +500,83 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
                     acc[k] = asum[i0 + k][lane];
                 }
             }
-#pragma unroll
-            for (int t = 0; t < kTile; ++t) {
+            float vr = 0.f;
+            each<kTile>([&](auto tt) {
+                constexpr int t = decltype(tt)::value, at = t * G::kSlots % 16;
+                if constexpr (at == 0) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
                 const float dv = sd[t][lane], uv = su[t][lane];
-                float y = 0.f;
-#pragma unroll
-                for (int k = 0; k < kHold; ++k) {
+                each<H>([&](auto kk) {
+                    constexpr int k = decltype(kk)::value;
                     e[t][k] = __builtin_amdgcn_exp2f(dv * a2[k]);
-                    h[t][k] = __builtin_fmaf(e[t][k], t ? h[t - 1][k] : h0[k],
-                                             uv * sb[t][i0 + k]);
-                    y = __builtin_fmaf(sc[t][i0 + k], h[t][k], y);
+                    h[t][k] = __builtin_fmaf(e[t][k], t ? h[t ? t - 1 : 0][k] : h0[k],
+                                             uv * lane_of16<at + k>(vr));
+                });
+                if (a.z.p) {
+                    const float y = dot_lanes<at + H>(vr, h[t]);
+                    yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
                 }
-                if (a.z.p) yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
                 __builtin_amdgcn_sched_barrier(0);
-            }
-            float part[3];
-#pragma unroll
-            for (int t = kTile - 1; t >= 0; --t) {
+            });
+            float part[4];
+            each<kTile>([&](auto tt) {
+                constexpr int t = kTile - 1 - decltype(tt)::value, at = t * G::kSlots % 16;
                 __builtin_amdgcn_sched_barrier(0);
+                if constexpr (at + G::kSlots == 16) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
                 const float dv = sd[t][lane], uv = su[t][lane], gv = sg[t][lane];
-                float gin = 0.f, gd = 0.f, vb[kHold], vc[kHold];
-#pragma unroll
-                for (int k = 0; k < kHold; ++k) {
-                    const float full = __builtin_fmaf(sc[t][i0 + k], gv, g[k]);
+                float gd = 0.f, vb[H], vc[H];
+                each<H>([&](auto kk) {
+                    constexpr int k = decltype(kk)::value;
+                    fma_lane<at + H + k>(g[k], vr, gv);
                     vc[k] = gv * h[t][k];
-                    vb[k] = full * uv;
-                    gin = __builtin_fmaf(full, sb[t][i0 + k], gin);
-                    g[k] = e[t][k] * full;
-                    const float x_ = g[k] * (t ? h[t - 1][k] : h0[k]);
+                    vb[k] = g[k] * uv;
+                });
+                const float gin = dot_lanes<at>(vr, g);
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                    g[k] *= e[t][k];
+                    const float x_ = g[k] * (t ? h[t ? t - 1 : 0][k] : h0[k]);
                     acc[k] = __builtin_fmaf(x_, dv, acc[k]);
                     gd = __builtin_fmaf(x_, a2[k], gd);
                 }
                 up[w][t][lane] = MANY && r ? up[w][t][lane] + gin : gin;
                 dp[w][t][lane] = MANY && r ? dp[w][t][lane] + gd : gd;
-                // bits of the lane: 32 b or c, 16 and 8 the integrator's, 4, 2, 1 the
-                // token's (1, 2, 4 of 8)
-                float v = halve<8>(halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[2], vc[2])),
-                                   halve<16>(halve<32>(vb[1], vc[1]), halve<32>(vb[3], vc[3])));
-                if (t & 1) {
-                    part[0] = v;
-                    continue;
+                // The sums over lanes.  Bits of the lane that a sum ends in: 32 b or c, then
+                // the integrator's from the high one on (16 and 8; 16), then the token's
+                // from the low one on.  Tokens are joined in pairs, fours and so on.
+                float v;
+                if constexpr (H == 4)
+                    v = halve<8>(halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[2], vc[2])),
+                                 halve<16>(halve<32>(vb[1], vc[1]), halve<32>(vb[3], vc[3])));
+                else
+                    v = halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[1], vc[1]));
+                each<H == 4 ? 3 : 4>([&](auto ll) {
+                    constexpr int l = decltype(ll)::value, bit = (H == 4 ? 4 : 8) >> l;
+                    if constexpr ((t & ((1 << l) - 1)) == 0) {
+                        if constexpr (t >> l & 1) part[l] = v;
+                        else v = halve<bit>(v, part[l]);
+                    }
+                });
+                if constexpr (t % (H == 4 ? 8 : 16) == 0) {
+                    const int i = i0 + (H == 4 ? lane >> 3 & 3 : lane >> 4 & 1);
+                    const int tt_ = t0 + t + (H == 4 ? (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4
+                                                     : (lane >> 3 & 1) + (lane >> 1 & 2) +
+                                                           (lane << 1 & 4) + (lane & 1) * 8);
+                    const int per = a.tiles / a.groups;
+                    if (tt_ < stop && i < a.N)
+                        q.vec[((((int64_t)(lane >> 5) * per + p.tile % per) * a.T + tt_) * a.B +
+                               p.b) * a.groups * a.N +
+                              p.g * a.N + i] = v;
                 }
-                v = halve<4>(v, part[0]);
-                if (t & 2) {
-                    part[1] = v;
-                    continue;
-                }
-                v = halve<2>(v, part[1]);
-                if (t & 4) {
-                    part[2] = v;
-                    continue;
-                }
-                v = halve<1>(v, part[2]);
-                const int tt = t0 + t + (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4;
-                const int i = i0 + (lane >> 3 & 3), per = a.tiles / a.groups;
-                if (tt < stop && i < a.N)
-                    q.vec[((((int64_t)(lane >> 5) * per + p.tile % per) * a.T + tt) * a.B + p.b) *
-                              a.groups * a.N +
-                          p.g * a.N + i] = v;
-            }
+            });
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < kHold; ++k) carry[i0 + k][lane] = g[k], asum[i0 + k][lane] = acc[k];
+                for (int k = 0; k < H; ++k) carry[i0 + k][lane] = g[k], asum[i0 + k][lane] = acc[k];
             }
         }
         __syncthreads();
         float gu[EL], gdt[EL];
+        float skip[EL] = {};
+        if (a.skip) load_run(a.skip + p.c0 + se, m, skip);
 #pragma unroll
         for (int j = 0; j < EL; ++j) {
             float y = a.z.p ? yp[0][st][se + j] : 0.f, gin = up[0][st][se + j],
@@ -476,10 +588,9 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
                 gd += dp[k][st][se + j];
             }
             const float d = sd[st][se + j], gi = sg[st][se + j];
-            const float skip = a.skip && j < m ? a.skip[p.c0 + se + j] : 0.f;
-            gu[j] = __builtin_fmaf(gin, d, gi * skip);
+            gu[j] = __builtin_fmaf(gin, d, gi * skip[j]);
             gdt[j] = in ? __builtin_fmaf(gin, u[j], gd * kLn2) * slope[j] : 0.f;
-            zs[j] *= __builtin_fmaf(skip, u[j], y);
+            zs[j] *= __builtin_fmaf(skip[j], u[j], y);
             gskip[j] = __builtin_fmaf(gi, u[j], gskip[j]);
             gbias[j] += gdt[j];
         }
@@ -494,7 +605,7 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
     float *rows = q.part + ((int64_t)p.b * a.segs + p.seg) * (a.N + 2) * a.n + p.c0 + lane;
     for (int r = 0; r < (MANY ? rounds : 1); ++r)
 #pragma unroll
-        for (int k = 0; k < kHold; ++k) {
+        for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             if (on && i < a.N) {
                 if (last) last[sbase + (int64_t)i * a.n] = MANY ? carry[i][lane] : g[k];
@@ -515,17 +626,17 @@ __global__ __launch_bounds__(Geo<W>::kThreads, MANY ? 1 : 2) void selscan_bwd_ke
 
 // The gradient that a segment passes on from its own tokens, and the sum of its steps:
 // segments 1 .. segs - 1.
-template <typename T, int W, bool MANY>
-__global__ __launch_bounds__(Geo<W>::kThreads) void selscan_back_kernel(SelscanBwd q) {
-    using G = Geo<W>;
+template <typename T, int W, int H, bool MANY>
+__global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) {
+    using G = Geo<W, H>;
     const Selscan &a = q.a;
-    constexpr int EL = G::kEl, ROW = G::kRow, MOST = MANY ? kSelscanMaxStates : ROW;
+    constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
     __shared__ float2 sd[kTile][kLanes];
-    __shared__ __attribute__((aligned(16))) float sc[kTile][MOST];
+    __shared__ Vecs<H> vecs[RND][W];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int st = tid / ROW, se = tid % ROW * EL, si = tid % ROW;
+    const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;
     Place p = place_of(a, a.segs - 1);
     p.seg += 1;
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
@@ -533,18 +644,18 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_back_kernel(SelscanB
     const int m = min(EL, max(0, p.live - se));
     const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;
     const bool on = lane < p.live;
-    float g[kHold], a2[kHold];
-    auto state = [&](int r, int k) { return r * ROW + w * kHold + k; };
+    float g[H], a2[H];
+    auto state = [&](int r, int k) { return r * ROW + w * H + k; };
     auto rates = [&](int r) {
 #pragma unroll
-        for (int k = 0; k < kHold; ++k) {
+        for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
         }
     };
     rates(0);
 #pragma unroll
-    for (int k = 0; k < kHold; ++k) g[k] = 0.f;
+    for (int k = 0; k < H; ++k) g[k] = 0.f;
     if (MANY)
         for (int i = w; i < kSelscanMaxStates; i += W) carry[i][lane] = 0.f;
     float bias[EL], sum[EL];
@@ -554,21 +665,17 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_back_kernel(SelscanB
         sum[j] = 0.f;
     }
     Raw<T, EL> rd, rz, rg;
-    float rc[RND];
+    T rc[RND];
     const int stop = min(end, len);
+    const SelscanRows gy_rows{q.gy, a.y_st, a.y_sb};
     auto fetch = [&](int t0) {
-        const int t = t0 + st;
-        const bool in = t < stop;
-        const int k = in ? m : 0;
-        rd.load(static_cast<const T *>(a.dt.p) + t * a.dt.st + p.b * a.dt.sb + p.c0 + se, k);
-        rg.load(static_cast<const T *>(q.gy) + t * a.y_st + p.b * a.y_sb + p.c0 + se, k);
-        if (a.z.p)
-            rz.load(static_cast<const T *>(a.z.p) + t * a.z.st + p.b * a.z.sb + p.c0 + se, k);
+        const int t = min(t0 + st, stop - 1);
+        fetch_run(rd, a.dt, t, p, se, m);
+        fetch_run(rg, gy_rows, t, p, se, m);
+        if (a.z.p) fetch_run(rz, a.z, t, p, se, m);
 #pragma unroll
-        for (int r = 0; r < RND; ++r) {
-            const int i = r * ROW + si;
-            rc[r] = vec_value<T, W>(a.c, t, p.b, p.g, i, in && i < a.N);
-        }
+        for (int r = 0; r < RND; ++r)
+            rc[r] = vec_value<T>(a.c, t, p.b, p.g, min(r * ROW + si, a.N - 1));
     };
     const int tiles = begin < stop ? (stop - begin + kTile - 1) / kTile : 0;
     if (tiles > 0) fetch(begin + (tiles - 1) * kTile);
@@ -580,16 +687,21 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_back_kernel(SelscanB
         rg.get(gy);
         if (a.z.p) rz.get(z);
         __syncthreads();  // the tile before has been read
+        steps<EL>(a.softplus, d, bias);
+        if (a.z.p)
+#pragma unroll
+            for (int j = 0; j < EL; ++j) gy[j] *= silu<sizeof(T) == 4>(z[j]);
 #pragma unroll
         for (int j = 0; j < EL; ++j) {
-            float v = d[j] + bias[j], s;
-            if (a.softplus) softplus(v, v, s);
-            v = in && j < m ? v : 0.f;
-            sd[st][se + j] = make_float2(v, a.z.p ? gy[j] * silu(z[j]) : gy[j]);
-            sum[j] += v;
+            d[j] = in && j < m ? d[j] : 0.f;
+            sd[st][se + j] = make_float2(d[j], in ? gy[j] : 0.f);
+            sum[j] += d[j];
         }
 #pragma unroll
-        for (int r = 0; r < RND; ++r) sc[st][r * ROW + si] = rc[r];
+        for (int r = 0; r < RND; ++r)
+            if (si < ROW)
+                (&vecs[r][si / H][0][0])[st * G::kSlots + H + si % H] =
+                    in && r * ROW + si < a.N ? (float)rc[r] : 0.f;
         if (x > 0) fetch(t0 - kTile);
         __syncthreads();
         for (int r = 0; r < (MANY ? rounds : 1); ++r) {
@@ -597,25 +709,28 @@ __global__ __launch_bounds__(Geo<W>::kThreads) void selscan_back_kernel(SelscanB
             if (MANY) {
                 rates(r);
 #pragma unroll
-                for (int k = 0; k < kHold; ++k) g[k] = carry[i0 + k][lane];
+                for (int k = 0; k < H; ++k) g[k] = carry[i0 + k][lane];
             }
-#pragma unroll
-            for (int t = kTile - 1; t >= 0; --t) {
+            float vr = 0.f;
+            each<kTile>([&](auto tt) {
+                constexpr int t = kTile - 1 - decltype(tt)::value, at = t * G::kSlots % 16;
+                if constexpr (at + G::kSlots == 16) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
                 const float2 v = sd[t][lane];
-#pragma unroll
-                for (int k = 0; k < kHold; ++k)
-                    g[k] = __builtin_amdgcn_exp2f(v.x * a2[k]) *
-                           __builtin_fmaf(sc[t][i0 + k], v.y, g[k]);
-            }
+                each<H>([&](auto kk) {
+                    constexpr int k = decltype(kk)::value;
+                    fma_lane<at + H + k>(g[k], vr, v.y);
+                    g[k] *= __builtin_amdgcn_exp2f(v.x * a2[k]);
+                });
+            });
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < kHold; ++k) carry[i0 + k][lane] = g[k];
+                for (int k = 0; k < H; ++k) carry[i0 + k][lane] = g[k];
             }
         }
     }
     for (int r = 0; r < (MANY ? rounds : 1); ++r)
 #pragma unroll
-        for (int k = 0; k < kHold; ++k) {
+        for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             if (on && i < a.N)
                 a.slot[(int64_t)p.seg * a.B * a.N * a.n + sbase + (int64_t)i * a.n] =
@@ -727,34 +842,34 @@ __global__ __launch_bounds__(256) void selscan_step_kernel(Selscan a, const int3
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         out[j] = __builtin_fmaf(sk[j], u[j], out[j]);
-        if (a.z.p) out[j] *= silu(z[j]);
+        if (a.z.p) out[j] *= silu<sizeof(T) == 4>(z[j]);
     }
     store_run(y, m, out);
 }
 
-template <typename T, int W, bool MANY>
+template <typename T, int W, int H, bool MANY>
 hipError_t run_fwd(const Selscan &a, hipStream_t s) {
-    const int units = a.tiles * a.B, threads = Geo<W>::kThreads;
+    const int units = a.tiles * a.B, threads = Geo<W, H>::kThreads;
     if (a.segs > 1) {
-        selscan_kernel<T, W, MANY, false><<<units * (a.segs - 1), threads, 0, s>>>(a);
+        selscan_kernel<T, W, H, MANY, false><<<units * (a.segs - 1), threads, 0, s>>>(a);
         const int64_t size = (int64_t)a.B * a.N * a.n;
         selscan_join_kernel<<<(unsigned)((size + 255) / 256), 256, 0, s>>>(a, a.state_in, false);
     }
-    selscan_kernel<T, W, MANY, true><<<units * a.segs, threads, 0, s>>>(a);
+    selscan_kernel<T, W, H, MANY, true><<<units * a.segs, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int W, bool MANY>
+template <typename T, int W, int H, bool MANY>
 hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
     const Selscan &a = q.a;
-    const int units = a.tiles * a.B, threads = Geo<W>::kThreads;
+    const int units = a.tiles * a.B, threads = Geo<W, H>::kThreads;
     if (units > 0 && a.segs > 1) {
-        selscan_back_kernel<T, W, MANY><<<units * (a.segs - 1), threads, 0, s>>>(q);
+        selscan_back_kernel<T, W, H, MANY><<<units * (a.segs - 1), threads, 0, s>>>(q);
         const int64_t size = (int64_t)a.B * a.N * a.n;
         selscan_join_kernel<<<(unsigned)((size + 255) / 256), 256, 0, s>>>(a, q.grad_state_out,
                                                                           true);
     }
-    if (units > 0) selscan_bwd_kernel<T, W, MANY><<<units * a.segs, threads, 0, s>>>(q);
+    if (units > 0) selscan_bwd_kernel<T, W, H, MANY><<<units * a.segs, threads, 0, s>>>(q);
     const int64_t per = (int64_t)a.T * a.B * a.groups * a.N;
     if (per > 0)
         selscan_vec_kernel<T><<<dim3((unsigned)((per + 255) / 256), 2), 256, 0, s>>>(q);
@@ -766,17 +881,17 @@ hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
 
 template <typename T>
 hipError_t by_states(const Selscan &a, hipStream_t s) {
-    if (a.N <= 4) return run_fwd<T, 1, false>(a, s);
-    if (a.N <= 8) return run_fwd<T, 2, false>(a, s);
-    if (a.N <= 16) return run_fwd<T, 4, false>(a, s);
-    return run_fwd<T, 4, true>(a, s);
+    if (a.N <= 4) return run_fwd<T, 1, 4, false>(a, s);
+    if (a.N <= 8) return run_fwd<T, 2, 4, false>(a, s);
+    if (a.N <= 16) return run_fwd<T, 4, 4, false>(a, s);
+    return run_fwd<T, 4, 4, true>(a, s);
 }
 template <typename T>
 hipError_t by_states(const SelscanBwd &q, hipStream_t s) {
-    if (q.a.N <= 4) return run_bwd<T, 1, false>(q, s);
-    if (q.a.N <= 8) return run_bwd<T, 2, false>(q, s);
-    if (q.a.N <= 16) return run_bwd<T, 4, false>(q, s);
-    return run_bwd<T, 4, true>(q, s);
+    if (q.a.N <= 4) return run_bwd<T, 1, 4, false>(q, s);
+    if (q.a.N <= 8) return run_bwd<T, 2, 4, false>(q, s);
+    if (q.a.N <= 16) return run_bwd<T, 4, 4, false>(q, s);
+    return run_bwd<T, 4, 4, true>(q, s);
 }
 
 template <typename T>

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void shortconv_kernel(Shortconv a, int ti
                 float s = bias[e];
 #pragma unroll
                 for (int j = 0; j < K; ++j) s = __builtin_fmaf(w[j][e], win[j][e], s);
-                out[e] = t < len ? (a.silu ? silu(s) : s) : 0.f;
+                out[e] = t < len ? (a.silu ? silu<sizeof(T) == 4>(s) : s) : 0.f;
             }
             store_run(y + t * a.y_st, p.m, out);
         }
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void shortconv_bwd_kernel(ShortconvBwd q,
                     float s = bias[e], act, slope;
 #pragma unroll
                     for (int j = 0; j < K; ++j) s = __builtin_fmaf(w[j][e], win[j][e], s);
-                    silu_slope(s, act, slope);
+                    silu_slope<sizeof(T) == 4>(s, act, slope);
                     g[e] *= slope;
                 }
                 if (t >= len) g[e] = 0.f;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256) void shortconv_step_kernel(Shortconv a, const 
         for (int e = 0; e < V; ++e) {
 #pragma unroll
             for (int j = 0; j < K; ++j) out[e] = __builtin_fmaf(w[j][e], v[j][e], out[e]);
-            if (a.silu) out[e] = silu(out[e]);
+            if (a.silu) out[e] = silu<sizeof(T) == 4>(out[e]);
         }
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) store_run(a.state_out + at + (int64_t)j * a.n, m, v[j + 1]);
