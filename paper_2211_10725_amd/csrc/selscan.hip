@@ -88,6 +88,13 @@ __device__ inline void steps(int soft, float (&d)[EL], const float (&bias)[EL]) 
 }
 
 // W waves of 64 channels, each with H integrators of them at once.
+template <typename T, int EL>
+__device__ inline void put_run(const SelscanRows &x, int t, const Place &p, int se, int m,
+                               const float (&v)[EL]) {
+    T *at = static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.c0 + se;
+    store_run(at, p.live == kLanes ? EL : m, v);
+}
+
 template <int W, int H>
 struct Geo {
     static constexpr int kThreads = kLanes * W;
@@ -121,6 +128,36 @@ __device__ inline void fma_lane(float &acc, float v, float x) {
     asm("s_nop 1\n\tv_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf"
         : "+v"(acc)
         : "v"(v), "v"(x), "n"(L));
+}
+// g[k] += (lane L + H + k of 16 of v) x, and the sum over k of (lane L + k of v) g[k]
+template <int L>
+__device__ inline float fma_dot_lanes(float (&g)[2], float v, float x) {
+    float r;
+    asm("s_nop 1\n\t"
+        "v_fmac_f32_dpp %0, %3, %4 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %1, %3, %4 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_mul_f32_dpp %2, %3, %0 row_newbcast:%5 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %2, %3, %1 row_newbcast:%6 row_mask:0xf bank_mask:0xf"
+        : "+&v"(g[0]), "+&v"(g[1]), "=&v"(r)
+        : "v"(v), "v"(x), "n"(L), "n"(L + 1), "n"(L + 2), "n"(L + 3));
+    return r;
+}
+template <int L>
+__device__ inline float fma_dot_lanes(float (&g)[4], float v, float x) {
+    float r;
+    asm("s_nop 1\n\t"
+        "v_fmac_f32_dpp %0, %5, %6 row_newbcast:%11 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %1, %5, %6 row_newbcast:%12 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %2, %5, %6 row_newbcast:%13 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %3, %5, %6 row_newbcast:%14 row_mask:0xf bank_mask:0xf\n\t"
+        "v_mul_f32_dpp %4, %5, %0 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %4, %5, %1 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %4, %5, %2 row_newbcast:%9 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %4, %5, %3 row_newbcast:%10 row_mask:0xf bank_mask:0xf"
+        : "+&v"(g[0]), "+&v"(g[1]), "+&v"(g[2]), "+&v"(g[3]), "=&v"(r)
+        : "v"(v), "v"(x), "n"(L), "n"(L + 1), "n"(L + 2), "n"(L + 3), "n"(L + 4), "n"(L + 5),
+          "n"(L + 6), "n"(L + 7));
+    return r;
 }
 // sum over k of (lane L + k of 16 of v) x[k]
 template <int L>
@@ -158,7 +195,8 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
     __shared__ Vecs<H> vecs[RND][W];
     __shared__ float yp[OUT ? W : 1][kTile][kLanes];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;  // staging
     const Place p = place_of(a, OUT ? a.segs : a.segs - 1);
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
@@ -196,6 +234,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
         skip[j] = a.skip && j < m ? a.skip[p.c0 + se + j] : 0.f;
         sum[j] = 0.f;
     }
+    const SelscanRows y_rows{a.y, a.y_st, a.y_sb};
     Raw<T, EL> ru, rd, rz;
     T rb[RND], rc[RND];
     const int stop = min(end, len);
@@ -287,9 +326,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
                 for (int j = 0; j < EL; ++j) y[j] *= silu<sizeof(T) == 4>(z[j]);
 #pragma unroll
             for (int j = 0; j < EL; ++j) y[j] = in ? y[j] : 0.f;
-            if (t0 + st < end)
-                store_run(static_cast<T *>(a.y) + (t0 + st) * a.y_st + p.b * a.y_sb + p.c0 + se, m,
-                          y);
+            if (t0 + st < end) put_run<T>(y_rows, t0 + st, p, se, m, y);
         }
     }
     // rows past the sequence, from the first tile that the loop left out
@@ -297,7 +334,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
         const float none[EL] = {};
         const int from = begin < stop ? begin + (stop - begin + kTile - 1) / kTile * kTile : begin;
         for (int t = from + st; t < end; t += kTile)
-            store_run(static_cast<T *>(a.y) + t * a.y_st + p.b * a.y_sb + p.c0 + se, m, none);
+            put_run<T>(y_rows, t, p, se, m, none);
     }
     float *last = OUT ? (p.seg == a.segs - 1 ? a.state_out : nullptr)
                       : a.slot + (int64_t)p.seg * a.B * a.N * a.n;
@@ -377,12 +414,14 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
     const Selscan &a = q.a;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
-    __shared__ float sd[kTile][kLanes], su[kTile][kLanes], sg[kTile][kLanes];
+    __shared__ float2 sd[kTile][kLanes];  // step, step times u
+    __shared__ float sg[kTile][kLanes];
     __shared__ Vecs<H> vecs[RND][W];
     __shared__ float yp[W][kTile][kLanes], up[W][kTile][kLanes], dp[W][kTile][kLanes];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     __shared__ float asum[MANY ? kSelscanMaxStates : 1][kLanes];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;
     const Place p = place_of(a, a.segs);
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
@@ -404,7 +443,15 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
             acc[k] = 0.f;
             if (MANY) carry[i][lane] = g[k], asum[i][lane] = 0.f;
         }
-    float gskip[EL] = {}, gbias[EL] = {};
+    float gskip[EL] = {}, gbias[EL] = {}, bias[EL] = {}, skip[EL] = {};
+    if (a.dt_bias) load_run(a.dt_bias + p.c0 + se, m, bias);
+    if (a.skip) load_run(a.skip + p.c0 + se, m, skip);
+    float hs[H];  // the states before a tile, on their way while the one after it is run
+    auto fetch_states = [&](int t0, int r) {
+        const float *s = q.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase - (on ? 0 : lane);
+#pragma unroll
+        for (int k = 0; k < H; ++k) hs[k] = s[(int64_t)min(state(r, k), a.N - 1) * a.n];
+    };
     Raw<T, EL> ru, rd, rz, rg;
     T rb[RND], rc[RND];
     const int stop = min(end, len);
@@ -424,8 +471,7 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
     };
     const float none[EL] = {};
     auto put = [&](const SelscanRows &x, int t, const float (&v)[EL]) {
-        store_run(static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.c0 + se, m,
-                  v);
+        put_run<T>(x, t, p, se, m, v);
     };
     // rows past the sequence
     for (int t = max(begin, stop) + st; t < end; t += kTile) {
@@ -434,14 +480,16 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
         if (a.z.p) put(q.dz, t, none);
     }
     const int tiles = begin < stop ? (stop - begin + kTile - 1) / kTile : 0;
-    if (tiles > 0) fetch(begin + (tiles - 1) * kTile);
+    if (tiles > 0) {
+        fetch(begin + (tiles - 1) * kTile);
+        if (!MANY) fetch_states(begin + (tiles - 1) * kTile, 0);
+    }
     for (int x = tiles - 1; x >= 0; --x) {
         const int t0 = begin + x * kTile;
         const bool in = t0 + st < stop;
         float u[EL], slope[EL], zs[EL] = {};  // zs: gradient of the gate's input over y
         {
-            float d[EL], gy[EL], bias[EL] = {};
-            if (a.dt_bias) load_run(a.dt_bias + p.c0 + se, m, bias);
+            float d[EL], gy[EL];
             ru.get(u);
             rd.get(d);
             rg.get(gy);
@@ -468,9 +516,8 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
 #pragma unroll
             for (int j = 0; j < EL; ++j) {
                 d[j] = in && j < m ? d[j] : 0.f;
-                sd[st][se + j] = d[j];
                 u[j] = in ? u[j] : 0.f;
-                su[st][se + j] = d[j] * u[j];
+                sd[st][se + j] = make_float2(d[j], d[j] * u[j]);
                 sg[st][se + j] = in ? gi[j] : 0.f;
             }
         }
@@ -488,10 +535,10 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
         for (int r = 0; r < (MANY ? rounds : 1); ++r) {
             const int i0 = state(r, 0);
             float h0[H], h[kTile][H], e[kTile][H];
-            const float *s = q.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase;
+            if (MANY) fetch_states(t0, r);
 #pragma unroll
             for (int k = 0; k < H; ++k) {
-                h0[k] = on && i0 + k < a.N ? s[(int64_t)(i0 + k) * a.n] : 0.f;
+                h0[k] = hs[k];
                 if (MANY) {
                     a2[k] = on && i0 + k < a.N
                                 ? a.a[(int64_t)(i0 + k) * a.n + p.c0 + lane] * kLog2e
@@ -500,11 +547,12 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                     acc[k] = asum[i0 + k][lane];
                 }
             }
+            if (!MANY && x > 0) fetch_states(t0 - kTile, 0);
             float vr = 0.f;
             each<kTile>([&](auto tt) {
                 constexpr int t = decltype(tt)::value, at = t * G::kSlots % 16;
                 if constexpr (at == 0) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
-                const float dv = sd[t][lane], uv = su[t][lane];
+                const float dv = sd[t][lane].x, uv = sd[t][lane].y;
                 each<H>([&](auto kk) {
                     constexpr int k = decltype(kk)::value;
                     e[t][k] = __builtin_amdgcn_exp2f(dv * a2[k]);
@@ -515,24 +563,20 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                     const float y = dot_lanes<at + H>(vr, h[t]);
                     yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (H == 4) __builtin_amdgcn_sched_barrier(0);
             });
             float part[4];
             each<kTile>([&](auto tt) {
                 constexpr int t = kTile - 1 - decltype(tt)::value, at = t * G::kSlots % 16;
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (H == 4) __builtin_amdgcn_sched_barrier(0);
                 if constexpr (at + G::kSlots == 16) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
-                const float dv = sd[t][lane], uv = su[t][lane], gv = sg[t][lane];
+                const float dv = sd[t][lane].x, uv = sd[t][lane].y, gv = sg[t][lane];
                 float gd = 0.f, vb[H], vc[H];
-                each<H>([&](auto kk) {
-                    constexpr int k = decltype(kk)::value;
-                    fma_lane<at + H + k>(g[k], vr, gv);
-                    vc[k] = gv * h[t][k];
-                    vb[k] = g[k] * uv;
-                });
-                const float gin = dot_lanes<at>(vr, g);
+                const float gin = fma_dot_lanes<at>(g, vr, gv);
 #pragma unroll
                 for (int k = 0; k < H; ++k) {
+                    vc[k] = gv * h[t][k];
+                    vb[k] = g[k] * uv;
                     g[k] *= e[t][k];
                     const float x_ = g[k] * (t ? h[t ? t - 1 : 0][k] : h0[k]);
                     acc[k] = __builtin_fmaf(x_, dv, acc[k]);
@@ -575,8 +619,6 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
         }
         __syncthreads();
         float gu[EL], gdt[EL];
-        float skip[EL] = {};
-        if (a.skip) load_run(a.skip + p.c0 + se, m, skip);
 #pragma unroll
         for (int j = 0; j < EL; ++j) {
             float y = a.z.p ? yp[0][st][se + j] : 0.f, gin = up[0][st][se + j],
@@ -587,7 +629,7 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                 gin += up[k][st][se + j];
                 gd += dp[k][st][se + j];
             }
-            const float d = sd[st][se + j], gi = sg[st][se + j];
+            const float d = sd[st][se + j].x, gi = sg[st][se + j];
             gu[j] = __builtin_fmaf(gin, d, gi * skip[j]);
             gdt[j] = in ? __builtin_fmaf(gin, u[j], gd * kLn2) * slope[j] : 0.f;
             zs[j] *= __builtin_fmaf(skip[j], u[j], y);
@@ -614,11 +656,11 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
         }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < EL; ++j) sd[st][se + j] = gskip[j], su[st][se + j] = gbias[j];
+    for (int j = 0; j < EL; ++j) sd[st][se + j] = make_float2(gskip[j], gbias[j]);
     __syncthreads();
     if (w == 0 && on) {
         float s0 = 0.f, s1 = 0.f;
-        for (int k = 0; k < kTile; ++k) s0 += sd[k][lane], s1 += su[k][lane];
+        for (int k = 0; k < kTile; ++k) s0 += sd[k][lane].x, s1 += sd[k][lane].y;
         rows[(int64_t)a.N * a.n] = s0;
         rows[(int64_t)(a.N + 1) * a.n] = s1;
     }
@@ -635,7 +677,8 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
     __shared__ float2 sd[kTile][kLanes];
     __shared__ Vecs<H> vecs[RND][W];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;
     Place p = place_of(a, a.segs - 1);
     p.seg += 1;
@@ -883,14 +926,14 @@ template <typename T>
 hipError_t by_states(const Selscan &a, hipStream_t s) {
     if (a.N <= 4) return run_fwd<T, 1, 4, false>(a, s);
     if (a.N <= 8) return run_fwd<T, 2, 4, false>(a, s);
-    if (a.N <= 16) return run_fwd<T, 4, 4, false>(a, s);
+    if (a.N <= 16) return run_fwd<T, 8, 2, false>(a, s);
     return run_fwd<T, 4, 4, true>(a, s);
 }
 template <typename T>
 hipError_t by_states(const SelscanBwd &q, hipStream_t s) {
     if (q.a.N <= 4) return run_bwd<T, 1, 4, false>(q, s);
     if (q.a.N <= 8) return run_bwd<T, 2, 4, false>(q, s);
-    if (q.a.N <= 16) return run_bwd<T, 4, 4, false>(q, s);
+    if (q.a.N <= 16) return run_bwd<T, 8, 2, false>(q, s);
     return run_bwd<T, 4, 4, true>(q, s);
 }
 
