@@ -59,18 +59,32 @@ __device__ inline int length_of(const Selscan &a, int b) {
     return a.lens ? min(max(a.lens[b], 0), a.T) : a.T;
 }
 
-// b or c of a token and integrator, not yet converted (that would wait for the load)
+// A thread's place in a tensor: its token of the segment's first tile, and from there on
+// whole tiles, which the scalar unit multiplies out.
 template <typename T>
-__device__ inline T vec_value(const SelscanVec &v, int t, int b, int g, int i) {
-    return static_cast<const T *>(v.p)[t * v.st + b * v.sb + g * v.sg + i];
+struct Walk {
+    T *at;
+    int64_t step;
+    __device__ inline T *tile(int tokens) const { return at + tokens * step; }
+};
+template <typename T>
+__device__ inline Walk<T> walk_rows(const SelscanRows &x, int t, const Place &p, int se) {
+    return {static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.c0 + se, x.st};
+}
+template <typename T>
+__device__ inline Walk<T> walk_vec(const SelscanVec &x, int t, const Place &p, int i) {
+    return {static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.g * x.sg + i,
+            x.st};
 }
 // EL values of a row, all of a workgroup's 64 channels there or only m of these
 template <typename T, int EL>
-__device__ inline void fetch_run(Raw<T, EL> &r, const SelscanRows &x, int t, const Place &p, int se,
-                                 int m) {
-    const T *at = static_cast<const T *>(x.p) + t * x.st + p.b * x.sb + p.c0 + se;
+__device__ inline void fetch_run(Raw<T, EL> &r, const T *at, const Place &p, int m) {
     if (p.live == kLanes) __builtin_memcpy(r.w, at, sizeof(r.w));
     else r.load(at, m);
+}
+template <typename T, int EL>
+__device__ inline void put_run(T *at, const Place &p, int m, const float (&v)[EL]) {
+    store_run(at, p.live == kLanes ? EL : m, v);
 }
 
 // raw steps and their bias to steps, the condition outside the loop: one stretch of
@@ -88,13 +102,6 @@ __device__ inline void steps(int soft, float (&d)[EL], const float (&bias)[EL]) 
 }
 
 // W waves of 64 channels, each with H integrators of them at once.
-template <typename T, int EL>
-__device__ inline void put_run(const SelscanRows &x, int t, const Place &p, int se, int m,
-                               const float (&v)[EL]) {
-    T *at = static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.c0 + se;
-    store_run(at, p.live == kLanes ? EL : m, v);
-}
-
 template <int W, int H>
 struct Geo {
     static constexpr int kThreads = kLanes * W;
@@ -234,21 +241,25 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
         skip[j] = a.skip && j < m ? a.skip[p.c0 + se + j] : 0.f;
         sum[j] = 0.f;
     }
-    const SelscanRows y_rows{a.y, a.y_st, a.y_sb};
+    const int t1 = begin + st;
+    const Walk<T> wu = walk_rows<T>(a.u, t1, p, se), wd = walk_rows<T>(a.dt, t1, p, se),
+                  wz = walk_rows<T>(a.z, t1, p, se),
+                  wy = walk_rows<T>(SelscanRows{a.y, a.y_st, a.y_sb}, t1, p, se),
+                  wb = walk_vec<T>(a.b, t1, p, 0), wc = walk_vec<T>(a.c, t1, p, 0);
     Raw<T, EL> ru, rd, rz;
     T rb[RND], rc[RND];
     const int stop = min(end, len);
+    // not converted yet: that would wait for the loads
     auto fetch = [&](int t0) {
-        // past the end the last token again, which the staging leaves out
-        const int t = min(t0 + st, stop - 1);
-        fetch_run(ru, a.u, t, p, se, m);
-        fetch_run(rd, a.dt, t, p, se, m);
-        if (OUT && a.z.p) fetch_run(rz, a.z, t, p, se, m);
+        if (t0 + st >= stop) return;
+        fetch_run(ru, wu.tile(t0 - begin), p, m);
+        fetch_run(rd, wd.tile(t0 - begin), p, m);
+        if (OUT && a.z.p) fetch_run(rz, wz.tile(t0 - begin), p, m);
 #pragma unroll
         for (int r = 0; r < RND; ++r) {
             const int i = min(r * ROW + si, a.N - 1);
-            rb[r] = vec_value<T>(a.b, t, p.b, p.g, i);
-            if (OUT) rc[r] = vec_value<T>(a.c, t, p.b, p.g, i);
+            rb[r] = wb.tile(t0 - begin)[i];
+            if (OUT) rc[r] = wc.tile(t0 - begin)[i];
         }
     };
     if (begin < stop) fetch(begin);
@@ -326,15 +337,14 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
                 for (int j = 0; j < EL; ++j) y[j] *= silu<sizeof(T) == 4>(z[j]);
 #pragma unroll
             for (int j = 0; j < EL; ++j) y[j] = in ? y[j] : 0.f;
-            if (t0 + st < end) put_run<T>(y_rows, t0 + st, p, se, m, y);
+            if (t0 + st < end) put_run(wy.tile(t0 - begin), p, m, y);
         }
     }
     // rows past the sequence, from the first tile that the loop left out
     if (OUT) {
         const float none[EL] = {};
         const int from = begin < stop ? begin + (stop - begin + kTile - 1) / kTile * kTile : begin;
-        for (int t = from + st; t < end; t += kTile)
-            put_run<T>(y_rows, t, p, se, m, none);
+        for (int t = from; t + st < end; t += kTile) put_run(wy.tile(t - begin), p, m, none);
     }
     float *last = OUT ? (p.seg == a.segs - 1 ? a.state_out : nullptr)
                       : a.slot + (int64_t)p.seg * a.B * a.N * a.n;
@@ -452,33 +462,46 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
 #pragma unroll
         for (int k = 0; k < H; ++k) hs[k] = s[(int64_t)min(state(r, k), a.N - 1) * a.n];
     };
+    const int t1 = begin + st;
+    const Walk<T> wu = walk_rows<T>(a.u, t1, p, se), wd = walk_rows<T>(a.dt, t1, p, se),
+                  wz = walk_rows<T>(a.z, t1, p, se),
+                  wg = walk_rows<T>(SelscanRows{q.gy, a.y_st, a.y_sb}, t1, p, se),
+                  wdu = walk_rows<T>(q.du, t1, p, se), wdd = walk_rows<T>(q.ddt, t1, p, se),
+                  wdz = walk_rows<T>(q.dz, t1, p, se), wb = walk_vec<T>(a.b, t1, p, 0),
+                  wc = walk_vec<T>(a.c, t1, p, 0);
     Raw<T, EL> ru, rd, rz, rg;
     T rb[RND], rc[RND];
     const int stop = min(end, len);
-    const SelscanRows gy_rows{q.gy, a.y_st, a.y_sb};
     auto fetch = [&](int t0) {
-        const int t = min(t0 + st, stop - 1);
-        fetch_run(ru, a.u, t, p, se, m);
-        fetch_run(rd, a.dt, t, p, se, m);
-        fetch_run(rg, gy_rows, t, p, se, m);
-        if (a.z.p) fetch_run(rz, a.z, t, p, se, m);
+        if (t0 + st >= stop) return;
+        fetch_run(ru, wu.tile(t0 - begin), p, m);
+        fetch_run(rd, wd.tile(t0 - begin), p, m);
+        fetch_run(rg, wg.tile(t0 - begin), p, m);
+        if (a.z.p) fetch_run(rz, wz.tile(t0 - begin), p, m);
 #pragma unroll
         for (int r = 0; r < RND; ++r) {
             const int i = min(r * ROW + si, a.N - 1);
-            rb[r] = vec_value<T>(a.b, t, p.b, p.g, i);
-            rc[r] = vec_value<T>(a.c, t, p.b, p.g, i);
+            rb[r] = wb.tile(t0 - begin)[i];
+            rc[r] = wc.tile(t0 - begin)[i];
         }
     };
     const float none[EL] = {};
-    auto put = [&](const SelscanRows &x, int t, const float (&v)[EL]) {
-        put_run<T>(x, t, p, se, m, v);
-    };
     // rows past the sequence
-    for (int t = max(begin, stop) + st; t < end; t += kTile) {
-        put(q.du, t, none);
-        put(q.ddt, t, none);
-        if (a.z.p) put(q.dz, t, none);
+    for (int t = max(begin, stop); t + st < end; t += kTile) {
+        put_run(wdu.tile(t - begin), p, m, none);
+        put_run(wdd.tile(t - begin), p, m, none);
+        if (a.z.p) put_run(wdz.tile(t - begin), p, m, none);
     }
+    // sums over this workgroup's channels: a lane's token, of 8 or 16, and integrator
+    const int per = a.tiles / a.groups;
+    const int vt = H == 4 ? (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4
+                          : (lane >> 3 & 1) + (lane >> 1 & 2) + (lane << 1 & 4) + (lane & 1) * 8;
+    const int vi = w * H + (H == 4 ? lane >> 3 & 3 : lane >> 4 & 1);
+    const int64_t vstep = (int64_t)a.B * a.groups * a.N;
+    const Walk<float> wv{q.vec + (((int64_t)(lane >> 5) * per + p.tile % per) * a.T + begin + vt) *
+                                     vstep +
+                             (p.b * a.groups + p.g) * a.N + vi,
+                         vstep};
     const int tiles = begin < stop ? (stop - begin + kTile - 1) / kTile : 0;
     if (tiles > 0) {
         fetch(begin + (tiles - 1) * kTile);
@@ -601,15 +624,8 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                     }
                 });
                 if constexpr (t % (H == 4 ? 8 : 16) == 0) {
-                    const int i = i0 + (H == 4 ? lane >> 3 & 3 : lane >> 4 & 1);
-                    const int tt_ = t0 + t + (H == 4 ? (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4
-                                                     : (lane >> 3 & 1) + (lane >> 1 & 2) +
-                                                           (lane << 1 & 4) + (lane & 1) * 8);
-                    const int per = a.tiles / a.groups;
-                    if (tt_ < stop && i < a.N)
-                        q.vec[((((int64_t)(lane >> 5) * per + p.tile % per) * a.T + tt_) * a.B +
-                               p.b) * a.groups * a.N +
-                              p.g * a.N + i] = v;
+                    if (t0 + t + vt < stop && vi + r * ROW < a.N)
+                        wv.tile(t0 + t - begin)[r * ROW] = v;
                 }
             });
             if (MANY) {
@@ -637,9 +653,9 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
             gbias[j] += gdt[j];
         }
         if (in) {
-            put(q.du, t0 + st, gu);
-            put(q.ddt, t0 + st, gdt);
-            if (a.z.p) put(q.dz, t0 + st, zs);
+            put_run(wdu.tile(t0 - begin), p, m, gu);
+            put_run(wdd.tile(t0 - begin), p, m, gdt);
+            if (a.z.p) put_run(wdz.tile(t0 - begin), p, m, zs);
         }
     }
     // the gradient of the state before the segment, and the sums over its tokens
@@ -707,18 +723,20 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
         bias[j] = a.dt_bias && j < m ? a.dt_bias[p.c0 + se + j] : 0.f;
         sum[j] = 0.f;
     }
+    const int t1 = begin + st;
+    const Walk<T> wd = walk_rows<T>(a.dt, t1, p, se), wz = walk_rows<T>(a.z, t1, p, se),
+                  wg = walk_rows<T>(SelscanRows{q.gy, a.y_st, a.y_sb}, t1, p, se),
+                  wc = walk_vec<T>(a.c, t1, p, 0);
     Raw<T, EL> rd, rz, rg;
     T rc[RND];
     const int stop = min(end, len);
-    const SelscanRows gy_rows{q.gy, a.y_st, a.y_sb};
     auto fetch = [&](int t0) {
-        const int t = min(t0 + st, stop - 1);
-        fetch_run(rd, a.dt, t, p, se, m);
-        fetch_run(rg, gy_rows, t, p, se, m);
-        if (a.z.p) fetch_run(rz, a.z, t, p, se, m);
+        if (t0 + st >= stop) return;
+        fetch_run(rd, wd.tile(t0 - begin), p, m);
+        fetch_run(rg, wg.tile(t0 - begin), p, m);
+        if (a.z.p) fetch_run(rz, wz.tile(t0 - begin), p, m);
 #pragma unroll
-        for (int r = 0; r < RND; ++r)
-            rc[r] = vec_value<T>(a.c, t, p.b, p.g, min(r * ROW + si, a.N - 1));
+        for (int r = 0; r < RND; ++r) rc[r] = wc.tile(t0 - begin)[min(r * ROW + si, a.N - 1)];
     };
     const int tiles = begin < stop ? (stop - begin + kTile - 1) / kTile : 0;
     if (tiles > 0) fetch(begin + (tiles - 1) * kTile);
