@@ -35,6 +35,8 @@ namespace {
 
 constexpr int kTile = kSelscanTile;  // tokens
 constexpr int kLanes = 64;           // channels of a workgroup
+constexpr int H = 2;                 // integrators of a wave
+constexpr int kSlots = 2 * H;        // its values of b and c for a token
 
 // Where this workgroup works.
 struct Place {
@@ -102,21 +104,20 @@ __device__ inline void steps(int soft, float (&d)[EL], const float (&bias)[EL]) 
 }
 
 // W waves of 64 channels, each with H integrators of them at once.
-template <int W, int H>
+template <int W>
 struct Geo {
     static constexpr int kThreads = kLanes * W;
     static constexpr int kTok = 4 * W;           // threads that stage a token
     static constexpr int kEl = kLanes / kTok;    // channels of such a thread
     static constexpr int kRow = W * H;           // integrators at once
-    static constexpr int kSlots = 2 * H;         // values of b and c for a wave and token
 };
 
 // b and c of a tile for a wave, 16 values to a register: token t's are the 2 H from
 // 2 H t on.  Every lane wants the same ones; a register read with its lanes' own 16
 // values (a quarter of the LDS traffic of a broadcast read) and the operand of an
 // instruction that takes one lane of 16 for all of them.
-template <int H>
-using Vecs = float[kTile * H / 8][16];
+constexpr int kVecRows = kTile * kSlots / 16;
+using Vecs = float[kVecRows][16];
 
 template <int N, int I = 0, typename F>
 __device__ inline void each(F f) {
@@ -138,7 +139,7 @@ __device__ inline void fma_lane(float &acc, float v, float x) {
 }
 // g[k] += (lane L + H + k of 16 of v) x, and the sum over k of (lane L + k of v) g[k]
 template <int L>
-__device__ inline float fma_dot_lanes(float (&g)[2], float v, float x) {
+__device__ inline float fma_dot_lanes(float (&g)[H], float v, float x) {
     float r;
     asm("s_nop 1\n\t"
         "v_fmac_f32_dpp %0, %3, %4 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
@@ -149,39 +150,9 @@ __device__ inline float fma_dot_lanes(float (&g)[2], float v, float x) {
         : "v"(v), "v"(x), "n"(L), "n"(L + 1), "n"(L + 2), "n"(L + 3));
     return r;
 }
-template <int L>
-__device__ inline float fma_dot_lanes(float (&g)[4], float v, float x) {
-    float r;
-    asm("s_nop 1\n\t"
-        "v_fmac_f32_dpp %0, %5, %6 row_newbcast:%11 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %1, %5, %6 row_newbcast:%12 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %2, %5, %6 row_newbcast:%13 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %3, %5, %6 row_newbcast:%14 row_mask:0xf bank_mask:0xf\n\t"
-        "v_mul_f32_dpp %4, %5, %0 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %4, %5, %1 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %4, %5, %2 row_newbcast:%9 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %4, %5, %3 row_newbcast:%10 row_mask:0xf bank_mask:0xf"
-        : "+&v"(g[0]), "+&v"(g[1]), "+&v"(g[2]), "+&v"(g[3]), "=&v"(r)
-        : "v"(v), "v"(x), "n"(L), "n"(L + 1), "n"(L + 2), "n"(L + 3), "n"(L + 4), "n"(L + 5),
-          "n"(L + 6), "n"(L + 7));
-    return r;
-}
 // sum over k of (lane L + k of 16 of v) x[k]
 template <int L>
-__device__ inline float dot_lanes(float v, const float (&x)[4]) {
-    float r;
-    asm("s_nop 1\n\t"
-        "v_mul_f32_dpp %0, %1, %2 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
-        : "=&v"(r)
-        : "v"(v), "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "n"(L), "n"(L + 1), "n"(L + 2),
-          "n"(L + 3));
-    return r;
-}
-template <int L>
-__device__ inline float dot_lanes(float v, const float (&x)[2]) {
+__device__ inline float dot_lanes(float v, const float (&x)[H]) {
     float r;
     asm("s_nop 1\n\t"
         "v_mul_f32_dpp %0, %1, %2 row_newbcast:%4 row_mask:0xf bank_mask:0xf\n\t"
@@ -193,13 +164,13 @@ __device__ inline float dot_lanes(float v, const float (&x)[2]) {
 
 // OUT: outputs (and saved states), from a.slot's or the caller's start; else the end
 // state from zero and the sum of the steps, into a.slot and a.sums.
-template <typename T, int W, int H, bool MANY, bool OUT>
+template <typename T, int W, bool MANY, bool OUT>
 __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
-    using G = Geo<W, H>;
+    using G = Geo<W>;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
     __shared__ float2 sd[kTile][kLanes];
-    __shared__ Vecs<H> vecs[RND][W];
+    __shared__ Vecs vecs[RND][W];
     __shared__ float yp[OUT ? W : 1][kTile][kLanes];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -262,6 +233,12 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
             if (OUT) rc[r] = wc.tile(t0 - begin)[i];
         }
     };
+    // Outputs are stored once the next tile's loads are there: memory accesses end in
+    // order, and those loads would be waited for together with a store before them.
+    float out[EL] = {};
+    auto write_out = [&](int t0) {
+        if (t0 + st < end) put_run(wy.tile(t0 - begin), p, m, out);
+    };
     if (begin < stop) fetch(begin);
     for (int t0 = begin; t0 < stop; t0 += kTile) {
         float u[EL], z[EL], d[EL];
@@ -279,12 +256,13 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
 #pragma unroll
         for (int r = 0; r < RND; ++r) {
             if (si < ROW) {
-                float *v = &vecs[r][si / H][0][0] + st * G::kSlots + si % H;
+                float *v = &vecs[r][si / H][0][0] + st * kSlots + si % H;
                 const bool there = in && r * ROW + si < a.N;
                 v[0] = there ? (float)rb[r] : 0.f;
                 if (OUT) v[H] = there ? (float)rc[r] : 0.f;
             }
         }
+        if (OUT && t0 > begin) write_out(t0 - kTile);
         if (t0 + kTile < stop) fetch(t0 + kTile);
         __syncthreads();
         for (int r = 0; r < (MANY ? rounds : 1); ++r) {
@@ -304,8 +282,8 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
             }
             float vr = 0.f;
             each<kTile>([&](auto tt) {
-                constexpr int t = decltype(tt)::value, at = t * G::kSlots % 16;
-                if constexpr (at == 0) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
+                constexpr int t = decltype(tt)::value, at = t * kSlots % 16;
+                if constexpr (at == 0) vr = vecs[r][w][t * kSlots / 16][lane & 15];
                 const float2 v = sd[t][lane];
                 each<H>([&](auto kk) {
                     constexpr int k = decltype(kk)::value;
@@ -337,9 +315,11 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
                 for (int j = 0; j < EL; ++j) y[j] *= silu<sizeof(T) == 4>(z[j]);
 #pragma unroll
             for (int j = 0; j < EL; ++j) y[j] = in ? y[j] : 0.f;
-            if (t0 + st < end) put_run(wy.tile(t0 - begin), p, m, y);
+#pragma unroll
+            for (int j = 0; j < EL; ++j) out[j] = y[j];
         }
     }
+    if (OUT && begin < stop) write_out((stop - begin - 1) / kTile * kTile + begin);
     // rows past the sequence, from the first tile that the loop left out
     if (OUT) {
         const float none[EL] = {};
@@ -418,15 +398,15 @@ __device__ inline float halve(float x, float y) {
     }
 }
 
-template <typename T, int W, int H, bool MANY>
+template <typename T, int W, bool MANY>
 __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(SelscanBwd q) {
-    using G = Geo<W, H>;
+    using G = Geo<W>;
     const Selscan &a = q.a;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
     __shared__ float2 sd[kTile][kLanes];  // step, step times u
     __shared__ float sg[kTile][kLanes];
-    __shared__ Vecs<H> vecs[RND][W];
+    __shared__ Vecs vecs[RND][W];
     __shared__ float yp[W][kTile][kLanes], up[W][kTile][kLanes], dp[W][kTile][kLanes];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     __shared__ float asum[MANY ? kSelscanMaxStates : 1][kLanes];
@@ -492,11 +472,10 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
         put_run(wdd.tile(t - begin), p, m, none);
         if (a.z.p) put_run(wdz.tile(t - begin), p, m, none);
     }
-    // sums over this workgroup's channels: a lane's token, of 8 or 16, and integrator
+    // sums over this workgroup's channels: a lane's token and integrator
     const int per = a.tiles / a.groups;
-    const int vt = H == 4 ? (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4
-                          : (lane >> 3 & 1) + (lane >> 1 & 2) + (lane << 1 & 4) + (lane & 1) * 8;
-    const int vi = w * H + (H == 4 ? lane >> 3 & 3 : lane >> 4 & 1);
+    const int vt = (lane >> 3 & 1) + (lane >> 1 & 2) + (lane << 1 & 4) + (lane & 1) * 8;
+    const int vi = w * H + (lane >> 4 & 1);
     const int64_t vstep = (int64_t)a.B * a.groups * a.N;
     const Walk<float> wv{q.vec + (((int64_t)(lane >> 5) * per + p.tile % per) * a.T + begin + vt) *
                                      vstep +
@@ -547,7 +526,7 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
 #pragma unroll
         for (int r = 0; r < RND; ++r) {
             if (si < ROW) {
-                float *v = &vecs[r][si / H][0][0] + st * G::kSlots + si % H;
+                float *v = &vecs[r][si / H][0][0] + st * kSlots + si % H;
                 const bool there = in && r * ROW + si < a.N;
                 v[0] = there ? (float)rb[r] : 0.f;
                 v[H] = there ? (float)rc[r] : 0.f;
@@ -571,11 +550,18 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                 }
             }
             if (!MANY && x > 0) fetch_states(t0 - kTile, 0);
-            float vr = 0.f;
+            // the tile's values of this lane, for both directions
+            float vrs[kVecRows], gvs[kTile];
+            float2 dus[kTile];
+#pragma unroll
+            for (int k = 0; k < kVecRows; ++k) vrs[k] = vecs[r][w][k][lane & 15];
+#pragma unroll
+            for (int t = 0; t < kTile; ++t) dus[t] = sd[t][lane];
+#pragma unroll
+            for (int t = kTile - 1; t >= 0; --t) gvs[t] = sg[t][lane];
             each<kTile>([&](auto tt) {
-                constexpr int t = decltype(tt)::value, at = t * G::kSlots % 16;
-                if constexpr (at == 0) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
-                const float dv = sd[t][lane].x, uv = sd[t][lane].y;
+                constexpr int t = decltype(tt)::value, at = t * kSlots % 16;
+                const float vr = vrs[t * kSlots / 16], dv = dus[t].x, uv = dus[t].y;
                 each<H>([&](auto kk) {
                     constexpr int k = decltype(kk)::value;
                     e[t][k] = __builtin_amdgcn_exp2f(dv * a2[k]);
@@ -586,14 +572,11 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                     const float y = dot_lanes<at + H>(vr, h[t]);
                     yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
                 }
-                if constexpr (H == 4) __builtin_amdgcn_sched_barrier(0);
             });
             float part[4];
             each<kTile>([&](auto tt) {
-                constexpr int t = kTile - 1 - decltype(tt)::value, at = t * G::kSlots % 16;
-                if constexpr (H == 4) __builtin_amdgcn_sched_barrier(0);
-                if constexpr (at + G::kSlots == 16) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
-                const float dv = sd[t][lane].x, uv = sd[t][lane].y, gv = sg[t][lane];
+                constexpr int t = kTile - 1 - decltype(tt)::value, at = t * kSlots % 16;
+                const float vr = vrs[t * kSlots / 16], dv = dus[t].x, uv = dus[t].y, gv = gvs[t];
                 float gd = 0.f, vb[H], vc[H];
                 const float gin = fma_dot_lanes<at>(g, vr, gv);
 #pragma unroll
@@ -607,25 +590,19 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                 }
                 up[w][t][lane] = MANY && r ? up[w][t][lane] + gin : gin;
                 dp[w][t][lane] = MANY && r ? dp[w][t][lane] + gd : gd;
-                // The sums over lanes.  Bits of the lane that a sum ends in: 32 b or c, then
-                // the integrator's from the high one on (16 and 8; 16), then the token's
-                // from the low one on.  Tokens are joined in pairs, fours and so on.
-                float v;
-                if constexpr (H == 4)
-                    v = halve<8>(halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[2], vc[2])),
-                                 halve<16>(halve<32>(vb[1], vc[1]), halve<32>(vb[3], vc[3])));
-                else
-                    v = halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[1], vc[1]));
-                each<H == 4 ? 3 : 4>([&](auto ll) {
-                    constexpr int l = decltype(ll)::value, bit = (H == 4 ? 4 : 8) >> l;
+                // The sums over lanes.  Bits of the lane that a sum ends in: 32 b or c, 16
+                // the integrator's, then the token's from the low one on.  Tokens are joined
+                // in pairs, fours and so on.
+                float v = halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[1], vc[1]));
+                each<4>([&](auto ll) {
+                    constexpr int l = decltype(ll)::value;
                     if constexpr ((t & ((1 << l) - 1)) == 0) {
                         if constexpr (t >> l & 1) part[l] = v;
-                        else v = halve<bit>(v, part[l]);
+                        else v = halve<(8 >> l)>(v, part[l]);
                     }
                 });
-                if constexpr (t % (H == 4 ? 8 : 16) == 0) {
-                    if (t0 + t + vt < stop && vi + r * ROW < a.N)
-                        wv.tile(t0 + t - begin)[r * ROW] = v;
+                if constexpr (t == 0) {
+                    if (t0 + vt < stop && vi + r * ROW < a.N) wv.tile(t0 - begin)[r * ROW] = v;
                 }
             });
             if (MANY) {
@@ -684,14 +661,14 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
 
 // The gradient that a segment passes on from its own tokens, and the sum of its steps:
 // segments 1 .. segs - 1.
-template <typename T, int W, int H, bool MANY>
+template <typename T, int W, bool MANY>
 __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) {
-    using G = Geo<W, H>;
+    using G = Geo<W>;
     const Selscan &a = q.a;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
     __shared__ float2 sd[kTile][kLanes];
-    __shared__ Vecs<H> vecs[RND][W];
+    __shared__ Vecs vecs[RND][W];
     __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -761,7 +738,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
 #pragma unroll
         for (int r = 0; r < RND; ++r)
             if (si < ROW)
-                (&vecs[r][si / H][0][0])[st * G::kSlots + H + si % H] =
+                (&vecs[r][si / H][0][0])[st * kSlots + H + si % H] =
                     in && r * ROW + si < a.N ? (float)rc[r] : 0.f;
         if (x > 0) fetch(t0 - kTile);
         __syncthreads();
@@ -774,8 +751,8 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
             }
             float vr = 0.f;
             each<kTile>([&](auto tt) {
-                constexpr int t = kTile - 1 - decltype(tt)::value, at = t * G::kSlots % 16;
-                if constexpr (at + G::kSlots == 16) vr = vecs[r][w][t * G::kSlots / 16][lane & 15];
+                constexpr int t = kTile - 1 - decltype(tt)::value, at = t * kSlots % 16;
+                if constexpr (at + kSlots == 16) vr = vecs[r][w][t * kSlots / 16][lane & 15];
                 const float2 v = sd[t][lane];
                 each<H>([&](auto kk) {
                     constexpr int k = decltype(kk)::value;
@@ -908,29 +885,29 @@ __global__ __launch_bounds__(256) void selscan_step_kernel(Selscan a, const int3
     store_run(y, m, out);
 }
 
-template <typename T, int W, int H, bool MANY>
+template <typename T, int W, bool MANY>
 hipError_t run_fwd(const Selscan &a, hipStream_t s) {
-    const int units = a.tiles * a.B, threads = Geo<W, H>::kThreads;
+    const int units = a.tiles * a.B, threads = Geo<W>::kThreads;
     if (a.segs > 1) {
-        selscan_kernel<T, W, H, MANY, false><<<units * (a.segs - 1), threads, 0, s>>>(a);
+        selscan_kernel<T, W, MANY, false><<<units * (a.segs - 1), threads, 0, s>>>(a);
         const int64_t size = (int64_t)a.B * a.N * a.n;
         selscan_join_kernel<<<(unsigned)((size + 255) / 256), 256, 0, s>>>(a, a.state_in, false);
     }
-    selscan_kernel<T, W, H, MANY, true><<<units * a.segs, threads, 0, s>>>(a);
+    selscan_kernel<T, W, MANY, true><<<units * a.segs, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int W, int H, bool MANY>
+template <typename T, int W, bool MANY>
 hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
     const Selscan &a = q.a;
-    const int units = a.tiles * a.B, threads = Geo<W, H>::kThreads;
+    const int units = a.tiles * a.B, threads = Geo<W>::kThreads;
     if (units > 0 && a.segs > 1) {
-        selscan_back_kernel<T, W, H, MANY><<<units * (a.segs - 1), threads, 0, s>>>(q);
+        selscan_back_kernel<T, W, MANY><<<units * (a.segs - 1), threads, 0, s>>>(q);
         const int64_t size = (int64_t)a.B * a.N * a.n;
         selscan_join_kernel<<<(unsigned)((size + 255) / 256), 256, 0, s>>>(a, q.grad_state_out,
                                                                           true);
     }
-    if (units > 0) selscan_bwd_kernel<T, W, H, MANY><<<units * a.segs, threads, 0, s>>>(q);
+    if (units > 0) selscan_bwd_kernel<T, W, MANY><<<units * a.segs, threads, 0, s>>>(q);
     const int64_t per = (int64_t)a.T * a.B * a.groups * a.N;
     if (per > 0)
         selscan_vec_kernel<T><<<dim3((unsigned)((per + 255) / 256), 2), 256, 0, s>>>(q);
@@ -942,17 +919,17 @@ hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
 
 template <typename T>
 hipError_t by_states(const Selscan &a, hipStream_t s) {
-    if (a.N <= 4) return run_fwd<T, 1, 4, false>(a, s);
-    if (a.N <= 8) return run_fwd<T, 2, 4, false>(a, s);
-    if (a.N <= 16) return run_fwd<T, 8, 2, false>(a, s);
-    return run_fwd<T, 4, 4, true>(a, s);
+    if (a.N <= 4) return run_fwd<T, 2, false>(a, s);
+    if (a.N <= 8) return run_fwd<T, 4, false>(a, s);
+    if (a.N <= 16) return run_fwd<T, 8, false>(a, s);
+    return run_fwd<T, 8, true>(a, s);
 }
 template <typename T>
 hipError_t by_states(const SelscanBwd &q, hipStream_t s) {
-    if (q.a.N <= 4) return run_bwd<T, 1, 4, false>(q, s);
-    if (q.a.N <= 8) return run_bwd<T, 2, 4, false>(q, s);
-    if (q.a.N <= 16) return run_bwd<T, 8, 2, false>(q, s);
-    return run_bwd<T, 4, 4, true>(q, s);
+    if (q.a.N <= 4) return run_bwd<T, 2, false>(q, s);
+    if (q.a.N <= 8) return run_bwd<T, 4, false>(q, s);
+    if (q.a.N <= 16) return run_bwd<T, 8, false>(q, s);
+    return run_bwd<T, 8, true>(q, s);
 }
 
 template <typename T>
