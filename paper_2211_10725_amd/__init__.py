@@ -534,9 +534,15 @@ def _need_heads(fn, what, t, dtype, shape, stride):
                      "what the descriptor says")
 
 
+_torch_dtypes = {}  # by code, once torch is there
+
+
 def _torch_dtype(code):
-    import torch
-    return torch.float32 if code == F32 else torch.float16 if code == F16 else torch.bfloat16
+    if not _torch_dtypes:
+        import torch
+        _torch_dtypes.update({F32: torch.float32, F16: torch.float16, BF16: torch.bfloat16,
+                              I32: torch.int32})
+    return _torch_dtypes.get(code, _torch_dtypes[BF16])
 
 
 def _need_linattn(fn, d, q, k, v, o, decay, prefix=""):
@@ -553,8 +559,7 @@ def _need_array(fn, t, dtype_code, count, what):
     """_need for an argument that must also be contiguous and of the type itself."""
     if t is None or isinstance(t, int):
         return
-    import torch
-    dt = torch.float32 if dtype_code == F32 else torch.int32
+    dt = _torch_dtype(F32 if dtype_code == F32 else I32)
     if t.dtype is not dt or t.numel() < count or not t.is_contiguous():
         raise ValueError(f"{fn}: {what} needs {count} contiguous elements of {dt}, got "
                          f"{t.numel()} of {t.dtype}")
@@ -759,9 +764,25 @@ def _strides(fn, t, dims):
     return (ctypes.c_int64 * dims)(*st)
 
 
-def _need_strided(fn, what, t, code, shape, stride):
+def _seen(desc, **tensors):
+    """Keeps with a descriptor the layouts it was made from: the usual arguments' check is
+    then a comparison or three (a small call is bound by the host)."""
+    desc.layouts = {k: (t.dtype, t.shape, t.stride()) for k, t in tensors.items()
+                    if t is not None}
+    desc.fields = bytes(desc)
+    return desc
+
+
+def _layouts(desc):
+    """What _seen kept, unless a field was changed since."""
+    return desc.layouts if getattr(desc, "fields", None) == bytes(desc) else {}
+
+
+def _need_strided(fn, what, t, code, seen, shape, stride):
     """A strided argument of the shape, type and strides the descriptor has."""
     if t is None or isinstance(t, int):
+        return
+    if seen is not None and t.dtype is seen[0] and t.shape == seen[1] and t.stride() == seen[2]:
         return
     if t.dtype is _torch_dtype(code) and t.shape == shape:
         st = t.stride()
@@ -785,10 +806,11 @@ def selscan_desc(u, dt, b, c, y, z=None, delta_softplus=True, forward_only=False
                          "together")
     if any(t is not None and t.dtype != u.dtype for t in (dt, b, c, y, z)):
         raise ValueError(f"{fn}: u, dt, b, c, y and z must have one dtype")
-    return SelscanDesc(T, B, n, b.shape[3], b.shape[2], _dtype_code(u), int(delta_softplus),
-                       int(forward_only), *(_strides(fn, t, 2) for t in (u, dt)),
-                       _strides(fn, z if z is not None else u, 2), _strides(fn, y, 2),
-                       _strides(fn, b, 3), _strides(fn, c, 3))
+    d = SelscanDesc(T, B, n, b.shape[3], b.shape[2], _dtype_code(u), int(delta_softplus),
+                    int(forward_only), *(_strides(fn, t, 2) for t in (u, dt)),
+                    _strides(fn, z if z is not None else u, 2), _strides(fn, y, 2),
+                    _strides(fn, b, 3), _strides(fn, c, 3))
+    return _seen(d, u=u, dt=dt, z=z, y=y, b=b, c=c)
 
 
 def snn_selscan_saved_bytes(desc: SelscanDesc) -> int:
@@ -800,15 +822,17 @@ def snn_selscan_workspace_bytes(desc: SelscanDesc) -> int:
 
 
 def _need_selscan(fn, d, u, dt, a, b, c, skip, dt_bias, z, y, prefix=""):
-    rows, vecs = (d.T, d.B, d.n), (d.T, d.B, d.groups, d.states)
-    for what, t, st in (("u", u, d.u_stride), ("dt", dt, d.dt_stride), ("z", z, d.z_stride)):
-        _need_strided(fn, prefix + what, t, d.dtype, rows, st)
-    _need_strided(fn, "y or its gradient", y, d.dtype, rows, d.y_stride)
-    _need_strided(fn, prefix + "b", b, d.dtype, vecs, d.b_stride)
-    _need_strided(fn, prefix + "c", c, d.dtype, vecs, d.c_stride)
-    _need_array(fn, a, F32, d.states * d.n, prefix + "a")
-    _need_array(fn, skip, F32, d.n, prefix + "skip")
-    _need_array(fn, dt_bias, F32, d.n, prefix + "dt_bias")
+    n, code, seen = d.n, d.dtype, _layouts(d).get
+    rows, vecs = (d.T, d.B, n), (d.T, d.B, d.groups, d.states)
+    _need_strided(fn, prefix + "u", u, code, seen("u"), rows, d.u_stride)
+    _need_strided(fn, prefix + "dt", dt, code, seen("dt"), rows, d.dt_stride)
+    _need_strided(fn, prefix + "z", z, code, seen("z"), rows, d.z_stride)
+    _need_strided(fn, "y or its gradient", y, code, seen("y"), rows, d.y_stride)
+    _need_strided(fn, prefix + "b", b, code, seen("b"), vecs, d.b_stride)
+    _need_strided(fn, prefix + "c", c, code, seen("c"), vecs, d.c_stride)
+    _need_array(fn, a, F32, d.states * n, prefix + "a")
+    _need_array(fn, skip, F32, n, prefix + "skip")
+    _need_array(fn, dt_bias, F32, n, prefix + "dt_bias")
 
 
 def _need_bytes(fn, t, need, what):
@@ -876,8 +900,9 @@ def shortconv_desc(x, y, width, act="none") -> ShortconvDesc:
     if x.dim() != 3 or x.shape != y.shape or x.dtype != y.dtype:
         raise ValueError(f"{fn}: {tuple(x.shape)} {x.dtype} and {tuple(y.shape)} {y.dtype} do "
                          "not go together")
-    return ShortconvDesc(*x.shape, width, _GATE[act], _dtype_code(x), _strides(fn, x, 2),
-                         _strides(fn, y, 2))
+    d = ShortconvDesc(*x.shape, width, _GATE[act], _dtype_code(x), _strides(fn, x, 2),
+                      _strides(fn, y, 2))
+    return _seen(d, x=x, y=y)
 
 
 def snn_shortconv_workspace_bytes(desc: ShortconvDesc) -> int:
@@ -885,9 +910,9 @@ def snn_shortconv_workspace_bytes(desc: ShortconvDesc) -> int:
 
 
 def _need_shortconv(fn, d, x, w, bias, y, prefix=""):
-    rows = (d.T, d.B, d.n)
-    _need_strided(fn, prefix + "x", x, d.dtype, rows, d.x_stride)
-    _need_strided(fn, "y or its gradient", y, d.dtype, rows, d.y_stride)
+    rows, code, seen = (d.T, d.B, d.n), d.dtype, _layouts(d).get
+    _need_strided(fn, prefix + "x", x, code, seen("x"), rows, d.x_stride)
+    _need_strided(fn, "y or its gradient", y, code, seen("y"), rows, d.y_stride)
     _need_array(fn, w, F32, d.width * d.n, prefix + "w")
     _need_array(fn, bias, F32, d.n, prefix + "bias")
 
