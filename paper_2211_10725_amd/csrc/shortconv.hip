@@ -62,13 +62,24 @@ __device__ inline void input(const Shortconv &a, const Where &p, int i, float (&
     }
 }
 
+template <typename T, int V>
+__device__ inline void load_whole(Raw<T, V> &r, const T *p) {
+    __builtin_memcpy(r.w, p, sizeof(r.w));
+}
+
+// Groups of AHEAD tokens, the next group's rows on their way while one is run.  Those
+// whose rows all lie in the sequence and whose channels all are there (`whole`) go
+// without a condition: past a conditional store the compiler waits for every store before
+// it when it means to wait for the loads.
 template <typename T, int K>
 __global__ __launch_bounds__(kThreads) void shortconv_kernel(Shortconv a, int times) {
     constexpr int V = run_of<T>(), AHEAD = 4;
     const Where p = where<V>(a, times);
     if (p.m <= 0) return;
-    const int len = length_of(a, p.b), slice = p.group * kWaves + (threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = length_of(a, p.b), slice = p.group * kWaves + wave;
     const int begin = min(slice * a.slice, a.T), end = min(begin + a.slice, a.T);
+    const int whole = __all(p.m == V) ? min(end, len) : begin;
     float w[K][V], bias[V] = {}, win[K][V];  // win[K - 1]: this token
 #pragma unroll
     for (int j = 0; j < K; ++j) load_run(a.w + (int64_t)j * a.n + p.c, p.m, w[j]);
@@ -78,31 +89,55 @@ __global__ __launch_bounds__(kThreads) void shortconv_kernel(Shortconv a, int ti
         for (int j = 1; j < K; ++j) input<T, K>(a, p, begin - K + j, win[j]);
     T *y = static_cast<T *>(a.y) + p.y;
     const T *x = static_cast<const T *>(a.x.p) + p.x;
-    for (int t0 = begin; t0 < end; t0 += AHEAD) {
-        Raw<T, V> r[AHEAD];
+    Raw<T, V> r[AHEAD], next[AHEAD];
+    auto token = [&](const Raw<T, V> &row, float (&out)[V]) {
+#pragma unroll
+        for (int j = 0; j + 1 < K; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e];
+        row.get(win[K - 1]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            out[e] = bias[e];
+#pragma unroll
+            for (int j = 0; j < K; ++j) out[e] = __builtin_fmaf(w[j][e], win[j][e], out[e]);
+        }
+        if (a.silu)
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = silu<sizeof(T) == 4>(out[e]);
+    };
+    auto fetch = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int t = t0 + i;
-            r[i].load(x + t * a.x.st, t < end && t < len ? p.m : 0);
+            next[i].load(x + t * a.x.st, t < end && t < len ? p.m : 0);
+        }
+    };
+    fetch(begin);
+    for (int t0 = begin; t0 < end; t0 += AHEAD) {
+        for (; t0 + 2 * AHEAD <= whole; t0 += AHEAD) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) r[i] = next[i];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) load_whole(next[i], x + (t0 + AHEAD + i) * a.x.st);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                float out[V];
+                token(r[i], out);
+                store_run(y + (t0 + i) * a.y_st, V, out);
+            }
         }
 #pragma unroll
+        for (int i = 0; i < AHEAD; ++i) r[i] = next[i];
+        if (t0 + AHEAD < end) fetch(t0 + AHEAD);
+#pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int t = t0 + i;
-            if (t >= end) break;
+            if (t0 + i >= end) break;
             float out[V];
+            token(r[i], out);
 #pragma unroll
-            for (int j = 0; j + 1 < K; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e];
-            r[i].get(win[K - 1]);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                float s = bias[e];
-#pragma unroll
-                for (int j = 0; j < K; ++j) s = __builtin_fmaf(w[j][e], win[j][e], s);
-                out[e] = t < len ? (a.silu ? silu<sizeof(T) == 4>(s) : s) : 0.f;
-            }
-            store_run(y + t * a.y_st, p.m, out);
+            for (int e = 0; e < V; ++e) out[e] = t0 + i < len ? out[e] : 0.f;
+            store_run(y + (t0 + i) * a.y_st, p.m, out);
         }
     }
     // the last inputs, by the thread that also reads the state (which may be the same)
@@ -121,11 +156,12 @@ __global__ __launch_bounds__(kThreads) void shortconv_bwd_kernel(ShortconvBwd q,
     constexpr int AHEAD = 4;
     const Shortconv &a = q.a;
     const Where p = where<V>(a, times);
-    const int len = length_of(a, p.b), wave = threadIdx.x >> 6;
-    const int slice = p.group * kWaves + wave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = length_of(a, p.b), slice = p.group * kWaves + wave;
     const int begin = min(slice * a.slice, a.T), end = min(begin + a.slice, a.T);
     // the first slice goes on to the gradients of the state's rows
     const int stop = begin < end || slice == 0 ? end + K - 1 : begin;
+    const int whole = __all(p.m == V) ? min(end, len) : begin;
     float w[K][V] = {}, bias[V] = {}, win[K][V] = {}, ps[K][V] = {}, dw[K][V] = {}, db[V] = {};
     if (p.m > 0) {
 #pragma unroll
@@ -137,54 +173,86 @@ __global__ __launch_bounds__(kThreads) void shortconv_bwd_kernel(ShortconvBwd q,
     }
     const T *x = static_cast<const T *>(a.x.p) + p.x, *gy = static_cast<const T *>(q.gy) + p.y;
     T *gx = static_cast<T *>(q.gx) + p.x;
-    for (int t0 = begin; t0 < stop; t0 += AHEAD) {
-        Raw<T, V> rx[AHEAD], rg[AHEAD];
+    Raw<T, V> rx[AHEAD], rg[AHEAD], nx[AHEAD], ng[AHEAD];
+    // the window a token on: its p, where it lies in the sequence
+    auto token = [&](const Raw<T, V> &xrow, const Raw<T, V> &grow, bool in) {
+        float g[V];
+#pragma unroll
+        for (int j = 0; j + 1 < K; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e], ps[j][e] = ps[j + 1][e];
+        xrow.get(win[K - 1]);
+        grow.get(g);
+        if (a.silu)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float s = bias[e], act, slope;
+#pragma unroll
+                for (int j = 0; j < K; ++j) s = __builtin_fmaf(w[j][e], win[j][e], s);
+                silu_slope<sizeof(T) == 4>(s, act, slope);
+                g[e] *= slope;
+            }
+#pragma unroll
+        for (int e = 0; e < V; ++e) ps[K - 1][e] = in ? g[e] : 0.f;
+    };
+    auto add_sums = [&]() {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            db[e] += ps[K - 1][e];
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                dw[j][e] = __builtin_fmaf(ps[K - 1][e], win[j][e], dw[j][e]);
+        }
+    };
+    auto input_grad = [&](float (&out)[V]) {  // of the input that left the window
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            out[e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < K; ++j) out[e] = __builtin_fmaf(w[j][e], ps[K - 1 - j][e], out[e]);
+        }
+    };
+    auto fetch = [&](int t0) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int t = t0 + i, k = t < stop && t < len ? p.m : 0;
-            rx[i].load(x + t * a.x.st, k);
-            rg[i].load(gy + t * a.y_st, k);
+            nx[i].load(x + t * a.x.st, k);
+            ng[i].load(gy + t * a.y_st, k);
         }
+    };
+    fetch(begin);
+    for (int t0 = begin; t0 < stop; t0 += AHEAD) {
+        // whole groups, past the tokens whose window began in another slice (shortconv_kernel)
+        for (; t0 >= begin + K - 1 && t0 + 2 * AHEAD <= whole; t0 += AHEAD) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) rx[i] = nx[i], rg[i] = ng[i];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                load_whole(nx[i], x + (t0 + AHEAD + i) * a.x.st);
+                load_whole(ng[i], gy + (t0 + AHEAD + i) * a.y_st);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                float out[V];
+                token(rx[i], rg[i], true);
+                add_sums();
+                input_grad(out);
+                store_run(gx + (t0 + i - K + 1) * a.x.st, V, out);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) rx[i] = nx[i], rg[i] = ng[i];
+        if (t0 + AHEAD < stop) fetch(t0 + AHEAD);
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int t = t0 + i;
             if (t >= stop) break;
-            float g[V], out[V];
-#pragma unroll
-            for (int j = 0; j + 1 < K; ++j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) win[j][e] = win[j + 1][e], ps[j][e] = ps[j + 1][e];
-            rx[i].get(win[K - 1]);
-            rg[i].get(g);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                if (a.silu) {
-                    float s = bias[e], act, slope;
-#pragma unroll
-                    for (int j = 0; j < K; ++j) s = __builtin_fmaf(w[j][e], win[j][e], s);
-                    silu_slope<sizeof(T) == 4>(s, act, slope);
-                    g[e] *= slope;
-                }
-                if (t >= len) g[e] = 0.f;
-                ps[K - 1][e] = g[e];
-            }
-            if (t < end && t < len)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    db[e] += g[e];
-#pragma unroll
-                    for (int j = 0; j < K; ++j)
-                        dw[j][e] = __builtin_fmaf(g[e], win[j][e], dw[j][e]);
-                }
+            token(rx[i], rg[i], t < len);
+            if (t < end && t < len) add_sums();
             const int from = t - K + 1;  // the input that left the window
             if (from < begin && slice > 0) continue;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                float s = 0.f;
-#pragma unroll
-                for (int j = 0; j < K; ++j) s = __builtin_fmaf(w[j][e], ps[K - 1 - j][e], s);
-                out[e] = s;
-            }
+            float out[V];
+            input_grad(out);
             const int row = from - (len - K + 1);  // of the state after the sequence
             if (q.grad_state_out && row >= 0 && row < K - 1 && p.m > 0) {
                 float v[V];
