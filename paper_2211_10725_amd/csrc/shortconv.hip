@@ -29,7 +29,9 @@ struct Where {
     int b, c, m, group;  // sequence, first channel, channels, workgroup along time
     int64_t x, y;        // element offsets of (0, b, c)
 };
-template <int V>
+// SHIFT: the last run of a row, if it is short, starts early enough to be whole, and takes
+// some of its neighbour's channels along (the same values for them).
+template <int V, bool SHIFT>
 __device__ inline Where where(const Shortconv &a, int times) {
     Where p;
     const int cols = (a.n + kRuns * V - 1) / (kRuns * V);
@@ -39,6 +41,7 @@ __device__ inline Where where(const Shortconv &a, int times) {
     p.group = k % times;
     p.b = k / times;
     p.c = (col * kRuns + (threadIdx.x & 63)) * V;
+    if (SHIFT && p.c < a.n) p.c = max(0, min(p.c, a.n - V));
     p.m = min(V, max(0, a.n - p.c));
     p.x = p.b * a.x.sb + p.c;
     p.y = p.b * a.y_sb + p.c;
@@ -74,7 +77,7 @@ __device__ inline void load_whole(Raw<T, V> &r, const T *p) {
 template <typename T, int K>
 __global__ __launch_bounds__(kThreads) void shortconv_kernel(Shortconv a, int times) {
     constexpr int V = run_of<T>(), AHEAD = 4;
-    const Where p = where<V>(a, times);
+    const Where p = where<V, true>(a, times);
     if (p.m <= 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int len = length_of(a, p.b), slice = p.group * kWaves + wave;
@@ -130,6 +133,15 @@ __global__ __launch_bounds__(kThreads) void shortconv_kernel(Shortconv a, int ti
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) r[i] = next[i];
         if (t0 + AHEAD < end) fetch(t0 + AHEAD);
+        if (t0 + AHEAD <= whole) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                float out[V];
+                token(r[i], out);
+                store_run(y + (t0 + i) * a.y_st, V, out);
+            }
+            continue;
+        }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (t0 + i >= end) break;
@@ -155,7 +167,7 @@ template <typename T, int K, int V>
 __global__ __launch_bounds__(kThreads) void shortconv_bwd_kernel(ShortconvBwd q, int times) {
     constexpr int AHEAD = 4;
     const Shortconv &a = q.a;
-    const Where p = where<V>(a, times);
+    const Where p = where<V, false>(a, times);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int len = length_of(a, p.b), slice = p.group * kWaves + wave;
     const int begin = min(slice * a.slice, a.T), end = min(begin + a.slice, a.T);
@@ -349,15 +361,18 @@ __global__ __launch_bounds__(256) void shortconv_step_kernel(Shortconv a, const 
     store_run(y, m, out);
 }
 
-// Tokens of a thread: 32, fewer (not below the window) while that leaves the device
-// without eight waves to a compute unit.
+// Tokens of a thread: `most`, fewer (not below the window) while that leaves the device
+// with less than eight waves to a compute unit.  8 x 2048 tokens of 4096 bf16 channels:
+// forward in slices of 64 57 us (32: 60), backward, whose threads go on past their slice,
+// of 128 100 us (64: 108, 32: 107).
+constexpr int kMostFwd = 64, kMostBwd = 128;
 struct Plan {
     int slice, times, cols;
 };
-Plan plan_of(int T, int B, int n, int runs) {
+Plan plan_of(int T, int B, int n, int runs, int most) {
     Plan p;
     p.cols = (n + kRuns * runs - 1) / (kRuns * runs);
-    p.slice = 32;
+    p.slice = most;
     while (p.slice > 8 &&
            (int64_t)p.cols * B * ((T + kWaves * p.slice - 1) / (kWaves * p.slice)) < 2 * kPlanCus)
         p.slice /= 2;
@@ -367,14 +382,14 @@ Plan plan_of(int T, int B, int n, int runs) {
 
 template <typename T, int K>
 void run_fwd(const Shortconv &a, hipStream_t s) {
-    const Plan p = plan_of(a.T, a.B, a.n, run_of<T>());
+    const Plan p = plan_of(a.T, a.B, a.n, run_of<T>(), kMostFwd);
     Shortconv c = a;
     c.slice = p.slice;
     shortconv_kernel<T, K><<<(unsigned)(p.cols * p.times * a.B), kThreads, 0, s>>>(c, p.times);
 }
 template <typename T, int K>
 void run_bwd(const ShortconvBwd &q, hipStream_t s) {
-    const Plan p = plan_of(q.a.T, q.a.B, q.a.n, 4);
+    const Plan p = plan_of(q.a.T, q.a.B, q.a.n, 4, kMostBwd);
     ShortconvBwd c = q;
     c.a.slice = p.slice;
     if (q.a.B > 0)
@@ -409,7 +424,7 @@ void run_step(const Shortconv &a, const int32_t *slots, int n_slots, hipStream_t
 }  // namespace
 
 size_t shortconv_workspace_bytes(int T, int B, int n, int width) {
-    const Plan p = plan_of(T, B, n, 4);
+    const Plan p = plan_of(T, B, n, 4, kMostBwd);
     return align_up((size_t)p.times * B * (width + 1) * n * sizeof(float));
 }
 
