@@ -775,7 +775,10 @@ def _seen(desc, **tensors):
 
 def _layouts(desc):
     """What _seen kept, unless a field was changed since."""
-    return desc.layouts if getattr(desc, "fields", None) == bytes(desc) else {}
+    try:
+        return desc.layouts if desc.fields == bytes(desc) else {}
+    except AttributeError:  # a descriptor made by hand
+        return {}
 
 
 def _need_strided(fn, what, t, code, seen, shape, stride):
@@ -964,9 +967,18 @@ def layer_norm_desc(x, y=None, eps=1e-5) -> LayerNormDesc:
     n = x.shape[-1]
     if y is not None and y.shape != x.shape:
         raise ValueError(f"layer_norm_desc: shapes {tuple(x.shape)} and {tuple(y.shape)}")
-    return LayerNormDesc(x.numel() // n if n else 0, n, _dtype_code(x),
-                         _dtype_code(x if y is None else y), eps, _row_stride(x),
-                         n if y is None else _row_stride(y))
+    d = LayerNormDesc(x.numel() // n if n else 0, n, _dtype_code(x),
+                      _dtype_code(x if y is None else y), eps, _row_stride(x),
+                      n if y is None else _row_stride(y))
+    return _seen(d, x=x, y=y)
+
+
+def _need_norm_rows(fn, what, t, d, seen, code, ld):
+    """_need_rows, first by the layout kept with the descriptor."""
+    if t is None or seen is not None and t.__class__ is not int and t.dtype is seen[0] and \
+            t.shape == seen[1] and t.stride() == seen[2]:
+        return
+    _need_rows(fn, what, t, d, _torch_dtype(code), ld)
 
 
 def snn_layer_norm_workspace_bytes(desc: LayerNormDesc) -> int:
@@ -976,10 +988,11 @@ def snn_layer_norm_workspace_bytes(desc: LayerNormDesc) -> int:
 def snn_layer_norm_fwd(desc, x, w, b, y, stream=None):
     """y = (x - mean) / sqrt(var + eps) w + b over each row (w, b: None for ones, zeros)."""
     fn, d = "snn_layer_norm_fwd", desc
-    _need_rows(fn, "x", x, d, _torch_dtype(d.x_dtype), d.ld_x)
-    _need_rows(fn, "y", y, d, _torch_dtype(d.y_dtype), d.ld_y)
-    _need_array(fn, w, F32, d.n, "w")
-    _need_array(fn, b, F32, d.n, "b")
+    n, seen = d.n, _layouts(d).get
+    _need_norm_rows(fn, "x", x, d, seen("x"), d.x_dtype, d.ld_x)
+    _need_norm_rows(fn, "y", y, d, seen("y"), d.y_dtype, d.ld_y)
+    _need_array(fn, w, F32, n, "w")
+    _need_array(fn, b, F32, n, "b")
     _check(fn, lib().snn_layer_norm_fwd(ctypes.byref(d), _p(x), _p(w), _p(b), _p(y),
                                         _stream(stream)))
 
@@ -987,10 +1000,10 @@ def snn_layer_norm_fwd(desc, x, w, b, y, stream=None):
 def snn_layer_norm_bwd(desc, x, grad_y, grad_res, w, grad_x, grad_w, grad_b, ws, stream=None):
     """grad_x = grad_res (or None) + the norm's gradient; grad_w, grad_b sums over rows."""
     fn, d = "snn_layer_norm_bwd", desc
-    xt = _torch_dtype(d.x_dtype)
+    seen = _layouts(d).get
     for what, t in (("x", x), ("grad_res", grad_res), ("grad_x", grad_x)):
-        _need_rows(fn, what, t, d, xt, d.ld_x)
-    _need_rows(fn, "grad_y", grad_y, d, _torch_dtype(d.y_dtype), d.ld_y)
+        _need_norm_rows(fn, what, t, d, seen("x"), d.x_dtype, d.ld_x)
+    _need_norm_rows(fn, "grad_y", grad_y, d, seen("y"), d.y_dtype, d.ld_y)
     for what, t in (("w", w), ("grad_w", grad_w), ("grad_b", grad_b)):
         _need_array(fn, t, F32, d.n, what)
     _check(fn, lib().snn_layer_norm_bwd(
