@@ -576,10 +576,10 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                     h[t][k] = __builtin_fmaf(e[t][k], t ? h[t ? t - 1 : 0][k] : h0[k],
                                              uv * lane_of16<at + k>(vr));
                 });
-                if (a.z.p) {
-                    const float y = dot_lanes<at + H>(vr, h[t]);
-                    yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
-                }
+                // only the gate's gradient wants it: without a condition the tokens are one
+                // stretch of code
+                const float y = dot_lanes<at + H>(vr, h[t]);
+                yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
             });
             float part[4];
             each<kTile>([&](auto tt) {

@@ -255,12 +255,12 @@ def main():
     import torch
     T, B, n_in, classes = 100, 64, 96, 4
     net = SelectiveNet(n_in, n=128, width=256, states=16, blocks=2, n_out=classes, T=T, B=B)
-    net.init_adamw(lr=1e-3)
-    for i in range(100):
+    net.init_adamw(lr=5e-4)
+    for i in range(200):
         x, y = (torch.as_tensor(a).cuda() for a in spike_trains(T, B, n_in, classes, seed=i))
         loss = net.train_step(x, y)
         net.update()
-        if i % 10 == 9:
+        if i % 20 == 19:
             print(f"step {i:3d}  loss {loss.item():.4f}", flush=True)
     # a prompt of 60 steps, then the rest one by one, against the whole sequence
     states, whole = net.states(B), net.states(B)
