@@ -794,6 +794,19 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
     }
 }
 
+// `count` values `step` apart added in order, 16 on their way at a time
+__device__ inline float ordered_sum(const float *p, int64_t step, int count) {
+    float s = 0.f;
+    for (int k0 = 0; k0 < count; k0 += 16) {
+        float x[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = k0 + j < count ? p[(k0 + j) * step] : 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s += x[j];
+    }
+    return s;
+}
+
 // Gradients of b and c: the channel tiles' sums, in order; tokens past a sequence 0.
 template <typename T>
 __global__ __launch_bounds__(256) void selscan_vec_kernel(SelscanBwd q) {
@@ -807,8 +820,7 @@ __global__ __launch_bounds__(256) void selscan_vec_kernel(SelscanBwd q) {
     const int b = (int)(tb % a.B), t = (int)(tb / a.B);
     float s = 0.f;
     if (t < length_of(a, b)) {
-        const float *p = q.vec + which * tiles * per + e;
-        for (int k = 0; k < tiles; ++k) s += p[k * per];
+        s = ordered_sum(q.vec + which * tiles * per + e, per, tiles);
     }
     const SelscanVec &v = which ? q.dc : q.db;
     static_cast<T *>(const_cast<void *>(v.p))[t * v.st + b * v.sb + g * v.sg + i] = (T)s;
@@ -823,8 +835,7 @@ __global__ __launch_bounds__(256) void selscan_rows_kernel(SelscanBwd q, int row
     const int i = (int)(e / a.n);
     float *out = i < a.N ? q.grad_a : i == a.N ? q.grad_skip : q.grad_dt_bias;
     if (!out) return;
-    float s = 0.f;
-    for (int k = 0; k < rows; ++k) s += q.part[k * size + e];
+    const float s = ordered_sum(q.part + e, size, rows);
     out[i < a.N ? e : e % a.n] = s;
 }
 
