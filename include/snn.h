@@ -647,12 +647,13 @@ snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t l
  *     h_t[i,c] = exp(d_t[c] a[i,c]) h_{t-1}[i,c] + d_t[c] u_t[c] b_t[g,i]
  *     y_t[c]   = (sum_i c_t[g,i] h_t[i,c] + skip[c] u_t[c]) silu(z_t[c])
  * with channel c in group g = c / (n / groups).  b and c are [T,B,groups,states]
- * with stride [time, sequence, group].  a is fp32 [states,n], meant to be negative;
- * states of a sequence or slot are fp32 [states,n]. */
+ * with stride [time, sequence, group].  a is fp32 [states,n], finite, meant to be
+ * negative; states of a sequence or slot are fp32 [states,n]. */
 typedef struct snn_selscan_desc {
     int32_t T, B;           /* tokens, sequences (snn_selscan_step: T = 1) */
     int32_t n, states;      /* channels; integrators of each, 1 .. 64 */
-    int32_t groups;         /* divides n; B groups < 2^24 */
+    int32_t groups;         /* divides n; B times the 64-channel tiles of all groups
+                               < 2^24 */
     int32_t dtype;          /* u, dt, z, b, c, y, their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
     int32_t delta_softplus; /* 0 or 1 */
     int32_t forward_only;   /* 1: no backward will follow (a prompt), which then is

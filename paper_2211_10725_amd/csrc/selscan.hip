@@ -4,28 +4,39 @@
 //     h_t[i] = exp(d_t a[i]) h_{t-1}[i] + d_t u_t b_t[i],   y_t = c_t . h_t + skip u_t
 //
 // Every decay is a channel's and an integrator's own, so nothing here is a matrix
-// product: a token costs each integrator an exponential and four multiply-adds, and
-// the vector unit bounds it.  The kernels are laid out for that: a lane is a channel,
-// so that the four integrators a wave holds of it need no exchange between lanes, and
-// the waves of a workgroup hold further integrators of the same 64 channels.  16 tokens
-// at a time: the workgroup stages their steps d and d u (one softplus for all of a
-// channel's integrators) and b and c in LDS, the waves run through them, and what they
-// add to each (token, channel) is summed over the waves through LDS, in order.
+// product: a token costs each integrator an exponential (two issue slots) and four
+// multiply-adds, and the vector unit bounds it, at 24 cycles for 64 lanes; 8 x 2048 tokens
+// of 2048 channels of 16 integrators take at least 82 us forward and, with 11 slots more
+// and the states computed again, 250 backward.  A lane is a channel, so that the two
+// integrators a wave holds of it need no exchange between lanes, and the waves of a
+// workgroup hold further integrators of the same 64 channels (rounds of 16 where there are
+// more).  16 tokens at a time: the workgroup stages their steps d and d u (one softplus for
+// all of a channel's integrators) and b and c in LDS, the waves run through them, and what
+// they add to each (token, channel) is summed over the waves through LDS, in order.
+//
+// Two integrators in eight waves: the 256 workgroups of the sizes above leave a SIMD two
+// waves (with four integrators in four waves one: forward 256 us against 228, backward 852
+// against 722 at that time).  Also tried: two buffers of staged tiles with the next one
+// staged before the barrier (forward 236, backward 632 against 228 and 610; fp32 76 against
+// 64), a tile's values prepared before the last one is stored (272, 1055: registers).
 //
 // Few channels and long sequences: the sequence is cut into segments.  A first pass
 // leaves each segment's end state from a zero start and its sum of steps (over a
 // segment the decay is exp(a sum d)), a second joins them, the third runs every segment
-// from its true start.
+// from its true start: 16384 tokens of 2048 channels, bf16, 118 + 7 + 165 us.
 //
 // Backward, tile by tile from the end: the forward left the states before each tile of
 // 16 tokens, the tile's states and decays are computed again into registers, then
 //     g_t = c_t gy_t + exp(d_{t+1} a) g_{t+1},   q = exp(d_t a) g_t h_{t-1},
 //     dc_t += gy_t h_t, db_t += d u g_t (sums over channels), d(d u) = b_t . g_t,
 //     d(d) += a q, da += d q.
-// The sums over channels are sums over lanes: 8 values of a token (4 integrators of b
-// and c) are halved three times by exchanges that leave each lane half of the values,
-// and joined with those of 7 more tokens, two instructions for a value of 64 lanes; the
-// workgroups' sums are added by another kernel in order.
+// The sums over channels are sums over lanes: the 4 values of a token (2 integrators of b
+// and c) are halved twice by exchanges that leave each lane half of the values, and joined
+// with those of 15 more tokens, two instructions for a value of 64 lanes; the workgroups'
+// sums are added by another kernel in order.  Times at the sizes above: forward 228 us,
+// backward 610, of which the reverse run takes about 265 (its sums over lanes 100), the
+// waves' sums 85, the rest staging and the states again; the vector unit is busy for two
+// thirds of it.
 #include <type_traits>
 
 #include "block_common.hpp"
@@ -931,14 +942,12 @@ hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
 
 template <typename T>
 hipError_t by_states(const Selscan &a, hipStream_t s) {
-    if (a.N <= 4) return run_fwd<T, 2, false>(a, s);
     if (a.N <= 8) return run_fwd<T, 4, false>(a, s);
     if (a.N <= 16) return run_fwd<T, 8, false>(a, s);
     return run_fwd<T, 8, true>(a, s);
 }
 template <typename T>
 hipError_t by_states(const SelscanBwd &q, hipStream_t s) {
-    if (q.a.N <= 4) return run_bwd<T, 2, false>(q, s);
     if (q.a.N <= 8) return run_bwd<T, 4, false>(q, s);
     if (q.a.N <= 16) return run_bwd<T, 8, false>(q, s);
     return run_bwd<T, 8, true>(q, s);

@@ -3,10 +3,11 @@
 //     y_t = act(bias + sum_j w_j x_{t-K+1+j})
 //
 // Bound by HBM: x is read and y written once.  A thread takes V neighbouring channels
-// (16 bytes of a row) over a slice of tokens, with the window of the last K - 1 inputs
-// in registers; four tokens' rows are on their way at a time.  Of a slice's rows only
-// the K - 1 before it are read twice (by the thread of the slice before, at about the
-// same time).
+// (16 bytes of a row, backward 4 channels) over a slice of tokens, with the window of the
+// last K - 1 inputs in registers; four tokens' rows are on their way while four are run.
+// Of a slice's rows only the K - 1 before it are read twice (by the thread of the slice
+// before, at about the same time).  8 x 2048 tokens of 4096 bf16 channels, 4 taps, silu:
+// forward 57 us (4.7 TB/s), backward 100 (4.0).
 //
 // Backward in one pass over x and grad_y: the thread goes on K - 1 tokens past its
 // slice, takes p = act'(.) grad_y again for each token from the window of x, and from
@@ -29,9 +30,10 @@ struct Where {
     int b, c, m, group;  // sequence, first channel, channels, workgroup along time
     int64_t x, y;        // element offsets of (0, b, c)
 };
-// SHIFT: the last run of a row, if it is short, starts early enough to be whole, and takes
-// some of its neighbour's channels along (the same values for them).
-template <int V, bool SHIFT>
+// The last run of a row, if it is short, starts early enough to be whole, and takes some
+// of its neighbour's channels along (the same values for them).  ALL: so do the threads
+// past the row, where every one has to go on to a barrier.
+template <int V, bool ALL>
 __device__ inline Where where(const Shortconv &a, int times) {
     Where p;
     const int cols = (a.n + kRuns * V - 1) / (kRuns * V);
@@ -41,7 +43,7 @@ __device__ inline Where where(const Shortconv &a, int times) {
     p.group = k % times;
     p.b = k / times;
     p.c = (col * kRuns + (threadIdx.x & 63)) * V;
-    if (SHIFT && p.c < a.n) p.c = max(0, min(p.c, a.n - V));
+    if (ALL || p.c < a.n) p.c = max(0, min(p.c, a.n - V));
     p.m = min(V, max(0, a.n - p.c));
     p.x = p.b * a.x.sb + p.c;
     p.y = p.b * a.y_sb + p.c;
@@ -77,7 +79,7 @@ __device__ inline void load_whole(Raw<T, V> &r, const T *p) {
 template <typename T, int K>
 __global__ __launch_bounds__(kThreads) void shortconv_kernel(Shortconv a, int times) {
     constexpr int V = run_of<T>(), AHEAD = 4;
-    const Where p = where<V, true>(a, times);
+    const Where p = where<V, false>(a, times);
     if (p.m <= 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int len = length_of(a, p.b), slice = p.group * kWaves + wave;
@@ -167,22 +169,20 @@ template <typename T, int K, int V>
 __global__ __launch_bounds__(kThreads) void shortconv_bwd_kernel(ShortconvBwd q, int times) {
     constexpr int AHEAD = 4;
     const Shortconv &a = q.a;
-    const Where p = where<V, false>(a, times);
+    const Where p = where<V, true>(a, times);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int len = length_of(a, p.b), slice = p.group * kWaves + wave;
     const int begin = min(slice * a.slice, a.T), end = min(begin + a.slice, a.T);
     // the first slice goes on to the gradients of the state's rows
     const int stop = begin < end || slice == 0 ? end + K - 1 : begin;
     const int whole = __all(p.m == V) ? min(end, len) : begin;
-    float w[K][V] = {}, bias[V] = {}, win[K][V] = {}, ps[K][V] = {}, dw[K][V] = {}, db[V] = {};
-    if (p.m > 0) {
+    float w[K][V], bias[V] = {}, win[K][V] = {}, ps[K][V] = {}, dw[K][V] = {}, db[V] = {};
 #pragma unroll
-        for (int j = 0; j < K; ++j) load_run(a.w + (int64_t)j * a.n + p.c, p.m, w[j]);
-        if (a.bias) load_run(a.bias + p.c, p.m, bias);
-        if (begin < len)
+    for (int j = 0; j < K; ++j) load_run(a.w + (int64_t)j * a.n + p.c, p.m, w[j]);
+    if (a.bias) load_run(a.bias + p.c, p.m, bias);
+    if (begin < len)
 #pragma unroll
-            for (int j = 1; j < K; ++j) input<T, K>(a, p, begin - K + j, win[j]);
-    }
+        for (int j = 1; j < K; ++j) input<T, K>(a, p, begin - K + j, win[j]);
     const T *x = static_cast<const T *>(a.x.p) + p.x, *gy = static_cast<const T *>(q.gy) + p.y;
     T *gx = static_cast<T *>(q.gx) + p.x;
     Raw<T, V> rx[AHEAD], rg[AHEAD], nx[AHEAD], ng[AHEAD];
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(kThreads) void shortconv_bwd_kernel(ShortconvBwd q,
             float out[V];
             input_grad(out);
             const int row = from - (len - K + 1);  // of the state after the sequence
-            if (q.grad_state_out && row >= 0 && row < K - 1 && p.m > 0) {
+            if (q.grad_state_out && row >= 0 && row < K - 1) {
                 float v[V];
                 load_run(q.grad_state_out + ((int64_t)p.b * (K - 1) + row) * a.n + p.c, p.m, v);
 #pragma unroll
