@@ -1339,17 +1339,18 @@ int64_t selscan_units(const snn_selscan_desc *d) {
 // workspace: segments' states and sums of steps, then (backward) the partial sums
 struct SelscanRoom {
     size_t slot, sums, vec, part;
-    size_t forward() const { return slot + sums; }
     size_t all() const { return slot + sums + vec + part; }
 };
 SelscanRoom selscan_room(const snn_selscan_desc *d) {
     SelscanRoom r{};
     if (d->n == 0 || d->B == 0) return r;
-    const SelscanPlan p = selscan_plan(d->T, selscan_units(d));
     const size_t row = (size_t)d->B * d->n * sizeof(float);
-    if (p.segs > 1) {
-        r.slot = align_up((size_t)p.segs * d->states * row);
-        r.sums = align_up((size_t)p.segs * row);
+    const SelscanPlan p = selscan_plan(d->T, selscan_units(d), true);
+    const int segs = std::max(selscan_plan(d->T, selscan_units(d), false).segs,
+                              d->forward_only ? 1 : p.segs);
+    if (segs > 1) {
+        r.slot = align_up((size_t)segs * d->states * row);
+        r.sums = align_up((size_t)segs * row);
     }
     if (!d->forward_only) {
         r.vec = align_up((size_t)2 * (selscan_tiles(d->n, d->groups) / d->groups) * d->T * d->B *
@@ -1366,12 +1367,12 @@ SelscanVec vec_of(const void *p, const int64_t *st) {
 
 Selscan selscan_args(const snn_selscan_desc *d, const void *u, const void *dt, const float *a,
                      const void *b, const void *c, const float *skip, const float *dt_bias,
-                     const void *z, const int32_t *lens) {
+                     const void *z, const int32_t *lens, bool backward) {
     Selscan s{};
     s.T = d->T, s.B = d->B, s.n = d->n, s.N = d->states, s.groups = d->groups;
     s.softplus = d->delta_softplus;
     s.tiles = selscan_tiles(d->n, d->groups);
-    const SelscanPlan p = selscan_plan(d->T, selscan_units(d));
+    const SelscanPlan p = selscan_plan(d->T, selscan_units(d), backward);
     s.segs = p.segs, s.seg_len = p.seg_len;
     s.lens = lens;
     s.u = rows_of(u, d->u_stride), s.dt = rows_of(dt, d->dt_stride), s.z = rows_of(z, d->z_stride);
@@ -1448,7 +1449,7 @@ snn_status snn_selscan_fwd(const snn_selscan_desc *d, const void *u, const void 
         return SNN_ERR_ALIGN;
     const SelscanRoom room = selscan_room(d);
     if (ws_bytes < room.all() || (room.all() > 0 && !ws)) return SNN_ERR_WORKSPACE;
-    Selscan s = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, lens);
+    Selscan s = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, lens, false);
     s.state_in = state_in;
     s.y = y;
     s.state_out = state_out;
@@ -1490,7 +1491,7 @@ snn_status snn_selscan_bwd(const snn_selscan_desc *d, const void *u, const void 
     const SelscanRoom room = selscan_room(d);
     if (ws_bytes < room.all() || (room.all() > 0 && !ws)) return SNN_ERR_WORKSPACE;
     SelscanBwd q{};
-    q.a = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, lens);
+    q.a = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, lens, true);
     q.gy = grad_y;
     q.saved = (const float *)saved;
     q.grad_state_out = grad_state_out;
@@ -1522,7 +1523,7 @@ snn_status snn_selscan_step(const snn_selscan_desc *d, const void *u, const void
     if (any_misaligned({a, skip, dt_bias, slots, state_in, state_out}) ||
         any_misaligned_rows(d->dtype, {u, dt, b, c, z, y}))
         return SNN_ERR_ALIGN;
-    Selscan s = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, nullptr);
+    Selscan s = selscan_args(d, u, dt, a, b, c, skip, dt_bias, z, nullptr, false);
     s.state_in = state_in;
     s.state_out = state_out;
     s.y = y;

@@ -446,7 +446,7 @@ struct SelscanPlan {
     int segs, seg_len;
 };
 int selscan_tiles(int n, int groups);
-SelscanPlan selscan_plan(int T, int64_t units);  // units: channel tiles by sequences
+SelscanPlan selscan_plan(int T, int64_t units, bool backward);  // units: channel tiles by sequences
 hipError_t launch_selscan(const Selscan &a, int dtype, hipStream_t s);
 hipError_t launch_selscan_bwd(const SelscanBwd &q, int dtype, hipStream_t s);
 hipError_t launch_selscan_step(const Selscan &a, const int32_t *slots, int n_slots, int dtype,
