@@ -32,7 +32,9 @@ struct Where {
 };
 // The last run of a row, if it is short, starts early enough to be whole, and takes some
 // of its neighbour's channels along (the same values for them).  ALL: so do the threads
-// past the row, where every one has to go on to a barrier.
+// past the row, where every one has to go on to a barrier.  The neighbour is one of the
+// same wave where the state is updated in place: another workgroup's would write it while
+// this one reads.
 template <int V, bool ALL>
 __device__ inline Where where(const Shortconv &a, int times) {
     Where p;
@@ -43,7 +45,8 @@ __device__ inline Where where(const Shortconv &a, int times) {
     p.group = k % times;
     p.b = k / times;
     p.c = (col * kRuns + (threadIdx.x & 63)) * V;
-    if (ALL || p.c < a.n) p.c = max(0, min(p.c, a.n - V));
+    const int least = a.state_in && a.state_in == a.state_out ? col * kRuns * V : 0;
+    if (ALL || p.c < a.n) p.c = max(least, min(p.c, a.n - V));
     p.m = min(V, max(0, a.n - p.c));
     p.x = p.b * a.x.sb + p.c;
     p.y = p.b * a.y_sb + p.c;

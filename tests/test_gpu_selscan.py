@@ -313,6 +313,30 @@ def test_infinite_and_huge_values_stay_in_their_token_and_channel():
     assert not torch.isfinite(c.y[9, 1, 4])
 
 
+@pytest.mark.parametrize("what", ["u", "step", "z", "gy"])
+def test_nan_shows_and_stays_in_its_channel(what):
+    """Forward: the channel's outputs from the token on (z: its own alone).  Backward: the
+    channel's gradients show it, other channels' du, ddt and dz do not."""
+    c = Case(20, 2, 70, 16, seed=11)
+    c.fwd()
+    c.bwd()
+    y, was = c.y.clone(), {k: c.got[k].clone() for k in ("du", "ddt", "dz")}
+    getattr(c, what)[9, 1, 4] = float("nan")
+    c.fwd()
+    c.bwd()
+    same = torch.ones_like(y, dtype=torch.bool)
+    if what == "z":
+        same[9, 1, 4] = False
+    elif what != "gy":
+        same[9:, 1, 4] = False
+    assert torch.equal(y[same], c.y[same]) and torch.isnan(c.y[~same]).all()
+    other = torch.ones_like(y, dtype=torch.bool)
+    other[:, 1, 4] = False
+    for k, v in was.items():
+        assert torch.equal(v[other], c.got[k][other]), k
+    assert torch.isnan(c.got["ddt"][9, 1, 4])
+
+
 def test_open_and_shut_steps():
     """Raw steps far from zero: softplus is the step itself, or almost nothing."""
     c = Case(18, 1, 8, 4, seed=10)

@@ -118,6 +118,18 @@ def test_state_in_place(T):
     assert torch.equal(c.y, y) and torch.equal(c.init, out)
 
 
+@pytest.mark.parametrize("n", [513, 519, 1030, 261])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_state_in_place_where_a_row_ends_within_a_run(n, dt):
+    """The last run's neighbour may belong to another workgroup."""
+    c = Case(5, 64, n, 4, dt=dt, seed=n, ragged=True)
+    c.fwd()
+    y, out = c.y.clone(), c.out.clone()
+    c.out = c.init
+    c.fwd()
+    assert torch.equal(c.y, y) and torch.equal(c.init, out)
+
+
 def test_same_call_same_bits_and_optional_outputs():
     c = Case(600, 3, 96, 4, dt="bf16")
     c.fwd()
