@@ -45,9 +45,10 @@ namespace snn {
 namespace {
 
 constexpr int kTile = kSelscanTile;  // tokens
-constexpr int kLanes = 64;           // channels of a workgroup
-constexpr int H = 2;                 // integrators of a wave
-constexpr int kSlots = 2 * H;        // its values of b and c for a token
+constexpr int kLanes = 64;
+constexpr int kChans = 32;           // channels of a workgroup, and of half a wave
+constexpr int H = 2;                 // integrators of a lane
+constexpr int kSlots = 2 * H;        // their values of b and c for a token
 
 // Where this workgroup works.
 struct Place {
@@ -55,7 +56,7 @@ struct Place {
 };
 __device__ inline Place place_of(const Selscan &a, int segs) {
     Place p;
-    int x = blockIdx.x;
+    int x = xcd_local_item();  // neighbours share lines of 64 channels: on one XCD
     p.tile = x % a.tiles;
     x /= a.tiles;
     p.seg = x % segs;
@@ -63,8 +64,8 @@ __device__ inline Place place_of(const Selscan &a, int segs) {
     const int per = a.tiles / a.groups, k = p.tile % per;
     p.g = p.tile / per;
     const int size = a.n / a.groups;
-    p.c0 = p.g * size + k * kLanes;
-    p.live = min(kLanes, size - k * kLanes);
+    p.c0 = p.g * size + k * kChans;
+    p.live = min(kChans, size - k * kChans);
     return p;
 }
 
@@ -92,12 +93,12 @@ __device__ inline Walk<T> walk_vec(const SelscanVec &x, int t, const Place &p, i
 // EL values of a row, all of a workgroup's 64 channels there or only m of these
 template <typename T, int EL>
 __device__ inline void fetch_run(Raw<T, EL> &r, const T *at, const Place &p, int m) {
-    if (p.live == kLanes) __builtin_memcpy(r.w, at, sizeof(r.w));
+    if (p.live == kChans) __builtin_memcpy(r.w, at, sizeof(r.w));
     else r.load(at, m);
 }
 template <typename T, int EL>
 __device__ inline void put_run(T *at, const Place &p, int m, const float (&v)[EL]) {
-    store_run(at, p.live == kLanes ? EL : m, v);
+    store_run(at, p.live == kChans ? EL : m, v);
 }
 
 // raw steps and their bias to steps, the condition outside the loop: one stretch of
@@ -114,16 +115,16 @@ __device__ inline void steps(int soft, float (&d)[EL], const float (&bias)[EL]) 
         }
 }
 
-// W waves of 64 channels, each with H integrators of them at once.
+// W waves, each with 2 H integrators of the 32 channels at once: H in each half.
 template <int W>
 struct Geo {
     static constexpr int kThreads = kLanes * W;
     static constexpr int kTok = 4 * W;           // threads that stage a token
-    static constexpr int kEl = kLanes / kTok;    // channels of such a thread
-    static constexpr int kRow = W * H;           // integrators at once
+    static constexpr int kEl = kChans / kTok;    // channels of such a thread
+    static constexpr int kRow = 2 * H * W;       // integrators at once
 };
 
-// b and c of a tile for a wave, 16 values to a register: token t's are the 2 H from
+// b and c of a tile for half a wave, 16 values to a register: token t's are the 2 H from
 // 2 H t on.  Every lane wants the same ones; a register read with its lanes' own 16
 // values (a quarter of the LDS traffic of a broadcast read) and the operand of an
 // instruction that takes one lane of 16 for all of them.
@@ -173,6 +174,44 @@ __device__ inline float dot_lanes(float v, const float (&x)[H]) {
     return r;
 }
 
+// Lanes add up pairs of registers so that half of the lanes go on with x's sum and half,
+// those with the bit BIT of their number set, with y's.  The other lane of a pair is the
+// one across BIT, for 4 across 7 and for 2 across 3 (a reversal is one instruction):
+// taken in the order 32, 16, 8, 4, 2, 1 it has every earlier bit in common.
+template <int BIT>
+__device__ inline float halve(float x, float y) {
+    if constexpr (BIT == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y),
+                                                        false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else if constexpr (BIT == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y),
+                                                        false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    } else {
+        // row_ror:8, row_half_mirror, quad_perm [3,2,1,0], quad_perm [1,0,3,2]
+        constexpr int kCtrl = BIT == 8 ? 0x128 : BIT == 4 ? 0x141 : BIT == 2 ? 0x1b : 0xb1;
+        const bool up = (threadIdx.x & BIT) != 0;
+        const float keep = up ? y : x, give = up ? x : y;
+        return keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), kCtrl,
+                                                                 0xf, 0xf, false));
+    }
+}
+
+// What the halves of a wave add to a token and channel.  Tokens come in pairs, either
+// way: `first` holds the one that came first, with the second each half of the lanes ends
+// with a token's sum, the even one's the lower, which lie side by side in LDS.
+template <int t, bool DOWN>
+__device__ inline void put_pair(float *tile, int lane, bool more, float &first, float v) {
+    if constexpr ((t % 2 == 1) == DOWN) {
+        first = v;
+    } else {
+        const float sum = DOWN ? halve<32>(v, first) : halve<32>(first, v);
+        float *at = tile + (t & ~1) * kChans + lane;
+        *at = more ? *at + sum : sum;
+    }
+}
+
 // OUT: outputs (and saved states), from a.slot's or the caller's start; else the end
 // state from zero and the sum of the steps, into a.slot and a.sums.
 template <typename T, int W, bool MANY, bool OUT>
@@ -180,30 +219,30 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
     using G = Geo<W>;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
-    __shared__ float2 sd[kTile][kLanes];
-    __shared__ Vecs vecs[RND][W];
-    __shared__ float yp[OUT ? W : 1][kTile][kLanes];
-    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
-    const int tid = threadIdx.x, lane = tid & 63;
+    __shared__ float2 sd[kTile][kChans];
+    __shared__ Vecs vecs[RND][2 * W];
+    __shared__ float yp[OUT ? W : 1][kTile][kChans];
+    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kChans];
+    const int tid = threadIdx.x, lane = tid & 63, ch = lane & 31, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;  // staging
     const Place p = place_of(a, OUT ? a.segs : a.segs - 1);
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
     const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
     const int m = min(EL, max(0, p.live - se));
-    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;  // state [b][0][c]
-    const bool on = lane < p.live;
+    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + ch;  // state [b][0][c]
+    const bool on = ch < p.live;
     const float *first = OUT && a.segs > 1
                              ? a.slot + (int64_t)p.seg * a.B * a.N * a.n
                              : OUT ? a.state_in : nullptr;
     float h[H], a2[H];
-    auto state = [&](int r, int k) { return r * ROW + w * H + k; };
+    auto state = [&](int r, int k) { return r * ROW + (2 * w + half) * H + k; };
     auto load_round = [&](int r) {
 #pragma unroll
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             const bool in = on && i < a.N;
-            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
             h[k] = in && first ? first[sbase + (int64_t)i * a.n] : 0.f;
         }
     };
@@ -211,7 +250,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
         for (int r = 0; r < rounds; ++r) {
             load_round(r);
 #pragma unroll
-            for (int k = 0; k < H; ++k) carry[state(r, k)][lane] = h[k];
+            for (int k = 0; k < H; ++k) carry[state(r, k)][ch] = h[k];
         }
     } else {
         load_round(0);
@@ -281,8 +320,8 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
 #pragma unroll
                 for (int k = 0; k < H; ++k) {
                     const int i = state(r, k);
-                    a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
-                    h[k] = carry[i][lane];
+                    a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
+                    h[k] = carry[i][ch];
                 }
             }
             if (OUT && a.saved) {
@@ -291,24 +330,22 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
                 for (int k = 0; k < H; ++k)
                     if (on && state(r, k) < a.N) s[(int64_t)state(r, k) * a.n] = h[k];
             }
-            float vr = 0.f;
+            float vr = 0.f, pair = 0.f;
+            (void)pair;
             each<kTile>([&](auto tt) {
                 constexpr int t = decltype(tt)::value, at = t * kSlots % 16;
-                if constexpr (at == 0) vr = vecs[r][w][t * kSlots / 16][lane & 15];
-                const float2 v = sd[t][lane];
+                if constexpr (at == 0) vr = vecs[r][2 * w + half][t * kSlots / 16][lane & 15];
+                const float2 v = sd[t][ch];
                 each<H>([&](auto kk) {
                     constexpr int k = decltype(kk)::value;
                     const float e = __builtin_amdgcn_exp2f(v.x * a2[k]);
                     h[k] = __builtin_fmaf(e, h[k], v.y * lane_of16<at + k>(vr));
                 });
-                if constexpr (OUT) {
-                    const float y = dot_lanes<at + H>(vr, h);
-                    yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
-                }
+                if constexpr (OUT) put_pair<t, false>(&yp[w][0][0], lane, MANY && r, pair, dot_lanes<at + H>(vr, h));
             });
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < H; ++k) carry[state(r, k)][lane] = h[k];
+                for (int k = 0; k < H; ++k) carry[state(r, k)][ch] = h[k];
             }
         }
         __syncthreads();
@@ -345,18 +382,18 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
             for (int k = 0; k < H; ++k) {
                 const int i = state(r, k);
                 if (on && i < a.N)
-                    last[sbase + (int64_t)i * a.n] = MANY ? carry[i][lane] : h[k];
+                    last[sbase + (int64_t)i * a.n] = MANY ? carry[i][ch] : h[k];
             }
     if (!OUT) {  // the steps' sum: over the staging threads of a channel
         __syncthreads();
         float *s = &sd[0][0].x;
 #pragma unroll
-        for (int j = 0; j < EL; ++j) s[st * kLanes + se + j] = sum[j];
+        for (int j = 0; j < EL; ++j) s[st * kChans + se + j] = sum[j];
         __syncthreads();
-        if (w == 0 && on) {
+        if (w == 0 && half == 0 && on) {
             float t = 0.f;
-            for (int k = 0; k < kTile; ++k) t += s[k * kLanes + lane];
-            a.sums[((int64_t)p.seg * a.B + p.b) * a.n + p.c0 + lane] = t;
+            for (int k = 0; k < kTile; ++k) t += s[k * kChans + ch];
+            a.sums[((int64_t)p.seg * a.B + p.b) * a.n + p.c0 + ch] = t;
         }
     }
 }
@@ -393,71 +430,47 @@ __global__ __launch_bounds__(256) void selscan_join_kernel(Selscan a, const floa
 
 // ---- backward ------------------------------------------------------------------------
 
-// Lanes add up pairs of registers so that half of the lanes go on with x's sum and half,
-// those with the bit BIT of their number set, with y's.  The other lane of a pair is the
-// one across BIT, for 4 across 7 and for 2 across 3 (a reversal is one instruction):
-// taken in the order 32, 16, 8, 4, 2, 1 it has every earlier bit in common.
-template <int BIT>
-__device__ inline float halve(float x, float y) {
-    if constexpr (BIT == 32) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y),
-                                                        false, false);
-        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    } else if constexpr (BIT == 16) {
-        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y),
-                                                        false, false);
-        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    } else {
-        // row_ror:8, row_half_mirror, quad_perm [3,2,1,0], quad_perm [1,0,3,2]
-        constexpr int kCtrl = BIT == 8 ? 0x128 : BIT == 4 ? 0x141 : BIT == 2 ? 0x1b : 0xb1;
-        const bool up = (threadIdx.x & BIT) != 0;
-        const float keep = up ? y : x, give = up ? x : y;
-        return keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), kCtrl,
-                                                                 0xf, 0xf, false));
-    }
-}
-
 template <typename T, int W, bool MANY>
 __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(SelscanBwd q) {
     using G = Geo<W>;
     const Selscan &a = q.a;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
-    __shared__ float2 sd[kTile][kLanes];  // step, step times u
-    __shared__ float sg[kTile][kLanes];
-    __shared__ Vecs vecs[RND][W];
-    __shared__ float yp[W][kTile][kLanes], up[W][kTile][kLanes], dp[W][kTile][kLanes];
-    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
-    __shared__ float asum[MANY ? kSelscanMaxStates : 1][kLanes];
-    const int tid = threadIdx.x, lane = tid & 63;
+    __shared__ float2 sd[kTile][kChans];  // step, step times u
+    __shared__ float sg[kTile][kChans];
+    __shared__ Vecs vecs[RND][2 * W];
+    __shared__ float yp[W][kTile][kChans], up[W][kTile][kChans], dp[W][kTile][kChans];
+    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kChans];
+    __shared__ float asum[MANY ? kSelscanMaxStates : 1][kChans];
+    const int tid = threadIdx.x, lane = tid & 63, ch = lane & 31, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;
     const Place p = place_of(a, a.segs);
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
     const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
     const int m = min(EL, max(0, p.live - se));
-    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;
-    const bool on = lane < p.live;
+    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + ch;
+    const bool on = ch < p.live;
     const float *first = a.segs > 1 ? a.slot + (int64_t)p.seg * a.B * a.N * a.n
                                     : q.grad_state_out;
     float g[H], a2[H], acc[H];
-    auto state = [&](int r, int k) { return r * ROW + w * H + k; };
+    auto state = [&](int r, int k) { return r * ROW + (2 * w + half) * H + k; };
     for (int r = 0; r < (MANY ? rounds : 1); ++r)
 #pragma unroll
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             const bool in = on && i < a.N;
-            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
             g[k] = in && first ? first[sbase + (int64_t)i * a.n] : 0.f;
             acc[k] = 0.f;
-            if (MANY) carry[i][lane] = g[k], asum[i][lane] = 0.f;
+            if (MANY) carry[i][ch] = g[k], asum[i][ch] = 0.f;
         }
     float gskip[EL] = {}, gbias[EL] = {}, bias[EL] = {}, skip[EL] = {};
     if (a.dt_bias) load_run(a.dt_bias + p.c0 + se, m, bias);
     if (a.skip) load_run(a.skip + p.c0 + se, m, skip);
     float hs[H];  // the states before a tile, on their way while the one after it is run
     auto fetch_states = [&](int t0, int r) {
-        const float *s = q.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase - (on ? 0 : lane);
+        const float *s = q.saved + (int64_t)(t0 / kTile) * a.B * a.N * a.n + sbase - (on ? 0 : ch);
 #pragma unroll
         for (int k = 0; k < H; ++k) hs[k] = s[(int64_t)min(state(r, k), a.N - 1) * a.n];
     };
@@ -493,10 +506,10 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
     }
     // sums over this workgroup's channels: a lane's token and integrator
     const int per = a.tiles / a.groups;
-    const int vt = (lane >> 3 & 1) + (lane >> 1 & 2) + (lane << 1 & 4) + (lane & 1) * 8;
-    const int vi = w * H + (lane >> 4 & 1);
+    const int vt = (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4;
+    const int vi = (2 * w + half) * H + (lane >> 3 & 1);
     const int64_t vstep = (int64_t)a.B * a.groups * a.N;
-    const Walk<float> wv{q.vec + (((int64_t)(lane >> 5) * per + p.tile % per) * a.T + begin + vt) *
+    const Walk<float> wv{q.vec + (((int64_t)(lane >> 4 & 1) * per + p.tile % per) * a.T + begin + vt) *
                                      vstep +
                              (p.b * a.groups + p.g) * a.N + vi,
                          vstep};
@@ -562,22 +575,22 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                 h0[k] = hs[k];
                 if (MANY) {
                     a2[k] = on && i0 + k < a.N
-                                ? a.a[(int64_t)(i0 + k) * a.n + p.c0 + lane] * kLog2e
+                                ? a.a[(int64_t)(i0 + k) * a.n + p.c0 + ch] * kLog2e
                                 : 0.f;
-                    g[k] = carry[i0 + k][lane];
-                    acc[k] = asum[i0 + k][lane];
+                    g[k] = carry[i0 + k][ch];
+                    acc[k] = asum[i0 + k][ch];
                 }
             }
             if (!MANY && x > 0) fetch_states(t0 - kTile, 0);
             // the tile's values of this lane, for both directions
-            float vrs[kVecRows], gvs[kTile];
+            float vrs[kVecRows], gvs[kTile], pair[2];
             float2 dus[kTile];
 #pragma unroll
-            for (int k = 0; k < kVecRows; ++k) vrs[k] = vecs[r][w][k][lane & 15];
+            for (int k = 0; k < kVecRows; ++k) vrs[k] = vecs[r][2 * w + half][k][lane & 15];
 #pragma unroll
-            for (int t = 0; t < kTile; ++t) dus[t] = sd[t][lane];
+            for (int t = 0; t < kTile; ++t) dus[t] = sd[t][ch];
 #pragma unroll
-            for (int t = kTile - 1; t >= 0; --t) gvs[t] = sg[t][lane];
+            for (int t = kTile - 1; t >= 0; --t) gvs[t] = sg[t][ch];
             each<kTile>([&](auto tt) {
                 constexpr int t = decltype(tt)::value, at = t * kSlots % 16;
                 const float vr = vrs[t * kSlots / 16], dv = dus[t].x, uv = dus[t].y;
@@ -589,10 +602,9 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                 });
                 // only the gate's gradient wants it: without a condition the tokens are one
                 // stretch of code
-                const float y = dot_lanes<at + H>(vr, h[t]);
-                yp[w][t][lane] = MANY && r ? yp[w][t][lane] + y : y;
+                put_pair<t, false>(&yp[w][0][0], lane, MANY && r, pair[0], dot_lanes<at + H>(vr, h[t]));
             });
-            float part[4];
+            float part[3];
             each<kTile>([&](auto tt) {
                 constexpr int t = kTile - 1 - decltype(tt)::value, at = t * kSlots % 16;
                 const float vr = vrs[t * kSlots / 16], dv = dus[t].x, uv = dus[t].y, gv = gvs[t];
@@ -607,26 +619,27 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
                     acc[k] = __builtin_fmaf(x_, dv, acc[k]);
                     gd = __builtin_fmaf(x_, a2[k], gd);
                 }
-                up[w][t][lane] = MANY && r ? up[w][t][lane] + gin : gin;
-                dp[w][t][lane] = MANY && r ? dp[w][t][lane] + gd : gd;
-                // The sums over lanes.  Bits of the lane that a sum ends in: 32 b or c, 16
+                put_pair<t, true>(&up[w][0][0], lane, MANY && r, pair[0], gin);
+                put_pair<t, true>(&dp[w][0][0], lane, MANY && r, pair[1], gd);
+                // The sums over lanes.  Bits of the lane that a sum ends in: 16 b or c, 8
                 // the integrator's, then the token's from the low one on.  Tokens are joined
-                // in pairs, fours and so on.
-                float v = halve<16>(halve<32>(vb[0], vc[0]), halve<32>(vb[1], vc[1]));
-                each<4>([&](auto ll) {
+                // in pairs, fours and eights.
+                float v = halve<8>(halve<16>(vb[0], vc[0]), halve<16>(vb[1], vc[1]));
+                each<3>([&](auto ll) {
                     constexpr int l = decltype(ll)::value;
                     if constexpr ((t & ((1 << l) - 1)) == 0) {
                         if constexpr (t >> l & 1) part[l] = v;
-                        else v = halve<(8 >> l)>(v, part[l]);
+                        else v = halve<(4 >> l)>(v, part[l]);
                     }
                 });
-                if constexpr (t == 0) {
-                    if (t0 + vt < stop && vi + r * ROW < a.N) wv.tile(t0 - begin)[r * ROW] = v;
+                if constexpr (t % 8 == 0) {
+                    if (t0 + t + vt < stop && vi + r * ROW < a.N)
+                        wv.tile(t0 + t - begin)[r * ROW] = v;
                 }
             });
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < H; ++k) carry[i0 + k][lane] = g[k], asum[i0 + k][lane] = acc[k];
+                for (int k = 0; k < H; ++k) carry[i0 + k][ch] = g[k], asum[i0 + k][ch] = acc[k];
             }
         }
         __syncthreads();
@@ -656,23 +669,23 @@ __global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(S
     }
     // the gradient of the state before the segment, and the sums over its tokens
     float *last = p.seg == 0 ? q.grad_state_in : nullptr;
-    float *rows = q.part + ((int64_t)p.b * a.segs + p.seg) * (a.N + 2) * a.n + p.c0 + lane;
+    float *rows = q.part + ((int64_t)p.b * a.segs + p.seg) * (a.N + 2) * a.n + p.c0 + ch;
     for (int r = 0; r < (MANY ? rounds : 1); ++r)
 #pragma unroll
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             if (on && i < a.N) {
-                if (last) last[sbase + (int64_t)i * a.n] = MANY ? carry[i][lane] : g[k];
-                rows[(int64_t)i * a.n] = MANY ? asum[i][lane] : acc[k];
+                if (last) last[sbase + (int64_t)i * a.n] = MANY ? carry[i][ch] : g[k];
+                rows[(int64_t)i * a.n] = MANY ? asum[i][ch] : acc[k];
             }
         }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < EL; ++j) sd[st][se + j] = make_float2(gskip[j], gbias[j]);
     __syncthreads();
-    if (w == 0 && on) {
+    if (w == 0 && half == 0 && on) {
         float s0 = 0.f, s1 = 0.f;
-        for (int k = 0; k < kTile; ++k) s0 += sd[k][lane].x, s1 += sd[k][lane].y;
+        for (int k = 0; k < kTile; ++k) s0 += sd[k][ch].x, s1 += sd[k][ch].y;
         rows[(int64_t)a.N * a.n] = s0;
         rows[(int64_t)(a.N + 1) * a.n] = s1;
     }
@@ -686,10 +699,10 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
     const Selscan &a = q.a;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
     constexpr int RND = MANY ? kSelscanMaxStates / ROW : 1;
-    __shared__ float2 sd[kTile][kLanes];
-    __shared__ Vecs vecs[RND][W];
-    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kLanes];
-    const int tid = threadIdx.x, lane = tid & 63;
+    __shared__ float2 sd[kTile][kChans];
+    __shared__ Vecs vecs[RND][2 * W];
+    __shared__ float carry[MANY ? kSelscanMaxStates : 1][kChans];
+    const int tid = threadIdx.x, lane = tid & 63, ch = lane & 31, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int st = tid / TOK, se = tid % TOK * EL, si = tid % TOK;
     Place p = place_of(a, a.segs - 1);
@@ -697,22 +710,22 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
     const int len = length_of(a, p.b), rounds = (a.N + ROW - 1) / ROW;
     const int begin = p.seg * a.seg_len, end = min(a.T, begin + a.seg_len);
     const int m = min(EL, max(0, p.live - se));
-    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + lane;
-    const bool on = lane < p.live;
+    const int64_t sbase = ((int64_t)p.b * a.N) * a.n + p.c0 + ch;
+    const bool on = ch < p.live;
     float g[H], a2[H];
-    auto state = [&](int r, int k) { return r * ROW + w * H + k; };
+    auto state = [&](int r, int k) { return r * ROW + (2 * w + half) * H + k; };
     auto rates = [&](int r) {
 #pragma unroll
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
-            a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + lane] * kLog2e : 0.f;
+            a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
         }
     };
     rates(0);
 #pragma unroll
     for (int k = 0; k < H; ++k) g[k] = 0.f;
     if (MANY)
-        for (int i = w; i < kSelscanMaxStates; i += W) carry[i][lane] = 0.f;
+        for (int i = w; i < kSelscanMaxStates; i += W) carry[i][ch] = 0.f;
     float bias[EL], sum[EL];
 #pragma unroll
     for (int j = 0; j < EL; ++j) {
@@ -766,13 +779,13 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
             if (MANY) {
                 rates(r);
 #pragma unroll
-                for (int k = 0; k < H; ++k) g[k] = carry[i0 + k][lane];
+                for (int k = 0; k < H; ++k) g[k] = carry[i0 + k][ch];
             }
             float vr = 0.f;
             each<kTile>([&](auto tt) {
                 constexpr int t = kTile - 1 - decltype(tt)::value, at = t * kSlots % 16;
-                if constexpr (at + kSlots == 16) vr = vecs[r][w][t * kSlots / 16][lane & 15];
-                const float2 v = sd[t][lane];
+                if constexpr (at + kSlots == 16) vr = vecs[r][2 * w + half][t * kSlots / 16][lane & 15];
+                const float2 v = sd[t][ch];
                 each<H>([&](auto kk) {
                     constexpr int k = decltype(kk)::value;
                     fma_lane<at + H + k>(g[k], vr, v.y);
@@ -781,7 +794,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
             });
             if (MANY) {
 #pragma unroll
-                for (int k = 0; k < H; ++k) carry[i0 + k][lane] = g[k];
+                for (int k = 0; k < H; ++k) carry[i0 + k][ch] = g[k];
             }
         }
     }
@@ -791,17 +804,17 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
             const int i = state(r, k);
             if (on && i < a.N)
                 a.slot[(int64_t)p.seg * a.B * a.N * a.n + sbase + (int64_t)i * a.n] =
-                    MANY ? carry[i][lane] : g[k];
+                    MANY ? carry[i][ch] : g[k];
         }
     __syncthreads();
     float *s = &sd[0][0].x;
 #pragma unroll
-    for (int j = 0; j < EL; ++j) s[st * kLanes + se + j] = sum[j];
+    for (int j = 0; j < EL; ++j) s[st * kChans + se + j] = sum[j];
     __syncthreads();
-    if (w == 0 && on) {
+    if (w == 0 && half == 0 && on) {
         float t = 0.f;
-        for (int k = 0; k < kTile; ++k) t += s[k * kLanes + lane];
-        a.sums[((int64_t)p.seg * a.B + p.b) * a.n + p.c0 + lane] = t;
+        for (int k = 0; k < kTile; ++k) t += s[k * kChans + ch];
+        a.sums[((int64_t)p.seg * a.B + p.b) * a.n + p.c0 + ch] = t;
     }
 }
 
@@ -942,15 +955,15 @@ hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
 
 template <typename T>
 hipError_t by_states(const Selscan &a, hipStream_t s) {
-    if (a.N <= 8) return run_fwd<T, 4, false>(a, s);
-    if (a.N <= 16) return run_fwd<T, 8, false>(a, s);
-    return run_fwd<T, 8, true>(a, s);
+    if (a.N <= 8) return run_fwd<T, 2, false>(a, s);
+    if (a.N <= 16) return run_fwd<T, 4, false>(a, s);
+    return run_fwd<T, 4, true>(a, s);
 }
 template <typename T>
 hipError_t by_states(const SelscanBwd &q, hipStream_t s) {
-    if (q.a.N <= 8) return run_bwd<T, 4, false>(q, s);
-    if (q.a.N <= 16) return run_bwd<T, 8, false>(q, s);
-    return run_bwd<T, 8, true>(q, s);
+    if (q.a.N <= 8) return run_bwd<T, 2, false>(q, s);
+    if (q.a.N <= 16) return run_bwd<T, 4, false>(q, s);
+    return run_bwd<T, 4, true>(q, s);
 }
 
 template <typename T>
@@ -961,7 +974,7 @@ void run_step(const Selscan &a, const int32_t *slots, int n_slots, hipStream_t s
 }  // namespace
 
 int selscan_tiles(int n, int groups) {
-    return groups * ((n / groups + kLanes - 1) / kLanes);
+    return groups * ((n / groups + kChans - 1) / kChans);
 }
 
 // Workgroups of 64 channels of a sequence, and of segments of it while they leave three
@@ -972,8 +985,8 @@ int selscan_tiles(int n, int groups) {
 // segments for two 89 us, for four 96.
 SelscanPlan selscan_plan(int T, int64_t units, bool backward) {
     SelscanPlan p{1, std::max(T, 1)};
-    if (units < 1 || units > kPlanCus * 5 / 8) return p;
-    const int tiles = (T + kTile - 1) / kTile, most = backward ? 2 : 4;
+    if (units < 1 || units > kPlanCus * 5 / 4) return p;
+    const int tiles = (T + kTile - 1) / kTile, most = backward ? 4 : 8;
     const int segs = (int)std::min<int64_t>(most * kPlanCus / units, tiles / 4);
     if (segs < 2) return p;
     p.seg_len = (tiles + segs - 1) / segs * kTile;
