@@ -652,7 +652,7 @@ snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t l
 typedef struct snn_selscan_desc {
     int32_t T, B;           /* tokens, sequences (snn_selscan_step: T = 1) */
     int32_t n, states;      /* channels; integrators of each, 1 .. 64 */
-    int32_t groups;         /* divides n; B times the 64-channel tiles of all groups
+    int32_t groups;         /* divides n; B times the 32-channel tiles of all groups
                                < 2^24 */
     int32_t dtype;          /* u, dt, z, b, c, y, their gradients: SNN_F32 | SNN_F16 | SNN_BF16 */
     int32_t delta_softplus; /* 0 or 1 */

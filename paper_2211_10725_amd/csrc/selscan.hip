@@ -8,35 +8,38 @@
 // multiply-adds, and the vector unit bounds it, at 24 cycles for 64 lanes; 8 x 2048 tokens
 // of 2048 channels of 16 integrators take at least 82 us forward and, with 11 slots more
 // and the states computed again, 250 backward.  A lane is a channel, so that the two
-// integrators a wave holds of it need no exchange between lanes, and the waves of a
-// workgroup hold further integrators of the same 64 channels (rounds of 16 where there are
-// more).  16 tokens at a time: the workgroup stages their steps d and d u (one softplus for
-// all of a channel's integrators) and b and c in LDS, the waves run through them, and what
-// they add to each (token, channel) is summed over the waves through LDS, in order.
+// integrators it holds need no exchange between lanes; the halves of a wave and the waves
+// of a workgroup hold further integrators of the same 32 channels (rounds of 16 where there
+// are more).  16 tokens at a time: the workgroup stages their steps d and d u (one softplus
+// for all of a channel's integrators) and b and c in LDS, the waves run through them, and
+// what they add to each (token, channel) is summed over the halves by an exchange and over
+// the waves through LDS, in order.
 //
-// Two integrators in eight waves: the 256 workgroups of the sizes above leave a SIMD two
-// waves (with four integrators in four waves one: forward 256 us against 228, backward 852
-// against 722 at that time).  Also tried: two buffers of staged tiles with the next one
-// staged before the barrier (forward 236, backward 632 against 228 and 610; fp32 76 against
-// 64), a tile's values prepared before the last one is stored (272, 1055: registers).
+// At the sizes above 512 workgroups of four waves leave a SIMD two waves, of two
+// workgroups, one of which runs while the other stages a tile or adds up its sums (256
+// workgroups of 64 channels in eight waves: backward 592 us against 552, and half of
+// what they are in fp32, 512 x 16 tokens of 1024 channels, 161 against 144).  Also tried:
+// four integrators a lane in half as many waves (forward 256 against 228, backward 852 against
+// 722 at that time); two buffers of staged tiles, the next one staged before the barrier
+// (backward 632 against 610); a tile's values prepared before the last one is stored (1055:
+// registers); three waves of a SIMD backward, a tile's values read from LDS twice (these
+// sizes there and back 791 against 766, in fp32 230 against 202; four times as many
+// sequences 2374 against 2598).
 //
 // Few channels and long sequences: the sequence is cut into segments.  A first pass
 // leaves each segment's end state from a zero start and its sum of steps (over a
 // segment the decay is exp(a sum d)), a second joins them, the third runs every segment
-// from its true start: 16384 tokens of 2048 channels, bf16, 118 + 7 + 165 us.
+// from its true start: 16384 tokens of 2048 channels, bf16, 119 + 7 + 171 us.
 //
 // Backward, tile by tile from the end: the forward left the states before each tile of
 // 16 tokens, the tile's states and decays are computed again into registers, then
 //     g_t = c_t gy_t + exp(d_{t+1} a) g_{t+1},   q = exp(d_t a) g_t h_{t-1},
 //     dc_t += gy_t h_t, db_t += d u g_t (sums over channels), d(d u) = b_t . g_t,
 //     d(d) += a q, da += d q.
-// The sums over channels are sums over lanes: the 4 values of a token (2 integrators of b
-// and c) are halved twice by exchanges that leave each lane half of the values, and joined
-// with those of 15 more tokens, two instructions for a value of 64 lanes; the workgroups'
-// sums are added by another kernel in order.  Times at the sizes above: forward 228 us,
-// backward 610, of which the reverse run takes about 265 (its sums over lanes 100), the
-// waves' sums 85, the rest staging and the states again; the vector unit is busy for two
-// thirds of it.
+// The sums over channels are sums over the lanes of a half: the 4 values of a token (2
+// integrators of b and c) are halved twice by exchanges that leave each lane half of the
+// values, and joined with those of 7 more tokens, two to three instructions for a value of 64
+// lanes; the workgroups' sums are added by another kernel in order.
 #include <type_traits>
 
 #include "block_common.hpp"
@@ -431,7 +434,7 @@ __global__ __launch_bounds__(256) void selscan_join_kernel(Selscan a, const floa
 // ---- backward ------------------------------------------------------------------------
 
 template <typename T, int W, bool MANY>
-__global__ __launch_bounds__(kLanes * W, MANY ? 1 : 2) void selscan_bwd_kernel(SelscanBwd q) {
+__global__ __launch_bounds__(kLanes * W, 2) void selscan_bwd_kernel(SelscanBwd q) {
     using G = Geo<W>;
     const Selscan &a = q.a;
     constexpr int EL = G::kEl, ROW = G::kRow, TOK = G::kTok;
@@ -977,12 +980,10 @@ int selscan_tiles(int n, int groups) {
     return groups * ((n / groups + kChans - 1) / kChans);
 }
 
-// Workgroups of 64 channels of a sequence, and of segments of it while they leave three
-// eighths of the compute units idle: the forward's four to a unit (three are resident at
-// once), the backward's two (one after the other).  1024 tokens, 16 integrators, bf16, in
-// segments and uncut: 160 workgroups 98 us and 110 forward, 365 and 415 there and back;
-// 192 106 and 109, 463 and 417.  4096 tokens of 1024 channels (16 workgroups) backward: in
-// segments for two 89 us, for four 96.
+// Workgroups of 32 channels of a sequence, and of segments of it while they leave three
+// eighths of the places (two to a compute unit) empty: the forward's eight to a unit, the
+// backward's four.  1024 tokens, 16 integrators, bf16, there and back: 288 workgroups in
+// segments 310 us, 384 uncut 375, as any from 257 to 512.
 SelscanPlan selscan_plan(int T, int64_t units, bool backward) {
     SelscanPlan p{1, std::max(T, 1)};
     if (units < 1 || units > kPlanCus * 5 / 4) return p;

@@ -421,7 +421,7 @@ struct SelscanVec {   // element (t, b, g, i) at t st + b sb + g sg + i
 };
 struct Selscan {
     int T, B, n, N, groups, softplus;
-    int tiles;            // of 64 channels, none over two groups
+    int tiles;            // of 32 channels, none over two groups
     int segs, seg_len;    // of tokens; whole tiles of kSelscanTile
     const int32_t *lens;
     SelscanRows u, dt, z;  // z.p NULL: no gate
