@@ -956,6 +956,8 @@ hipError_t run_bwd(const SelscanBwd &q, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Two waves for up to 8 integrators: 512 x 64 tokens of 1024 channels of 8, bf16, there and
+// back 450 us, in four waves half of whose integrators are none 654 (512 x 16: 222, 209).
 template <typename T>
 hipError_t by_states(const Selscan &a, hipStream_t s) {
     if (a.N <= 8) return run_fwd<T, 2, false>(a, s);
