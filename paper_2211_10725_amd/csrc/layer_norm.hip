@@ -11,7 +11,7 @@
 // (two sums more, in registers too) instead of reading stored ones.  Workgroups take
 // rows in turn and hold the weights and the weights' sums of their rows; another kernel
 // adds the workgroups' sums in order.  16384 rows of 2048, bf16 from and to an fp32 stream:
-// forward 41 us (4.9 TB/s), backward with the stream's gradient 87 (5.4), 6.5 the sums.
+// forward 41 us (4.9 TB/s), backward with the stream's gradient 88 (5.3), 5 the sums.
 #include "block_common.hpp"
 
 namespace snn {
@@ -260,10 +260,13 @@ int threads_per_row(int n) {
     return t;
 }
 
-// Workgroups: as many as are resident at once, four of 256 threads to a compute unit.
-int row_blocks(int64_t rows, int64_t n) {
+// Workgroups: forward as many as are resident at once, four of 256 threads to a compute
+// unit (16384 rows of 2048 41 us, half as many 62), backward half as many, whose sums are
+// fewer to add (89 + 5 us against 89 + 6.5; 3201 rows of 1001 16 + 4.4 against 14 + 6.8).
+constexpr int kFwd = 4, kBwd = 2;
+int row_blocks(int64_t rows, int64_t n, int each) {
     const int t = threads_per_row((int)n), rpb = std::max(1, 256 / t);
-    const int64_t most = 4 * kPlanCus * 256 / std::max(256, t);
+    const int64_t most = (int64_t)each * kPlanCus * 256 / std::max(256, t);
     return (int)std::min<int64_t>((rows + rpb - 1) / rpb, most);
 }
 
@@ -277,14 +280,14 @@ int row_blocks(int64_t rows, int64_t n) {
 
 template <typename XT, typename YT>
 void run(const LayerNorm &c, hipStream_t s) {
-    const int n = c.n, grid = row_blocks(c.rows, n);
+    const int n = c.n, grid = row_blocks(c.rows, n, kFwd);
     if (grid > 0) {
         LAYER_NORM_SIZES(layer_norm_kernel, XT, YT)
     }
 }
 template <typename XT, typename YT>
 void run(const LayerNormBwd &c, hipStream_t s) {
-    const int n = c.a.n, grid = row_blocks(c.a.rows, n);
+    const int n = c.a.n, grid = row_blocks(c.a.rows, n, kBwd);
     if (grid > 0) {
         LAYER_NORM_SIZES(layer_norm_bwd_kernel, XT, YT)
     }
@@ -305,7 +308,7 @@ hipError_t by_types(const C &c, int xt, int yt, hipStream_t s) {
 }  // namespace
 
 size_t layer_norm_workspace_bytes(int64_t rows, int64_t n) {
-    return align_up((size_t)2 * row_blocks(rows, n) * n * sizeof(float));
+    return align_up((size_t)2 * row_blocks(rows, n, kBwd) * n * sizeof(float));
 }
 hipError_t launch_layer_norm(const LayerNorm &a, int xt, int yt, hipStream_t s) {
     return by_types(a, xt, yt, s);
