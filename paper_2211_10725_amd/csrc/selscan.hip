@@ -17,8 +17,8 @@
 //
 // At the sizes above 512 workgroups of four waves leave a SIMD two waves, of two
 // workgroups, one of which runs while the other stages a tile or adds up its sums (256
-// workgroups of 64 channels in eight waves: backward 592 us against 552, and half of
-// what they are in fp32, 512 x 16 tokens of 1024 channels, 161 against 144).  Also tried:
+// workgroups of 64 channels in eight waves: backward 592 us against 552; 512 x 16 tokens
+// of 1024 channels in fp32 161 against 144).  Also tried:
 // four integrators a lane in half as many waves (forward 256 against 228, backward 852 against
 // 722 at that time); two buffers of staged tiles, the next one staged before the barrier
 // (backward 632 against 610); a tile's values prepared before the last one is stored (1055:
@@ -93,7 +93,7 @@ __device__ inline Walk<T> walk_vec(const SelscanVec &x, int t, const Place &p, i
     return {static_cast<T *>(const_cast<void *>(x.p)) + t * x.st + p.b * x.sb + p.g * x.sg + i,
             x.st};
 }
-// EL values of a row, all of a workgroup's 64 channels there or only m of these
+// EL values of a row, all of a workgroup's channels there or only m of these
 template <typename T, int EL>
 __device__ inline void fetch_run(Raw<T, EL> &r, const T *at, const Place &p, int m) {
     if (p.live == kChans) __builtin_memcpy(r.w, at, sizeof(r.w));
