@@ -260,14 +260,15 @@ int threads_per_row(int n) {
     return t;
 }
 
-// Workgroups: forward as many as are resident at once, four of 256 threads to a compute
-// unit (16384 rows of 2048 41 us, half as many 62), backward half as many, whose sums are
-// fewer to add (89 + 5 us against 89 + 6.5; 3201 rows of 1001 16 + 4.4 against 14 + 6.8).
-constexpr int kFwd = 4, kBwd = 2;
-int row_blocks(int64_t rows, int64_t n, int each) {
+// Workgroups: as many as are resident at once, four of 256 threads to a compute unit
+// (forward of 16384 rows of 2048 41 us, half as many 62); backward half as many, whose sums
+// are fewer to add, where each takes eight turns at its rows or more (there and back 131 us
+// against 135; 3201 rows of 1001 28 against 26).
+int row_blocks(int64_t rows, int64_t n, bool backward) {
     const int t = threads_per_row((int)n), rpb = std::max(1, 256 / t);
-    const int64_t most = (int64_t)each * kPlanCus * 256 / std::max(256, t);
-    return (int)std::min<int64_t>((rows + rpb - 1) / rpb, most);
+    const int64_t turns = (rows + rpb - 1) / rpb;
+    const int64_t most = (int64_t)4 * kPlanCus * 256 / std::max(256, t);
+    return (int)std::min<int64_t>(turns, backward && turns >= 4 * most ? most / 2 : most);
 }
 
 #define LAYER_NORM_SIZES(KERNEL, ...)                                                          \
@@ -280,14 +281,14 @@ int row_blocks(int64_t rows, int64_t n, int each) {
 
 template <typename XT, typename YT>
 void run(const LayerNorm &c, hipStream_t s) {
-    const int n = c.n, grid = row_blocks(c.rows, n, kFwd);
+    const int n = c.n, grid = row_blocks(c.rows, n, false);
     if (grid > 0) {
         LAYER_NORM_SIZES(layer_norm_kernel, XT, YT)
     }
 }
 template <typename XT, typename YT>
 void run(const LayerNormBwd &c, hipStream_t s) {
-    const int n = c.a.n, grid = row_blocks(c.a.rows, n, kBwd);
+    const int n = c.a.n, grid = row_blocks(c.a.rows, n, true);
     if (grid > 0) {
         LAYER_NORM_SIZES(layer_norm_bwd_kernel, XT, YT)
     }
@@ -308,7 +309,7 @@ hipError_t by_types(const C &c, int xt, int yt, hipStream_t s) {
 }  // namespace
 
 size_t layer_norm_workspace_bytes(int64_t rows, int64_t n) {
-    return align_up((size_t)2 * row_blocks(rows, n, kBwd) * n * sizeof(float));
+    return align_up((size_t)2 * row_blocks(rows, n, true) * n * sizeof(float));
 }
 hipError_t launch_layer_norm(const LayerNorm &a, int xt, int yt, hipStream_t s) {
     return by_types(a, xt, yt, s);
