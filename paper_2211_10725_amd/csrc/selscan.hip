@@ -145,7 +145,8 @@ template <int L>
 __device__ inline float lane_of16(float v) {
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + L, 0xf, 0xf, true));
 }
-// acc + (lane L of 16 of v) x.  The wait is for a v that the instruction before wrote.
+// acc + (lane L of 16 of v) x.  The wait is for a v that the instruction before wrote; for
+// the result see settle.
 template <int L>
 __device__ inline void fma_lane(float &acc, float v, float x) {
     asm("s_nop 1\n\tv_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf"
@@ -177,6 +178,11 @@ __device__ inline float dot_lanes(float v, const float (&x)[H]) {
     return r;
 }
 
+// What one of the asm blocks above wrote, before lanes exchange it: the exchange may read a
+// register two wait states after a vector instruction wrote it, and the compiler counts
+// them for its own instructions only.
+__device__ inline void settle(float &x, float &y) { asm("s_nop 1" : "+v"(x), "+v"(y)); }
+
 // Lanes add up pairs of registers so that half of the lanes go on with x's sum and half,
 // those with the bit BIT of their number set, with y's.  The other lane of a pair is the
 // one across BIT, for 4 across 7 and for 2 across 3 (a reversal is one instruction):
@@ -203,12 +209,14 @@ __device__ inline float halve(float x, float y) {
 
 // What the halves of a wave add to a token and channel.  Tokens come in pairs, either
 // way: `first` holds the one that came first, with the second each half of the lanes ends
-// with a token's sum, the even one's the lower, which lie side by side in LDS.
-template <int t, bool DOWN>
+// with a token's sum, the even one's the lower, which lie side by side in LDS.  ASM: an asm
+// block wrote the values.
+template <int t, bool DOWN, bool ASM>
 __device__ inline void put_pair(float *tile, int lane, bool more, float &first, float v) {
     if constexpr ((t % 2 == 1) == DOWN) {
         first = v;
     } else {
+        if (ASM) settle(first, v);
         const float sum = DOWN ? halve<32>(v, first) : halve<32>(first, v);
         float *at = tile + (t & ~1) * kChans + lane;
         *at = more ? *at + sum : sum;
@@ -344,7 +352,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
                     const float e = __builtin_amdgcn_exp2f(v.x * a2[k]);
                     h[k] = __builtin_fmaf(e, h[k], v.y * lane_of16<at + k>(vr));
                 });
-                if constexpr (OUT) put_pair<t, false>(&yp[w][0][0], lane, MANY && r, pair, dot_lanes<at + H>(vr, h));
+                if constexpr (OUT) put_pair<t, false, true>(&yp[w][0][0], lane, MANY && r, pair, dot_lanes<at + H>(vr, h));
             });
             if (MANY) {
 #pragma unroll
@@ -605,7 +613,7 @@ __global__ __launch_bounds__(kLanes * W, 2) void selscan_bwd_kernel(SelscanBwd q
                 });
                 // only the gate's gradient wants it: without a condition the tokens are one
                 // stretch of code
-                put_pair<t, false>(&yp[w][0][0], lane, MANY && r, pair[0], dot_lanes<at + H>(vr, h[t]));
+                put_pair<t, false, true>(&yp[w][0][0], lane, MANY && r, pair[0], dot_lanes<at + H>(vr, h[t]));
             });
             float part[3];
             each<kTile>([&](auto tt) {
@@ -622,8 +630,8 @@ __global__ __launch_bounds__(kLanes * W, 2) void selscan_bwd_kernel(SelscanBwd q
                     acc[k] = __builtin_fmaf(x_, dv, acc[k]);
                     gd = __builtin_fmaf(x_, a2[k], gd);
                 }
-                put_pair<t, true>(&up[w][0][0], lane, MANY && r, pair[0], gin);
-                put_pair<t, true>(&dp[w][0][0], lane, MANY && r, pair[1], gd);
+                put_pair<t, true, true>(&up[w][0][0], lane, MANY && r, pair[0], gin);
+                put_pair<t, true, false>(&dp[w][0][0], lane, MANY && r, pair[1], gd);
                 // The sums over lanes.  Bits of the lane that a sum ends in: 16 b or c, 8
                 // the integrator's, then the token's from the low one on.  Tokens are joined
                 // in pairs, fours and eights.
