@@ -735,8 +735,11 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
     rates(0);
 #pragma unroll
     for (int k = 0; k < H; ++k) g[k] = 0.f;
+    // by the lanes that read them: a segment past the sequence's end has no barrier between
     if (MANY)
-        for (int i = w; i < kSelscanMaxStates; i += W) carry[i][ch] = 0.f;
+        for (int r = 0; r < rounds; ++r)
+#pragma unroll
+            for (int k = 0; k < H; ++k) carry[state(r, k)][ch] = 0.f;
     float bias[EL], sum[EL];
 #pragma unroll
     for (int j = 0; j < EL; ++j) {
