@@ -738,9 +738,9 @@ snn_status snn_shortconv_fwd(const snn_shortconv_desc *d, const void *x, const f
 
 /* Backward.  grad_y has y's strides; grad_state_out fp32 [B,width-1,n] or NULL for
  * zeros; grad_x (x's strides) is required; grad_w fp32 [width,n] and grad_bias fp32
- * [n] (sums over tokens and sequences in a fixed order) and grad_state_in (not
- * grad_state_out: SNN_ERR_UNSUPPORTED) may be NULL.  No output may overlap an input
- * or another output. */
+ * [n] (sums over tokens and sequences in a fixed order; (width + 1) n < 2^28 - 63) and
+ * grad_state_in (not grad_state_out: SNN_ERR_UNSUPPORTED) may be NULL.  No output may
+ * overlap an input or another output. */
 snn_status snn_shortconv_bwd(const snn_shortconv_desc *d, const void *x, const float *w,
                              const float *bias, const int32_t *lens, const float *state_in,
                              const void *grad_y, const float *grad_state_out, void *grad_x,

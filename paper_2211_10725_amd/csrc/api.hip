@@ -1388,8 +1388,9 @@ snn_status check_shortconv(const snn_shortconv_desc *d) {
     if (!float_dtype(d->dtype)) return SNN_ERR_DTYPE;
     if (d->act != SNN_GATE_NONE && d->act != SNN_GATE_SILU) return SNN_ERR_UNSUPPORTED;
     if (!strides_valid(d->x_stride, 2) || !strides_valid(d->y_stride, 2)) return SNN_ERR_SHAPE;
-    // workgroups of 256 threads for 256 channels and 32 tokens or more
-    if (d->T > ((int32_t)1 << 30) ||
+    // workgroups of 256 threads for 256 channels and 32 tokens or more; channels counted in
+    // 32 bits, in workgroups of up to 1024
+    if (d->T > ((int32_t)1 << 30) || d->n > INT32_MAX - 1023 ||
         ((int64_t)d->n + 255) / 256 * d->B > (kMostBlocks - 1) / (d->T / 32 + 1))
         return SNN_ERR_SHAPE;
     return SNN_OK;
@@ -1563,6 +1564,9 @@ snn_status snn_shortconv_bwd(const snn_shortconv_desc *d, const void *x, const f
     if (st != SNN_OK) return st;
     if (d->n == 0) return SNN_OK;
     if (grad_bias && !bias) return SNN_ERR_UNSUPPORTED;
+    // their sums over workgroups: 16 threads a channel and tap
+    if ((grad_w || grad_bias) && (int64_t)(d->width + 1) * d->n > (((int64_t)1 << 22) - 1) * 64)
+        return SNN_ERR_SHAPE;
     // the first tokens' threads write rows that others read as the last tokens'
     if (grad_state_in && grad_state_in == grad_state_out) return SNN_ERR_UNSUPPORTED;
     if (strided_overlap({d->T, d->B}, d->x_stride, d->n)) return SNN_ERR_SHAPE;

@@ -1,0 +1,47 @@
+"""Sizes of the selective leaky block that no launch takes, or that do not fit their
+counters, are refused on the host before any launch (no GPU needed; the addresses are never
+dereferenced)."""
+import ctypes
+
+import pytest
+
+import paper_2211_10725_amd as snn
+from tests.test_block_abi import ALIGN, OK, SHAPE
+
+torch = pytest.importorskip("torch")
+BIG = 1 << 62
+
+
+def _sc(T, B, n, width=8):
+    S = ctypes.c_int64 * 2
+    return snn.ShortconvDesc(T, B, n, width, snn.GATE_SILU, snn.F32, S(B * n, n), S(B * n, n))
+
+
+def _sc_bwd(d, gw=16, gb=16):
+    # a call that is right otherwise stops at grad_state_in's alignment
+    return snn.lib().snn_shortconv_bwd(ctypes.byref(d), 16, 16, 16, None, None, 16, None, 16, gw, gb,
+                                       17, 16, BIG, None)
+
+
+@pytest.mark.parametrize("width", [2, 4, 8])
+def test_sums_of_the_convolution_of_one_launch(width):
+    most = ((1 << 22) - 1) * 64 // (width + 1)  # 16 threads a tap and channel, below 2^32
+    assert _sc_bwd(_sc(1, 1, most, width)) == ALIGN
+    over = _sc(1, 1, most + 1, width)
+    assert _sc_bwd(over) == SHAPE
+    assert _sc_bwd(over, gw=None) == SHAPE and _sc_bwd(over, gb=None) == SHAPE
+    assert _sc_bwd(over, None, None) == ALIGN  # no sum is launched
+    assert snn.lib().snn_shortconv_fwd(ctypes.byref(over), 16, 16, 16, None, None, 16, 17,
+                                       None) == ALIGN
+
+
+def test_channels_of_the_convolution_are_counted_in_32_bits():
+    for n, want in ((2 ** 31 - 1, SHAPE), (2 ** 31 - 1023, SHAPE), (2 ** 31 - 1024, ALIGN)):
+        d = _sc(1, 1, n)
+        got = snn.lib().snn_shortconv_fwd(ctypes.byref(d), 16, 16, 16, None, None, 16, 17, None)
+        assert got == want, n
+        assert snn.lib().snn_shortconv_step(ctypes.byref(d), 16, 16, None, None, 1, 16, 17, 16,
+                                            None) == want
+        assert (snn.snn_shortconv_workspace_bytes(d) == 0) == (want == SHAPE)
+    assert snn.lib().snn_shortconv_fwd(ctypes.byref(_sc(1, 0, 2 ** 31 - 1024)), 16, 16, 16, None,
+                                       None, 16, None, None) == OK
