@@ -87,8 +87,7 @@ class SelectiveNet(SequenceNet):
     def _new_plan(self, T, B, train):
         torch = self.torch
         p = type("Plan", (), {})()
-        p.bufs, p.others, p.stays = [], {}, False
-        p.stream = snn._stream(None) if torch.device(self.device).type == "cuda" else None
+        p.bufs, p.stays = [], train
         L, n, m, N = len(self.W), self.n, self.width, self.n_states
 
         def new(*shape, dtype=torch.float32):

@@ -29,7 +29,11 @@ class SequenceNet:
     neurons.  checkpoints: what the backward needs of a block (its attention
     output and gate, its q, k, v and its normed input) is held in 8 bits between
     the passes, in one fourth of the memory; the gradients are then taken at the
-    values those stand for."""
+    values those stand for.
+
+    Prompts and steps may run on several streams at a time, each with states of its
+    own (calls that change the same states, or the parameters and gradients, have to
+    be ordered by the caller), and be captured into graphs."""
 
     def __init__(self, n_in, heads, kv_heads, d_k, d_v, blocks, n_out, T, B, beta=0.5,
                  slope=3.0, checkpoints=False, eps=1e-6, seed=0, device="cuda"):
@@ -76,26 +80,27 @@ class SequenceNet:
     # ---- buffers and descriptors of one shape -------------------------------
     def _plan(self, T, B, train=False):
         """Descriptors and buffers for T steps of B sequences (`train`: with what
-        the backward needs), kept for later calls of the shape.  Those of prompts
-        and steps hold at most four times the largest's memory together: the
-        longest unused go first, but never one that a graph was captured from."""
+        the backward needs), kept for later calls of the shape on the stream: calls
+        on two streams never share a buffer.  A call that is captured into a graph
+        has its own, in the graph's memory.  Those of one stream's prompts and steps
+        hold at most four times the largest's memory together: the longest unused
+        go first."""
         key = (T, B, train)
+        if self.torch.device(self.device).type == "cuda":
+            if self.torch.cuda.is_current_stream_capturing():
+                return self._new_plan(T, B, train)
+            key += (snn._stream(None),)
         p = self.plans.pop(key, None)
         made = p is None
         if made:
             p = self._new_plan(T, B, train)
         self.plans[key] = p  # the last one used is the last
-        if p.stream is not None:
-            stream = snn._stream(None)
-            if stream != p.stream and stream not in p.others:
-                p.others[stream] = self.torch.cuda.current_stream()
-            p.stays = p.stays or self.torch.cuda.is_current_stream_capturing()
         if made:
-            self._drop_plans(p)
+            self._drop_plans(p, key[3:])
         return p
 
-    def _drop_plans(self, newest):
-        old = {k: p for k, p in self.plans.items() if not k[2] and not p.stays}
+    def _drop_plans(self, newest, stream):
+        old = {k: p for k, p in self.plans.items() if k[3:] == stream and not p.stays}
         held = [p.bytes for p in old.values()]
         most, held, count = 4 * max(held, default=0), sum(held), len(held)
         for k, p in old.items():
@@ -103,15 +108,11 @@ class SequenceNet:
                 break
             del self.plans[k]
             held, count = held - p.bytes, count - 1
-            for t in p.bufs:  # their memory is free once those streams are done, too
-                for other in p.others.values():
-                    t.record_stream(other)
 
     def _new_plan(self, T, B, train):
         torch = self.torch
         p = type("Plan", (), {})()
-        p.bufs, p.others, p.stays = [], {}, False
-        p.stream = snn._stream(None) if torch.device(self.device).type == "cuda" else None
+        p.bufs, p.stays = [], train
         L = len(self.W)
 
         def new(*shape, dtype):
