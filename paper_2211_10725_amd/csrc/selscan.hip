@@ -104,6 +104,12 @@ __device__ inline void put_run(T *at, const Place &p, int m, const float (&v)[EL
     store_run(at, p.live == kChans ? EL : m, v);
 }
 
+// a log2 e, finite for every finite a: times a step of 0, as past a sequence, it has to be 0
+__device__ inline float rate(float a) {
+    const float x = a * kLog2e;
+    return __builtin_fabsf(x) > __FLT_MAX__ ? __builtin_copysignf(__FLT_MAX__, x) : x;
+}
+
 // raw steps and their bias to steps, the condition outside the loop: one stretch of
 // code in which the elements' chains overlap
 template <int EL>
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             const bool in = on && i < a.N;
-            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
+            a2[k] = in ? rate(a.a[(int64_t)i * a.n + p.c0 + ch]) : 0.f;
             h[k] = in && first ? first[sbase + (int64_t)i * a.n] : 0.f;
         }
     };
@@ -331,7 +337,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_kernel(Selscan a) {
 #pragma unroll
                 for (int k = 0; k < H; ++k) {
                     const int i = state(r, k);
-                    a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
+                    a2[k] = on && i < a.N ? rate(a.a[(int64_t)i * a.n + p.c0 + ch]) : 0.f;
                     h[k] = carry[i][ch];
                 }
             }
@@ -418,7 +424,7 @@ __global__ __launch_bounds__(256) void selscan_join_kernel(Selscan a, const floa
     const int64_t size = (int64_t)a.B * a.N * a.n;
     if (e >= size) return;
     const uint32_t row = e / (uint32_t)a.n, c = e - row * a.n, b = row / a.N, i = row - b * a.N;
-    const float a2 = a.a[(int64_t)i * a.n + c] * kLog2e;
+    const float a2 = rate(a.a[(int64_t)i * a.n + c]);
     float h = from ? from[e] : 0.f;
     constexpr int AHEAD = 8;  // segments on their way: one after the other they cost 12 us
     for (int k0 = 0; k0 < a.segs; k0 += AHEAD) {
@@ -471,7 +477,7 @@ __global__ __launch_bounds__(kLanes * W, 2) void selscan_bwd_kernel(SelscanBwd q
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
             const bool in = on && i < a.N;
-            a2[k] = in ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
+            a2[k] = in ? rate(a.a[(int64_t)i * a.n + p.c0 + ch]) : 0.f;
             g[k] = in && first ? first[sbase + (int64_t)i * a.n] : 0.f;
             acc[k] = 0.f;
             if (MANY) carry[i][ch] = g[k], asum[i][ch] = 0.f;
@@ -586,7 +592,7 @@ __global__ __launch_bounds__(kLanes * W, 2) void selscan_bwd_kernel(SelscanBwd q
                 h0[k] = hs[k];
                 if (MANY) {
                     a2[k] = on && i0 + k < a.N
-                                ? a.a[(int64_t)(i0 + k) * a.n + p.c0 + ch] * kLog2e
+                                ? rate(a.a[(int64_t)(i0 + k) * a.n + p.c0 + ch])
                                 : 0.f;
                     g[k] = carry[i0 + k][ch];
                     acc[k] = asum[i0 + k][ch];
@@ -729,7 +735,7 @@ __global__ __launch_bounds__(kLanes * W) void selscan_back_kernel(SelscanBwd q) 
 #pragma unroll
         for (int k = 0; k < H; ++k) {
             const int i = state(r, k);
-            a2[k] = on && i < a.N ? a.a[(int64_t)i * a.n + p.c0 + ch] * kLog2e : 0.f;
+            a2[k] = on && i < a.N ? rate(a.a[(int64_t)i * a.n + p.c0 + ch]) : 0.f;
         }
     };
     rates(0);
