@@ -755,6 +755,13 @@ def snn_checkpoint_load(ckpt, x, block=128, stream=None):
 # --------------------------------------------------------------------------
 # selective leaky block
 # --------------------------------------------------------------------------
+def _fit(fn, *sizes):
+    """A descriptor's sizes: a field of 32 bits would keep the rest of a larger one."""
+    if any(not 0 <= n < 1 << 31 for n in sizes):
+        raise ValueError(f"{fn}: sizes {sizes} do not fit 32 bits")
+    return sizes
+
+
 def _strides(fn, t, dims):
     """Strides of the leading `dims` dimensions of a tensor whose last is contiguous
     (0 for a dimension of one element: it has none to speak of)."""
@@ -809,8 +816,8 @@ def selscan_desc(u, dt, b, c, y, z=None, delta_softplus=True, forward_only=False
                          "together")
     if any(t is not None and t.dtype != u.dtype for t in (dt, b, c, y, z)):
         raise ValueError(f"{fn}: u, dt, b, c, y and z must have one dtype")
-    d = SelscanDesc(T, B, n, b.shape[3], b.shape[2], _dtype_code(u), int(delta_softplus),
-                    int(forward_only), *(_strides(fn, t, 2) for t in (u, dt)),
+    d = SelscanDesc(*_fit(fn, T, B, n, b.shape[3], b.shape[2]), _dtype_code(u),
+                    int(delta_softplus), int(forward_only), *(_strides(fn, t, 2) for t in (u, dt)),
                     _strides(fn, z if z is not None else u, 2), _strides(fn, y, 2),
                     _strides(fn, b, 3), _strides(fn, c, 3))
     return _seen(d, u=u, dt=dt, z=z, y=y, b=b, c=c)
@@ -903,7 +910,7 @@ def shortconv_desc(x, y, width, act="none") -> ShortconvDesc:
     if x.dim() != 3 or x.shape != y.shape or x.dtype != y.dtype:
         raise ValueError(f"{fn}: {tuple(x.shape)} {x.dtype} and {tuple(y.shape)} {y.dtype} do "
                          "not go together")
-    d = ShortconvDesc(*x.shape, width, _GATE[act], _dtype_code(x), _strides(fn, x, 2),
+    d = ShortconvDesc(*_fit(fn, *x.shape, width), _GATE[act], _dtype_code(x), _strides(fn, x, 2),
                       _strides(fn, y, 2))
     return _seen(d, x=x, y=y)
 
@@ -967,7 +974,7 @@ def layer_norm_desc(x, y=None, eps=1e-5) -> LayerNormDesc:
     n = x.shape[-1]
     if y is not None and y.shape != x.shape:
         raise ValueError(f"layer_norm_desc: shapes {tuple(x.shape)} and {tuple(y.shape)}")
-    d = LayerNormDesc(x.numel() // n if n else 0, n, _dtype_code(x),
+    d = LayerNormDesc(*_fit("layer_norm_desc", x.numel() // n if n else 0, n), _dtype_code(x),
                       _dtype_code(x if y is None else y), eps, _row_stride(x),
                       n if y is None else _row_stride(y))
     return _seen(d, x=x, y=y)

@@ -45,3 +45,31 @@ def test_channels_of_the_convolution_are_counted_in_32_bits():
         assert (snn.snn_shortconv_workspace_bytes(d) == 0) == (want == SHAPE)
     assert snn.lib().snn_shortconv_fwd(ctypes.byref(_sc(1, 0, 2 ** 31 - 1024)), 16, 16, 16, None,
                                        None, 16, None, None) == OK
+
+
+@pytest.mark.parametrize("shape", [((1 << 32) + 5, 2, 8), (2, (1 << 32) + 5, 8), ((1 << 31), 1, 8),
+                                   (1, 1, (1 << 32) + 8)], ids=str)
+def test_descriptors_refuse_sizes_past_32_bits(shape):
+    """The fields would hold what is left of them, and the call do that much."""
+    x = torch.empty(shape, device="meta")
+    v = torch.empty(*shape[:2], 1, 4, device="meta")
+    with pytest.raises(ValueError):
+        snn.selscan_desc(x, x, v, v, x, x)
+    with pytest.raises(ValueError):
+        snn.shortconv_desc(x, x, 4)
+    with pytest.raises(ValueError):
+        snn.layer_norm_desc(x)
+    with pytest.raises(ValueError):
+        snn.layer_norm_desc(x, x)
+
+
+def test_descriptors_refuse_other_fields_past_32_bits():
+    x = torch.empty(4, 2, 8)
+    with pytest.raises(ValueError):
+        snn.shortconv_desc(x, x, (1 << 32) + 4)
+    v = torch.empty(4, 2, 1, (1 << 32) + 16, device="meta")
+    with pytest.raises(ValueError):
+        snn.selscan_desc(x, x, v, v, x)
+    v = torch.empty(4, 2, (1 << 32) + 1, 16, device="meta")
+    with pytest.raises(ValueError):
+        snn.selscan_desc(x, x, v, v, x)
