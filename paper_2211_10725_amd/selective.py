@@ -153,8 +153,6 @@ class SelectiveNet(SequenceNet):
         """Embedding and blocks; conv(block, v, u) and scan(block, inputs, s) run their
         operators."""
         at = (lambda a, i: a[i % len(a)])
-        if spikes.data_ptr() % 16:  # a slice of a wider tensor: the synapse wants its alignment
-            spikes = spikes.clone()
         snn.snn_synapse_fwd(p.embed, spikes, self.E, None, p.x[0], None, p.ws)
         for i in range(len(self.W)):
             x, h, vz, dbc = at(p.x, i), at(p.h, i), at(p.vz, i), at(p.dbc, i)
@@ -176,7 +174,8 @@ class SelectiveNet(SequenceNet):
     def prompt(self, spikes, states, lens=None):
         """Whole sequences spikes [T,B,n_in] u8 from `states` (updated in place); returns
         the readout's currents [T,B,n_out], a tensor of their own.  lens: int32 [B]."""
-        p = self._plan(*spikes.shape[:2])
+        T, B = spikes.shape[:2]
+        spikes, p = self._spikes(spikes, T, B), self._plan(T, B)
 
         def conv(i, v, u):
             snn.snn_shortconv_fwd(p.conv, v, self.conv_w[i], self.conv_b[i], lens, states[i][0], u,
@@ -190,7 +189,8 @@ class SelectiveNet(SequenceNet):
     def step(self, spikes, states, slots=None):
         """One time step spikes [B,n_in] of running requests; request b's states lie in slot
         slots[b] (int32, or b), updated in place.  Returns the currents [B,n_out]."""
-        p = self._plan(1, spikes.shape[0])
+        B = spikes.shape[0]
+        spikes, p = self._spikes(spikes.unsqueeze(0), 1, B), self._plan(1, B)
 
         def conv(i, v, u):
             snn.snn_shortconv_step(p.conv, v, self.conv_w[i], self.conv_b[i], slots, states[i][0],
@@ -199,14 +199,15 @@ class SelectiveNet(SequenceNet):
         def scan(i, ins, s):
             snn.snn_selscan_step(p.scan, *ins, slots, states[i][1], states[i][1], s)
 
-        return self._currents(p, self._blocks(p, spikes.unsqueeze(0), conv, scan))[0]
+        return self._currents(p, self._blocks(p, spikes, conv, scan))[0]
 
     # ---- training ------------------------------------------------------------
     def train_step(self, spikes, labels):
         """Forward, cross-entropy on the readout's spike counts, and backward: gradients in
-        ``grads`` (of ``params``), the loss in the returned tensor.  spikes [T,B,n_in] u8 as
-        allocated, labels int32 [B]."""
+        ``grads`` (of ``params``), the loss in the returned tensor.  spikes [T,B,n_in] u8,
+        labels int32 [B]."""
         B, L, m = self.B, len(self.W), self.width
+        spikes, labels = self._spikes(spikes, self.T, B), self._labels(labels, B)
         p = self._plan(self.T, B, True)
         ins = [None] * L
 

@@ -171,6 +171,24 @@ class SequenceNet:
                 for _ in self.W]
 
     # ---- forward -------------------------------------------------------------
+    def _spikes(self, spikes, T, B):
+        """Spikes [T,B,n_in] as the synapse reads them, in one piece from an aligned
+        address: slices of other tensors are copied."""
+        if tuple(spikes.shape) != (T, B, self.n_in) or spikes.element_size() != 1 or \
+                spikes.device.type != self.R.device.type:
+            raise ValueError(f"spikes {tuple(spikes.shape)} {spikes.dtype} on {spikes.device}, not "
+                             f"{(T, B, self.n_in)} of bytes on {self.R.device}")
+        if spikes.data_ptr() % 16 or not spikes.is_contiguous():
+            spikes = spikes.clone(memory_format=self.torch.contiguous_format)
+        return spikes
+
+    def _labels(self, labels, B):
+        if labels.dtype is not self.torch.int32 or tuple(labels.shape) != (B,) or \
+                not labels.is_contiguous() or labels.device.type != self.R.device.type:
+            raise ValueError(f"labels {tuple(labels.shape)} {labels.dtype} on {labels.device}, not "
+                             f"int32 [{B}] on {self.R.device}")
+        return labels
+
     def _run(self, p, spikes, attend, train):
         """Embedding and blocks; attend(block, q, k, v, o) runs the attention."""
         L = len(self.W)
@@ -201,7 +219,7 @@ class SequenceNet:
         returns the readout's currents [T,B,n_out], a tensor of their own.  lens:
         int32 [B] lengths."""
         T, B = spikes.shape[:2]
-        p = self._plan(T, B)
+        spikes, p = self._spikes(spikes, T, B), self._plan(T, B)
 
         def attend(i, q, k, v, o):
             snn.snn_linattn_fwd(p.attn, q, k, v, self.decay, lens, states[i], o, states[i], p.ws)
@@ -213,18 +231,20 @@ class SequenceNet:
         lie in slot slots[b] (int32, or b) of `states`, updated in place.  Returns
         the currents [B,n_out]."""
         B = spikes.shape[0]
-        p = self._plan(1, B)
+        spikes, p = self._spikes(spikes.unsqueeze(0), 1, B), self._plan(1, B)
 
         def attend(i, q, k, v, o):
             snn.snn_linattn_step(p.attn, q, k, v, self.decay, slots, states[i], states[i], o)
 
-        return self._currents(p, self._run(p, spikes.unsqueeze(0), attend, False))[0]
+        return self._currents(p, self._run(p, spikes, attend, False))[0]
 
     # ---- training ------------------------------------------------------------
     def train_step(self, spikes, labels):
         """Forward, cross-entropy on the readout's spike counts, and backward:
-        gradients in ``grads`` (of ``params``), the loss in the returned tensor."""
+        gradients in ``grads`` (of ``params``), the loss in the returned tensor.
+        spikes [T,B,n_in] u8, labels int32 [B]."""
         T, B, L = self.T, self.B, len(self.W)
+        spikes, labels = self._spikes(spikes, T, B), self._labels(labels, B)
         p = self._plan(T, B, True)
 
         def attend(i, q, k, v, o):
