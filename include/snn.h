@@ -634,8 +634,10 @@ snn_status snn_checkpoint_load(int32_t rows, int32_t n, int32_t block, int64_t l
  * (t,b,c) lies at t stride[0] + b stride[1] + c, so they may be slices of wider
  * projections; they need only their element's alignment, and strides are >= 0 and
  * at most 2^32.  What is only read may be a broadcast (stride 0); of what is
- * written no two rows may share addresses (SNN_ERR_SHAPE).  Gradients have their
- * tensors' strides.  Arithmetic and states are fp32, each output rounded once.
+ * written no two rows may share addresses, and a stride that makes them (below the
+ * row's values, or another dimension's multiple) is SNN_ERR_SHAPE.  Gradients have
+ * their tensors' strides.  Arithmetic and states are fp32, each output rounded once;
+ * an infinite value makes what it reaches infinite or NaN.
  *
  * lens (device int32 [B], or NULL: every sequence has T tokens) gives each
  * sequence's length, taken as within [0, T]; tokens at and past it are not read,
@@ -755,7 +757,8 @@ snn_status snn_shortconv_step(const snn_shortconv_desc *d, const void *x, const 
                               hipStream_t stream);
 
 /* Layer norm, per row of n values:
- *     y = (x - mean) / sqrt(mean((x - mean)^2) + eps) w + b */
+ *     y = (x - mean) / sqrt(mean((x - mean)^2) + eps) w + b
+ * The sum of the squares is fp32: |x - mean| below 2^57. */
 typedef struct snn_layer_norm_desc {
     int32_t rows, n;        /* n 1 .. 16384 */
     int32_t x_dtype;        /* x, grad_x, grad_res: SNN_F32, or y_dtype */

@@ -68,7 +68,8 @@ __device__ inline void store_run(T *p, int m, const float (&v)[V]) {
 
 // e^x, within e^-150 .. e^88.5 (past that 1 + e^x is 1, or its reciprocal as good as
 // nothing).  FINE: to about 1e-7 of itself, 2^p e^(x - p ln 2) with p = fl(x log2 e);
-// else with p's error, |x| 2^-24, which a result of 16 bits does not show.
+// else with p's error, |x| 2^-24 of itself: for gates of 16-bit tensors, whose outputs of
+// 16 bits do not show it and whose sums of gradients in 32 bits have it in each term.
 template <bool FINE>
 __device__ inline float exp_of(float x) {
     if (!FINE) return __builtin_amdgcn_exp2f(fminf(x * kLog2e, 127.f));
@@ -92,7 +93,7 @@ __device__ inline void silu_slope(float z, float &act, float &slope) {
 
 // softplus log(1 + e^x) = max(x, 0) + log1p(e^-|x|) and its slope, the sigmoid.
 // log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by the series in s^2 to s^15 (the
-// next term is below 2^-31 of the sum): good to the last digits where e is small, as
+// next term is at most 2^-29.5 of the sum): good to the last digits where e is small, as
 // the logarithm of a rounded 1 + e is not.  Fine always: states of 32 bits come of it.
 __device__ inline void softplus(float x, float &value, float &slope) {
     const float e = exp_of<true>(-__builtin_fabsf(x));

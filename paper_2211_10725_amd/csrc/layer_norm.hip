@@ -263,9 +263,9 @@ int threads_per_row(int n) {
 // Workgroups: as many as are resident at once, four of 256 threads to a compute unit
 // (forward of 16384 rows of 2048 41 us, half as many 62); backward half as many, whose sums
 // are fewer to add, where each takes eight turns at its rows or more (there and back 131 us
-// against 135; 3201 rows of 1001 28 against 26) and two are left to a unit: of rows past
-// 2048 as many workgroups of more threads (backward of 8192 fp32 rows of 4096 80 us, half as
-// many 116; 4096 of 8192 115 and 192; 4096 of 12288 171 and 283).
+// against 135; 3201 rows of 1001 28 against 26) and two are left to a unit: rows past 2048
+// values keep all of theirs (backward of 8192 fp32 rows of 4096 80 us, half as many 116;
+// 4096 of 8192 115 and 192; 4096 of 12288 171 and 283).
 int row_blocks(int64_t rows, int64_t n, bool backward) {
     const int t = threads_per_row((int)n), rpb = std::max(1, 256 / t);
     const int64_t turns = (rows + rpb - 1) / rpb;

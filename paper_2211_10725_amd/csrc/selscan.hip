@@ -15,10 +15,10 @@
 // what they add to each (token, channel) is summed over the halves by an exchange and over
 // the waves through LDS, in order.
 //
-// At the sizes above 512 workgroups of four waves leave a SIMD two waves, of two
-// workgroups, one of which runs while the other stages a tile or adds up its sums (256
-// workgroups of 64 channels in eight waves: backward 592 us against 552; 512 x 16 tokens
-// of 1024 channels in fp32 161 against 144).  Also tried:
+// At the sizes above (forward 216 us, backward 533) 512 workgroups of four waves leave a
+// SIMD two waves, of two workgroups, one of which runs while the other stages a tile or
+// adds up its sums (256 workgroups of 64 channels in eight waves: backward 592 us where
+// these took 552; 512 x 16 tokens of 1024 channels in fp32 161 and 144).  Also tried:
 // four integrators a lane in half as many waves (forward 256 against 228, backward 852 against
 // 722 at that time); two buffers of staged tiles, the next one staged before the barrier
 // (backward 632 against 610); a tile's values prepared before the last one is stored (1055:
@@ -29,7 +29,8 @@
 // Few channels and long sequences: the sequence is cut into segments.  A first pass
 // leaves each segment's end state from a zero start and its sum of steps (over a
 // segment the decay is exp(a sum d)), a second joins them, the third runs every segment
-// from its true start: 16384 tokens of 2048 channels, bf16, 119 + 7 + 171 us.
+// from its true start: 16384 tokens of 2048 channels, bf16, 258 us, of which the first pass
+// takes two fifths.
 //
 // Backward, tile by tile from the end: the forward left the states before each tile of
 // 16 tokens, the tile's states and decays are computed again into registers, then
@@ -39,7 +40,10 @@
 // The sums over channels are sums over the lanes of a half: the 4 values of a token (2
 // integrators of b and c) are halved twice by exchanges that leave each lane half of the
 // values, and joined with those of 7 more tokens, two to three instructions for a value of 64
-// lanes; the workgroups' sums are added by another kernel in order.
+// lanes; the workgroups' sums are added by another kernel in order.  The sums over tokens,
+// of da and of skip's and dt_bias' gradients, are chains of T / 16 additions of a segment or
+// a sequence: a tile's terms are added up first, da's by themselves and the others by their
+// 16 threads at the end.
 #include <type_traits>
 
 #include "block_common.hpp"

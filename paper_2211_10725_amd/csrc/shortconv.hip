@@ -7,7 +7,8 @@
 // last K - 1 inputs in registers; four tokens' rows are on their way while four are run.
 // Of a slice's rows only the K - 1 before it are read twice (by the thread of the slice
 // before, at about the same time).  8 x 2048 tokens of 4096 bf16 channels, 4 taps, silu:
-// forward 57 us (4.7 TB/s), backward 100 (4.0).
+// forward 57 us (4.7 TB/s), backward 91 and its sums 5 (4.4; behind the forward of a
+// training pass about 110).
 //
 // Backward in one pass over x and grad_y: the thread goes on K - 1 tokens past its
 // slice, takes p = act'(.) grad_y again for each token from the window of x, and from
@@ -366,8 +367,8 @@ __global__ __launch_bounds__(256) void shortconv_step_kernel(Shortconv a, const 
 
 // Tokens of a thread: `most`, fewer (not below the window) while that leaves the device
 // with less than eight waves to a compute unit.  8 x 2048 tokens of 4096 bf16 channels:
-// forward in slices of 64 57 us (32: 60), backward, whose threads go on past their slice,
-// of 128 100 us (64: 108, 32: 107).
+// forward in slices of 64 57 us (32: 64), backward with its sums, whose threads go on past
+// their slice, of 128 95 us (64: 102, 32: 102).
 constexpr int kMostFwd = 64, kMostBwd = 128;
 struct Plan {
     int slice, times, cols;

@@ -47,6 +47,7 @@ def test_plans_of_two_streams_and_of_graphs_share_no_buffer(make):
             graphs.append(torch.cuda.CUDAGraph())
             with torch.cuda.graph(graphs[-1], stream=side):
                 kept.append(net._plan(T, 3, train))
+                kept[-1].ws.zero_()
             seen.append(_pointers(kept[-1]))
         assert len(set.union(*seen)) == sum(len(s) for s in seen)
         assert net._plan(T, 3, train) is here
